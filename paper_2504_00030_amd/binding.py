@@ -17,17 +17,18 @@ _PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_PKG, "lib", "libspecdecode.so")
 
 SPEC_OK, SPEC_EINVAL, SPEC_ESTATE, SPEC_ENOMEM, SPEC_EHIP, SPEC_ECAP, SPEC_ENOTIMPL = 0, -1, -2, -3, -4, -5, -6
-SPEC_F32, SPEC_BF16, SPEC_Q8 = 0, 1, 2
+SPEC_F32, SPEC_BF16, SPEC_Q8, SPEC_F8 = 0, 1, 2, 3
 ACCEPT_NATURAL, ACCEPT_FORCED = 0, 1
 PATH_AUTO, PATH_WAVEDOT, PATH_MFMA = 0, 1, 2
 GT_EXPAND_A, GT_LITERAL, GT_SHORT_TERM = 0, 1, 2
 
-# every symbol include/spec.h and include/gammatune.h declare
+# every symbol the headers in include/ declare
 EXPORTS = [
     "spec_init", "spec_prefill", "spec_prefill_ragged", "spec_debug_set_step", "spec_draft", "spec_draft_batch", "spec_verify", "spec_accept",
     "spec_set_forced_alpha", "spec_set_early_stop", "spec_generate", "spec_read_tokens", "spec_debug_logits",
     "spec_debug_drafted", "spec_debug_read", "spec_debug_fill_kv", "spec_debug_write_kv", "spec_debug_set_block_table", "spec_device_bytes", "spec_profile_kernel", "spec_profile_read", "spec_profile_read_class", "spec_debug_verify_rows", "spec_destroy",
     "spec_strerror", "spec_last_error", "spec_k_gemv", "spec_k_gemv_tiled", "spec_k_gemm_tiled", "spec_k_retile_q8", "spec_k_gemv_tiled_q8", "spec_k_gemm_tiled_q8", "spec_k_retile", "spec_k_copy", "spec_k_philox", "spec_k_accept", "spec_k_accept_static",
+    "spec_k_quant_f8", "spec_k_gemm_f8", "spec_k_gemm_f8_workspace", "spec_k_qk_norm_rope",
     "gammatune_init", "gammatune_update",
 ]
 
@@ -134,6 +135,13 @@ def load() -> C.CDLL:
     lib.spec_k_accept.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_int32, C.c_float, C.c_uint64,
                                   C.c_int32, C.c_void_p, C.c_void_p]
     lib.spec_k_accept_static.argtypes = lib.spec_k_accept.argtypes
+    vp, i32, i64 = C.c_void_p, C.c_int32, C.c_int64
+    lib.spec_k_quant_f8.argtypes = [vp, i32, i64, i32, i32, vp, vp, vp]
+    lib.spec_k_gemm_f8.argtypes = [vp, vp, i32, i32, vp, i32, i64, vp, i32, vp, i32, i64, vp, i64, vp]
+    lib.spec_k_gemm_f8_workspace.argtypes = [i32, i32, i32]
+    lib.spec_k_gemm_f8_workspace.restype = i64
+    lib.spec_k_qk_norm_rope.argtypes = [vp, i64, i32, vp, i64, i32, i32, i32, i32, vp, vp, C.c_float, vp, vp, i32, vp, vp, i64,
+                                        vp, i64, i32, vp]
     lib.gammatune_init.argtypes = [C.POINTER(GtState), C.POINTER(GtParams), C.c_int32]
     lib.gammatune_update.argtypes = [C.POINTER(GtState), C.c_int32, C.c_int32]
     lib.gammatune_update.restype = C.c_int32
@@ -479,3 +487,123 @@ def k_accept_static(p_logits, q_logits, drafted, temperature: float, seed: int, 
                                      temperature, seed, step, result.data_ptr(), stream)
     if rc != 0:
         raise SpecError(rc, "spec_k_accept_static", load().spec_last_error(None).decode())
+
+
+# ---- operators of an 8-bit checkpoint with normed heads (include/spec_ops.h) ------------------------------------------
+def _kind(t) -> int:
+    """Element type of a GPU tensor as the library names it."""
+    import torch
+    if t.dtype == torch.float32:
+        return SPEC_F32
+    if t.dtype == torch.bfloat16:
+        return SPEC_BF16
+    if t.dtype in (torch.float8_e4m3fn, torch.uint8):
+        return SPEC_F8
+    raise ValueError(f"unsupported element type {t.dtype}")
+
+
+def _flat(t, name: str, shape, dtypes):
+    """t is a contiguous tensor of this shape and one of these types; only data_ptr() is taken."""
+    if tuple(t.shape) != tuple(shape) or t.dtype not in dtypes or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {tuple(shape)} tensor of {dtypes}, not {tuple(t.shape)} of {t.dtype}")
+
+
+def _here(*tensors):
+    """The pointers belong to the current device."""
+    import torch
+    dev = torch.cuda.current_device() if torch.cuda.is_available() else -1
+    for t in tensors:
+        if not t.is_cuda or t.device.index != dev:
+            raise ValueError("operands must be tensors on the current GPU")
+
+
+def _rows(t, name: str) -> int:
+    """Row stride of a [R][n] tensor whose rows are contiguous."""
+    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError(f"{name} must be two-dimensional with contiguous rows")
+    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+
+
+def _ops_chk(rc: int, where: str):
+    if rc != 0:
+        raise SpecError(rc, where, load().spec_last_error(None).decode())
+
+
+def k_quant_f8(x, q, scale, stream: int = 0):
+    """Rows of x (fp32 or bf16 [R][K], any row stride) to e4m3: q [R][K] (float8_e4m3fn or uint8) and scale fp32
+    [ceil(K / 128)][R]."""
+    import torch
+    R, K = x.shape
+    ldx = _rows(x, "x")
+    _flat(q, "q", (R, K), (torch.float8_e4m3fn, torch.uint8))
+    _flat(scale, "scale", ((K + 127) // 128, R), (torch.float32,))
+    _here(x, q, scale)
+    _ops_chk(load().spec_k_quant_f8(x.data_ptr(), _kind(x), ldx, R, K, q.data_ptr(), scale.data_ptr(), stream),
+             "spec_k_quant_f8")
+
+
+def k_gemm_f8_workspace(K: int, R: int, x_dtype) -> int:
+    """Bytes of workspace k_gemm_f8 needs for R rows of K elements of this torch type."""
+    import torch
+    n = load().spec_k_gemm_f8_workspace(K, R, _kind(torch.empty(0, dtype=x_dtype)))
+    if n < 0:
+        raise SpecError(int(n), "spec_k_gemm_f8_workspace", load().spec_last_error(None).decode())
+    return int(n)
+
+
+def k_gemm_f8(w, w_scale, x, y, x_scale=None, workspace=None, stream: int = 0):
+    """y [R][N] (fp32 or bf16, any row stride) = x . w^T with w e4m3 [N][K] and w_scale fp32 [ceil(N / 128)][ceil(K / 128)].
+    x: e4m3 [R][K] with its x_scale as k_quant_f8 leaves them, or fp32 / bf16 rows, which the call quantises in
+    `workspace` (a GPU tensor of at least k_gemm_f8_workspace() bytes; more, up to 32 MiB, lets K be shared out)."""
+    import torch
+    N, K = w.shape
+    R = x.shape[0]
+    f8 = (torch.float8_e4m3fn, torch.uint8)
+    _flat(w, "w", (N, K), f8)
+    _flat(w_scale, "w_scale", ((N + 127) // 128, (K + 127) // 128), (torch.float32,))
+    if tuple(x.shape) != (R, K) or tuple(y.shape) != (R, N):
+        raise ValueError(f"x must be [R][{K}] and y [R][{N}], not {tuple(x.shape)} and {tuple(y.shape)}")
+    ldx, ldy = _rows(x, "x"), _rows(y, "y")
+    _here(w, w_scale, x, y)
+    if x_scale is not None:
+        _flat(x, "x", (R, K), f8)
+        _flat(x_scale, "x_scale", ((K + 127) // 128, R), (torch.float32,))
+        _here(x_scale)
+        ldx = K
+    nb = 0
+    if workspace is not None:
+        _here(workspace)
+        if not workspace.is_contiguous():
+            raise ValueError("workspace must be contiguous")
+        nb = workspace.numel() * workspace.element_size()
+    _ops_chk(load().spec_k_gemm_f8(w.data_ptr(), w_scale.data_ptr(), N, K, x.data_ptr(), _kind(x), ldx,
+                                   None if x_scale is None else x_scale.data_ptr(), R, y.data_ptr(), _kind(y), ldy,
+                                   None if workspace is None else workspace.data_ptr(), nb, stream), "spec_k_gemm_f8")
+
+
+def _heads(t, name: str, R: int, hd: int) -> int:
+    """Row stride of a [R][heads][hd] tensor whose rows hold their heads one after the other."""
+    if t.dim() != 3 or t.shape[0] != R or t.shape[2] != hd or (t.shape[1] > 1 and t.stride(1) != hd) or (hd > 1 and t.stride(2) != 1):
+        raise ValueError(f"{name} must be [{R}][heads][{hd}] with the heads of a row one after the other")
+    return t.stride(0) if R > 1 else max(t.stride(0), t.shape[1] * hd)
+
+
+def k_qk_norm_rope(q, k, q_norm, k_norm, cos, sin, pos, q_out, k_out, eps: float = 1e-5, stream: int = 0):
+    """RMS norm (weights q_norm, k_norm fp32 [hd]) and rotation of the heads of q [R][nq][hd] and k [R][nkv][hd] (fp32 or
+    bf16, views into fused rows included) into q_out, k_out (fp32 or bf16, may be the inputs).  cos, sin: fp32
+    [n_pos][hd / 2]; pos: int32 [R], rows with a position outside the tables are left as they were."""
+    import torch
+    R, nq, hd = q.shape
+    nkv = k.shape[1]
+    strides = [_heads(t, n, R, hd) for t, n in ((q, "q"), (k, "k"), (q_out, "q_out"), (k_out, "k_out"))]
+    if q.dtype != k.dtype or q_out.dtype != k_out.dtype or q_out.shape != q.shape or k_out.shape != k.shape:
+        raise ValueError("q and k must have one type, and the outputs theirs and the inputs' shapes")
+    n_pos = cos.shape[0]
+    for t, n, s in ((q_norm, "q_norm", (hd,)), (k_norm, "k_norm", (hd,)), (cos, "cos", (n_pos, hd // 2)), (sin, "sin", (n_pos, hd // 2))):
+        _flat(t, n, s, (torch.float32,))
+    _flat(pos, "pos", (R,), (torch.int32,))
+    _here(q, k, q_norm, k_norm, cos, sin, pos, q_out, k_out)
+    _ops_chk(load().spec_k_qk_norm_rope(q.data_ptr(), strides[0], nq, k.data_ptr(), strides[1], nkv, _kind(q), hd, R,
+                                        q_norm.data_ptr(), k_norm.data_ptr(), eps, cos.data_ptr(), sin.data_ptr(), n_pos,
+                                        pos.data_ptr(), q_out.data_ptr(), strides[2], k_out.data_ptr(), strides[3],
+                                        _kind(q_out), stream), "spec_k_qk_norm_rope")

@@ -33,9 +33,11 @@ HIP_SOURCES = [
     "kernels/attention.hip",
     "kernels/sampler.hip",
     "kernels/misc.hip",
+    "kernels/f8.hip",
+    "kernels/headnorm.hip",
 ]
 C_SOURCES = ["gammatune.c"]
-MFMA_SOURCES = ["kernels/gemv_mfma.hip", "kernels/gemm_mfma.hip", "kernels/attention.hip"]  # scanned by isa_guard after compiling
+MFMA_SOURCES = ["kernels/gemv_mfma.hip", "kernels/gemm_mfma.hip", "kernels/attention.hip", "kernels/f8.hip"]  # scanned by isa_guard after compiling
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 HIP_FLAGS = [

@@ -6,6 +6,7 @@
 // estimates (launch_proj).
 #include "spec.h"
 #include "spec_debug.h"
+#include "spec_ops.h"
 #include "gammatune.h"
 
 #include <hip/hip_runtime.h>
@@ -1668,6 +1669,87 @@ int spec_k_accept_static(const float *p_logits, const float *q_logits, const int
     hipLaunchKernelGGL(accept_result_k, dim3(1), dim3(64), 0, st, reinterpret_cast<const int32_t *>(buf + L.o_state) + 12, result);
     if (hipGetLastError() != hipSuccess) return fail(nullptr, SPEC_EHIP, "accept_static: launch failed");
     return SPEC_OK;
+}
+
+// ---- operators of an 8-bit checkpoint with normed heads (spec_ops.h) ---------------------------------------------
+
+// A failure that belongs to no context; the text is a literal (keeping it must not throw across the C boundary).
+static int refuse(int code, const char *msg) noexcept {
+    try { g_last_err = msg; } catch (...) {}
+    return code;
+}
+static int launched(hipError_t e, const char *msg) noexcept {
+    return e == hipSuccess ? SPEC_OK : refuse(e == hipErrorInvalidValue ? SPEC_EINVAL : SPEC_EHIP, msg);
+}
+static bool off(const void *p, size_t align) { return reinterpret_cast<uintptr_t>(p) % align != 0; }
+static bool wide(int32_t dtype) { return dtype == SPEC_F32 || dtype == SPEC_BF16; }
+static size_t width(int32_t dtype) { return dtype == SPEC_F32 ? 4 : 2; }
+
+int spec_k_quant_f8(const void *x, int32_t dtype, int64_t ldx, int32_t R, int32_t K, void *q, float *scale, void *stream) {
+    if (!wide(dtype)) return refuse(SPEC_EINVAL, "quant_f8: x must be fp32 or bf16");
+    if (R < 0 || K < 16 || K % 16 || ldx < K) return refuse(SPEC_EINVAL, "quant_f8: R < 0, K not a positive multiple of 16, or ldx < K");
+    if (R == 0) return SPEC_OK;
+    if (!x || !q || !scale) return refuse(SPEC_EINVAL, "quant_f8: null pointer");
+    if (off(x, width(dtype)) || off(q, 16) || off(scale, 4)) return refuse(SPEC_EINVAL, "quant_f8: misaligned pointer");
+    return launched(launch_quant_f8(x, dtype, ldx, R, K, q, scale, reinterpret_cast<hipStream_t>(stream)), "quant_f8: launch failed");
+}
+
+int64_t spec_k_gemm_f8_workspace(int32_t K, int32_t R, int32_t x_dtype) {
+    if (K < 16 || K % 16 || R < 0 || (x_dtype != SPEC_F8 && !wide(x_dtype)))
+        return refuse(SPEC_EINVAL, "gemm_f8_workspace: R < 0, K not a positive multiple of 16, or unknown type of x");
+    return x_dtype == SPEC_F8 ? 0 : (int64_t)132 * R * ((K + 127) / 128);
+}
+
+int spec_k_gemm_f8(const void *w, const float *w_scale, int32_t N, int32_t K, const void *x, int32_t x_dtype, int64_t ldx,
+                   const float *x_scale, int32_t R, void *y, int32_t y_dtype, int64_t ldy, void *workspace,
+                   int64_t workspace_bytes, void *stream) {
+    const bool f8 = x_dtype == SPEC_F8;
+    if ((!f8 && !wide(x_dtype)) || !wide(y_dtype)) return refuse(SPEC_EINVAL, "gemm_f8: x must be e4m3, fp32 or bf16, y fp32 or bf16");
+    if (N < 1 || K < 16 || K % 16 || R < 0 || ldx < K || ldy < N || workspace_bytes < 0 || (f8 && ldx != K))
+        return refuse(SPEC_EINVAL, "gemm_f8: N < 1, R < 0, K not a positive multiple of 16, or a row stride that does not fit");
+    if (R == 0) return SPEC_OK;
+    if (!w || !w_scale || !x || !y || (f8 ? !x_scale : x_scale != nullptr))
+        return refuse(SPEC_EINVAL, "gemm_f8: null pointer (x_scale goes with e4m3 rows, and only with them)");
+    if (off(w, 16) || off(w_scale, 4) || off(x, f8 ? 16 : width(x_dtype)) || off(x_scale, 4) || off(y, width(y_dtype)) || off(workspace, 16))
+        return refuse(SPEC_EINVAL, "gemm_f8: misaligned pointer");
+    const int64_t need = spec_k_gemm_f8_workspace(K, R, x_dtype);
+    if ((workspace ? workspace_bytes : 0) < need) return refuse(SPEC_EINVAL, "gemm_f8: workspace too small");
+    const hipStream_t st = reinterpret_cast<hipStream_t>(stream);
+    F8Args a{};
+    a.w = reinterpret_cast<const uint8_t *>(w); a.ws = w_scale; a.N = N; a.K = K; a.KB = (K + 127) / 128; a.R = R;
+    a.y = y; a.y_dtype = y_dtype; a.ldy = ldy;
+    a.x = x; a.xs = x_scale; a.ldx = ldx; a.x_type = f8 ? 0 : (x_dtype == SPEC_F32 ? 1 : 2);
+    if (!f8) {
+        uint8_t *q = reinterpret_cast<uint8_t *>(workspace);
+        float *scale = reinterpret_cast<float *>(q + (int64_t)128 * R * a.KB);
+        const int rc = launched(launch_quant_f8(x, x_dtype, ldx, R, K, q, scale, st), "gemm_f8: launch failed");
+        if (rc != SPEC_OK) return rc;
+        a.x = q; a.xs = scale; a.ldx = K; a.x_type = 0;
+    }
+    return launched(launch_gemm_f8(a, st), "gemm_f8: launch failed");
+}
+
+int spec_k_qk_norm_rope(const void *q, int64_t ldq, int32_t nq, const void *k, int64_t ldk, int32_t nkv, int32_t dtype,
+                        int32_t hd, int32_t R, const float *q_norm, const float *k_norm, float eps, const float *rope_cos,
+                        const float *rope_sin, int32_t n_pos, const int32_t *pos, void *q_out, int64_t ldqo, void *k_out,
+                        int64_t ldko, int32_t out_dtype, void *stream) {
+    if (!wide(dtype) || !wide(out_dtype)) return refuse(SPEC_EINVAL, "qk_norm_rope: heads must be fp32 or bf16");
+    if (hd < 2 || hd > 512 || hd % 2) return refuse(SPEC_EINVAL, "qk_norm_rope: hd must be even, 2 to 512");
+    if (nq < 0 || nkv < 0 || (int64_t)nq + nkv < 1 || (int64_t)nq + nkv > 0x7fffffff || R < 0 || n_pos < 1 || !(eps >= 0.f))
+        return refuse(SPEC_EINVAL, "qk_norm_rope: no heads, R < 0, n_pos < 1 or eps < 0");
+    if ((nq && (ldq < (int64_t)nq * hd || ldqo < (int64_t)nq * hd)) || (nkv && (ldk < (int64_t)nkv * hd || ldko < (int64_t)nkv * hd)))
+        return refuse(SPEC_EINVAL, "qk_norm_rope: row stride below the heads' width");
+    if (R == 0) return SPEC_OK;
+    if (!rope_cos || !rope_sin || !pos || (nq && (!q || !q_out || !q_norm)) || (nkv && (!k || !k_out || !k_norm)))
+        return refuse(SPEC_EINVAL, "qk_norm_rope: null pointer");
+    if (off(rope_cos, 4) || off(rope_sin, 4) || off(pos, 4) || (nq && (off(q, width(dtype)) || off(q_out, width(out_dtype)) || off(q_norm, 4))) ||
+        (nkv && (off(k, width(dtype)) || off(k_out, width(out_dtype)) || off(k_norm, 4))))
+        return refuse(SPEC_EINVAL, "qk_norm_rope: misaligned pointer");
+    HeadNormArgs a{};
+    a.q = q; a.k = k; a.ldq = ldq; a.ldk = ldk; a.nq = nq; a.nkv = nkv; a.dtype = dtype; a.hd = hd; a.R = R;
+    a.q_norm = q_norm; a.k_norm = k_norm; a.eps = eps; a.rope_cos = rope_cos; a.rope_sin = rope_sin; a.n_pos = n_pos; a.pos = pos;
+    a.q_out = q_out; a.k_out = k_out; a.ldqo = ldqo; a.ldko = ldko; a.out_dtype = out_dtype;
+    return launched(launch_head_norm(a, reinterpret_cast<hipStream_t>(stream)), "qk_norm_rope: launch failed");
 }
 
 }  // extern "C"

@@ -192,6 +192,34 @@ struct AcceptArgs {
     int32_t *A_dev, *y_dev;     // [B] device copies
 };
 
+// e4m3 product with block scales (f8.hip): y [R][N] = x [R][K] . w [N][K]^T
+struct F8Args {
+    const uint8_t *w;     // e4m3 [N][K]
+    const float *ws;      // [ceil(N / 128)][KB]
+    const void *x;        // x_type rows, row r at element r * ldx
+    int64_t ldx;
+    int32_t x_type;       // 0 e4m3 (ldx == K) with xs, 1 fp32, 2 bf16
+    const float *xs;      // e4m3 rows: [KB][R]
+    void *y;              // y_dtype, row stride ldy
+    int64_t ldy;
+    int32_t y_dtype, N, K, KB, R;  // KB = ceil(K / 128)
+};
+
+// Norm and rotation of query and key heads (headnorm.hip); strides in elements.
+struct HeadNormArgs {
+    const void *q, *k;
+    int64_t ldq, ldk;
+    int32_t nq, nkv, dtype, hd, R;
+    const float *q_norm, *k_norm;      // [hd]
+    float eps;
+    const float *rope_cos, *rope_sin;  // [n_pos][hd/2]
+    int32_t n_pos;
+    const int32_t *pos;                // [R]
+    void *q_out, *k_out;
+    int64_t ldqo, ldko;
+    int32_t out_dtype;
+};
+
 // ---- launchers (defined next to the kernels) -----------------------------------------------------
 hipError_t launch_begin_draft(const State &st, const int32_t *gamma_plan, hipStream_t s);
 hipError_t launch_embed(const EmbedArgs &a, hipStream_t s);
@@ -233,5 +261,8 @@ hipError_t launch_kv_write(const KVCache &kv, int kv_dtype, int seq, int pos0, i
 hipError_t launch_copy(const void *src, void *dst, int64_t bytes, hipStream_t s);
 hipError_t launch_cast_to_bf16(const float *src, uint16_t *dst, int64_t lo_off, int64_t n, hipStream_t s);
 hipError_t launch_cast_to_f32(const void *src, int dtype, float *dst, int64_t n, hipStream_t s);
+hipError_t launch_quant_f8(const void *x, int dtype, int64_t ldx, int R, int K, void *q, float *scale, hipStream_t s);
+hipError_t launch_gemm_f8(const F8Args &a, hipStream_t s);
+hipError_t launch_head_norm(const HeadNormArgs &a, hipStream_t s);
 
 }  // namespace sd

@@ -1,0 +1,434 @@
+"""Operators of include/spec_ops.h against plain 64-bit implementations (tests/ops_reference.py).
+
+Tolerances, derived from the number formats.  A sum of n fp32 terms in any order is off by at most (n - 1) 2^-23 of the
+sum of their magnitudes (2^-24 a rounding to nearest, twice that where an adder truncates).
+  product: 128 terms inside a block, the scale product and its multiplication (3 roundings), one addition per block:
+           (128 + 3 + blocks) 2^-23 of the sum of magnitudes, then half a step of the output type (bf16: 2^-8 of the value,
+           fp32: 2^-24);
+  norm:    the mean of hd squares is off by (hd + 1) 2^-23 of itself, its root by half that; then the division, the two
+           products and the two rotations round 6 times: (hd / 2 + 8) 2^-23 of the magnitudes of the two terms, then half a
+           step of the output type;
+  quantiser: every step is rounded by definition, so the values are equal."""
+import numpy as np
+import pytest
+import torch
+
+import ops_reference as ref
+import paper_2504_00030_amd as pk
+from paper_2504_00030_amd import binding
+
+pytestmark = pytest.mark.gpu
+
+F8 = torch.float8_e4m3fn
+F32, BF16 = torch.float32, torch.bfloat16
+HALF_STEP = {F32: 2.0 ** -24, BF16: 2.0 ** -8}
+
+
+def _stream():
+    return torch.cuda.current_stream().cuda_stream
+
+
+def _f8(values):
+    return torch.from_numpy(values.astype(np.float32)).to(F8).cuda()
+
+
+def _weights(rng, N, K):
+    """e4m3 values over the whole range with block scales over three powers of ten."""
+    v = ref.e4m3_values()
+    w = rng.standard_normal((N, K)) * 60.0
+    w = ref.e4m3(np.clip(w, -448, 448))
+    w[rng.random((N, K)) < 0.02] = v[0x7e]  # some of the largest value
+    scale = (10.0 ** rng.uniform(-5, -2, (ref.blocks(N), ref.blocks(K)))).astype(np.float32)
+    return w, scale
+
+
+def _activations(rng, R, K, dtype):
+    x = rng.standard_normal((R, K)) * np.exp(0.5 * rng.standard_normal((1, K))) * np.exp(rng.standard_normal((R, 1)))
+    return torch.from_numpy(x.astype(np.float32)).to(dtype)
+
+
+def _product_tol(mag, y, KB, dtype):
+    return (128 + 3 + KB) * 2.0 ** -23 * mag + HALF_STEP[dtype] * np.abs(y) + 1e-38
+
+
+def _gemm_case(rng, R, N, K, x_kind, y_dtype, ldy_extra=0):
+    w, ws = _weights(rng, N, K)
+    wd, wsd = _f8(w), torch.from_numpy(ws).cuda()
+    buf = torch.full((R, N + ldy_extra), 7.0, dtype=y_dtype, device="cuda")
+    y = buf[:, :N]
+    work = torch.empty(132 * R * ref.blocks(K) + (1 << 20), dtype=torch.uint8, device="cuda")
+    x = _activations(rng, R, K, F32 if x_kind == F8 else x_kind)
+    q, xs = ref.quantise(x.float().numpy())
+    if x_kind == F8:
+        pk.k_gemm_f8(wd, wsd, _f8(q), y, x_scale=torch.from_numpy(xs).cuda(), stream=_stream())
+    else:
+        pk.k_gemm_f8(wd, wsd, x.cuda(), y, workspace=work, stream=_stream())
+    torch.cuda.synchronize()
+    want, mag = ref.product(q, xs, w, ws)
+    got = buf.double().cpu().numpy()
+    err = np.abs(got[:, :N] - want)
+    tol = _product_tol(mag, want, ref.blocks(K), y_dtype)
+    assert (err <= tol).all(), f"worst {np.max(err / tol):.3g} of the tolerance at {np.unravel_index(np.argmax(err / tol), err.shape)}"
+    assert (got[:, N:] == 7.0).all(), "columns behind the rows were written"
+
+
+# ---- quantiser -----------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("R,K", [(1, 16), (1, 128), (3, 144), (5, 112), (17, 1040), (64, 4096), (130, 272), (1, 14336), (300, 2048)])
+def test_quantiser_equals_its_definition(R, K, dtype):
+    rng = np.random.default_rng(R * 1000 + K)
+    x = _activations(rng, R, K, dtype)
+    x[0, :8] = 0.0
+    q = torch.zeros((R, K), dtype=F8, device="cuda")
+    scale = torch.zeros((ref.blocks(K), R), device="cuda")
+    pk.k_quant_f8(x.cuda(), q, scale, stream=_stream())
+    want_q, want_s = ref.quantise(x.float().numpy())
+    assert np.array_equal(scale.cpu().numpy(), want_s)
+    assert np.array_equal(q.cpu().float().numpy().astype(np.float64), want_q)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("extra,shift", [(0, 0), (8, 0), (3, 0), (1, 1), (5, 3)])
+def test_quantiser_row_strides_and_alignment(extra, shift, dtype):
+    rng = np.random.default_rng(extra * 10 + shift)
+    R, K = 21, 400
+    x = _activations(rng, R, K, dtype)
+    flat = torch.full((R * (K + extra) + shift + 8,), 1e30, dtype=dtype, device="cuda")
+    view = flat[shift: shift + R * (K + extra)].view(R, K + extra)[:, :K]
+    view.copy_(x)
+    q = torch.zeros((R, K), dtype=F8, device="cuda")
+    scale = torch.zeros((ref.blocks(K), R), device="cuda")
+    pk.k_quant_f8(view, q, scale, stream=_stream())
+    want_q, want_s = ref.quantise(x.float().numpy())
+    assert np.array_equal(scale.cpu().numpy(), want_s)
+    assert np.array_equal(q.cpu().float().numpy().astype(np.float64), want_q)
+
+
+def test_quantiser_extreme_values():
+    """All-zero blocks, the smallest and largest magnitudes, NaN in its place, infinities."""
+    K = 640
+    x = np.zeros((6, K), dtype=np.float32)
+    x[1, :] = np.float32(1e-40)                       # below the least magnitude: rounds to zero against 2^-96
+    x[2, :] = np.linspace(-3.4e38, 3.4e38, K)
+    x[3, :] = np.linspace(-1e-28, 1e-28, K)
+    x[4, :] = np.linspace(-2.0, 2.0, K)
+    x[4, 200] = np.nan
+    x[5, :] = 1.0
+    x[5, 300] = np.inf
+    q = torch.zeros((6, K), dtype=F8, device="cuda")
+    scale = torch.zeros((5, 6), device="cuda")
+    pk.k_quant_f8(torch.from_numpy(x).cuda(), q, scale, stream=_stream())
+    got, s = q.cpu().float().numpy().astype(np.float64), scale.cpu().numpy()
+    want_q, want_s = ref.quantise(x)
+    assert np.array_equal(got[:4], want_q[:4]) and np.array_equal(s[:, :4], want_s[:, :4])
+    assert (got[:2] == 0).all() and (s[:, :2] > 0).all()
+    assert np.isnan(got[4, 200]) and np.isfinite(np.delete(got[4], 200)).all() and np.array_equal(s[:, 4], want_s[:, 4])
+    assert np.isinf(s[2, 5]) and np.isfinite(np.delete(s[:, 5], 2)).all()
+    assert np.isnan(got[5, 300])
+
+
+def test_quantiser_reaches_every_code():
+    """Every finite e4m3 value, in both signs, is produced from itself (blocks whose largest is 448)."""
+    v = ref.e4m3_values()
+    v = np.concatenate([v[np.isfinite(v)], [448.0, -448.0]])
+    v = np.concatenate([v, v])[:256].reshape(2, 128)
+    v[:, 0] = 448.0
+    x = v.astype(np.float32).reshape(1, 256)
+    q = torch.zeros((1, 256), dtype=F8, device="cuda")
+    scale = torch.zeros((2, 1), device="cuda")
+    pk.k_quant_f8(torch.from_numpy(x).cuda(), q, scale, stream=_stream())
+    assert np.array_equal(q.cpu().float().numpy(), x) and (scale.cpu().numpy() == 1.0).all()
+
+
+# ---- product -------------------------------------------------------------------------------------------------------
+SIZES = [(1, 1, 16), (1, 16, 128), (1, 2048, 2048), (2, 5, 144), (3, 100, 1040), (7, 130, 272), (16, 128, 128), (17, 777, 1040),
+         (33, 48, 4096), (64, 256, 512), (65, 640, 384), (100, 96, 1536), (129, 1000, 640), (250, 264, 2064), (300, 520, 256),
+         (513, 300, 400), (1, 130, 14336), (20, 4100, 144)]
+
+
+@pytest.mark.parametrize("x_kind", [F8, F32, BF16])
+@pytest.mark.parametrize("R,N,K", SIZES)
+def test_product_sizes(R, N, K, x_kind):
+    rng = np.random.default_rng(R + 7 * N + 13 * K)
+    _gemm_case(rng, R, N, K, x_kind, F32)
+
+
+@pytest.mark.parametrize("R,N,K", SIZES[::2])
+def test_product_bf16_result(R, N, K):
+    rng = np.random.default_rng(R + 7 * N + 13 * K)
+    _gemm_case(rng, R, N, K, F8, BF16)
+
+
+@pytest.mark.parametrize("y_dtype", [F32, BF16])
+@pytest.mark.parametrize("R,N,K,extra", [(5, 33, 128, 1), (40, 64, 256, 3), (200, 260, 384, 4), (300, 255, 144, 2), (18, 2050, 272, 8)])
+def test_product_row_strides(R, N, K, extra, y_dtype):
+    rng = np.random.default_rng(R + N + extra)
+    _gemm_case(rng, R, N, K, BF16, y_dtype, ldy_extra=extra)
+
+
+def test_product_result_rows_far_apart():
+    """Offsets of y beyond 32 bits: rows 2^30 + 4 elements apart."""
+    rng = np.random.default_rng(5)
+    R, N, K = 4, 20, 144
+    w, ws = _weights(rng, N, K)
+    q, xs = ref.quantise(_activations(rng, R, K, F32).numpy())
+    ld = (1 << 30) + 4
+    buf = torch.empty(ld * (R - 1) + N, dtype=BF16, device="cuda")
+    y = torch.as_strided(buf, (R, N), (ld, 1))
+    pk.k_gemm_f8(_f8(w), torch.from_numpy(ws).cuda(), _f8(q), y, x_scale=torch.from_numpy(xs).cuda(), stream=_stream())
+    want, mag = ref.product(q, xs, w, ws)
+    err = np.abs(y.double().cpu().numpy() - want)
+    assert (err <= _product_tol(mag, want, ref.blocks(K), BF16)).all()
+
+
+def test_product_keeps_nan_and_infinite_rows_to_themselves():
+    """A NaN in a row of x or w reaches that row or column only; a row with an infinity comes out NaN; other values stand."""
+    rng = np.random.default_rng(8)
+    R, N, K = 35, 70, 400
+    w, ws = _weights(rng, N, K)
+    x = _activations(rng, R, K, F32).numpy()
+    x[3, 399] = np.nan
+    x[20, 5] = np.inf
+    wn = w.copy()
+    wn[50, 130] = np.nan
+    y = torch.zeros((R, N), device="cuda")
+    work = torch.empty(132 * R * ref.blocks(K), dtype=torch.uint8, device="cuda")
+    pk.k_gemm_f8(_f8(wn), torch.from_numpy(ws).cuda(), torch.from_numpy(x).cuda(), y, workspace=work, stream=_stream())
+    got = y.double().cpu().numpy()
+    assert np.isnan(got[3]).all() and np.isnan(got[20]).all() and np.isnan(got[:, 50]).all()
+    rows, cols = np.delete(np.arange(R), [3, 20]), np.delete(np.arange(N), 50)
+    q, xs = ref.quantise(x[rows])
+    want, mag = ref.product(q, xs, w, ws)
+    want, mag = want[:, cols], mag[:, cols]
+    assert (np.abs(got[np.ix_(rows, cols)] - want) <= _product_tol(mag, want, ref.blocks(K), F32)).all()
+
+
+def test_product_repeats_bit_for_bit():
+    rng = np.random.default_rng(9)
+    for R, N, K in [(1, 1024, 4096), (40, 520, 2048), (300, 640, 4096)]:
+        w, ws = _weights(rng, N, K)
+        wd, wsd, x = _f8(w), torch.from_numpy(ws).cuda(), _activations(rng, R, K, BF16).cuda()
+        work = torch.empty(132 * R * ref.blocks(K) + (32 << 20), dtype=torch.uint8, device="cuda")
+        ys = [torch.zeros((R, N), device="cuda") for _ in range(3)]
+        for y in ys:
+            pk.k_gemm_f8(wd, wsd, x, y, workspace=work, stream=_stream())
+            work.fill_(0xff)  # contents between calls do not matter
+        assert torch.equal(ys[0], ys[1]) and torch.equal(ys[0], ys[2])
+
+
+# ---- norm and rotation -------------------------------------------------------------------------------------------
+def _tables(n_pos, hd):
+    ang = np.arange(n_pos)[:, None] * 10000.0 ** (-2.0 * np.arange(hd // 2) / hd)[None, :]
+    return np.cos(ang).astype(np.float32), np.sin(ang).astype(np.float32)
+
+
+def _norm_case(rng, R, nq, nkv, hd, t_in, t_out, fused=True, in_place=False, n_pos=97, eps=1e-5, pad=0.25):
+    width = (nq + 2 * nkv) * hd
+    qkv = torch.from_numpy((rng.standard_normal((R, width)) * np.exp(rng.standard_normal((R, 1)))).astype(np.float32)).to(t_in)
+    dev = qkv.cuda()
+    q = dev[:, : nq * hd].unflatten(1, (nq, hd))
+    k = dev[:, nq * hd: (nq + nkv) * hd].unflatten(1, (nkv, hd))
+    if not fused:
+        q, k = q.contiguous(), k.contiguous()
+    gq, gk = (1 + 0.3 * rng.standard_normal(hd)).astype(np.float32), (1 + 0.3 * rng.standard_normal(hd)).astype(np.float32)
+    cos, sin = _tables(n_pos, hd)
+    pos = rng.integers(0, n_pos, R).astype(np.int32)
+    bad = rng.random(R) < pad
+    pos[bad] = np.where(rng.random(bad.sum()) < 0.5, -1, n_pos).astype(np.int32)
+    q_out, k_out = (q, k) if in_place else (torch.full((R, nq, hd), 3.0, dtype=t_out, device="cuda"),
+                                            torch.full((R, nkv, hd), 3.0, dtype=t_out, device="cuda"))
+    before = [t.double().cpu().numpy() for t in (q_out, k_out)]
+    heads = [t.double().cpu().numpy() for t in (q, k)]
+    cu = lambda a: torch.from_numpy(a).cuda()
+    pk.k_qk_norm_rope(q, k, cu(gq), cu(gk), cu(cos), cu(sin), cu(pos), q_out, k_out, eps=eps, stream=_stream())
+    torch.cuda.synchronize()
+    on = (pos >= 0) & (pos < n_pos)
+    at = np.clip(pos, 0, n_pos - 1)
+    for h, g, got, old in zip(heads, (gq, gk), (q_out, k_out), before):
+        got = got.double().cpu().numpy()
+        want, mag = ref.norm_rope(h, g.astype(np.float64), eps, cos[at].astype(np.float64), sin[at].astype(np.float64))
+        tol = (hd / 2 + 8) * 2.0 ** -23 * mag + HALF_STEP[t_out] * np.abs(want) + 1e-38
+        assert (np.abs(got[on] - want[on]) <= tol[on]).all()
+        assert np.array_equal(got[~on], old[~on]), "a padding row was written"
+    if fused:  # the value columns stay as they are
+        assert torch.equal(dev[:, (nq + nkv) * hd:].cpu(), qkv[:, (nq + nkv) * hd:])
+
+
+@pytest.mark.parametrize("t_in,t_out", [(F32, F32), (F32, BF16), (BF16, F32), (BF16, BF16)])
+@pytest.mark.parametrize("R,nq,nkv,hd", [(1, 32, 8, 128), (1, 1, 1, 2), (3, 4, 4, 32), (5, 7, 1, 80), (130, 12, 12, 64), (33, 8, 2, 96),
+                                         (9, 2, 2, 6), (64, 5, 5, 256), (17, 3, 1, 512), (11, 2, 1, 510), (600, 32, 8, 128)])
+def test_norm_and_rotation(R, nq, nkv, hd, t_in, t_out):
+    _norm_case(np.random.default_rng(R + nq + hd), R, nq, nkv, hd, t_in, t_out)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("fused", [True, False])
+def test_norm_in_place(dtype, fused):
+    _norm_case(np.random.default_rng(3), 50, 8, 2, 64, dtype, dtype, fused=fused, in_place=True)
+    _norm_case(np.random.default_rng(4), 700, 8, 2, 128, dtype, dtype, fused=fused, in_place=True)
+
+
+def test_norm_zero_heads_and_all_padding():
+    R, hd = 4, 64
+    cos, sin = (torch.from_numpy(t).cuda() for t in _tables(8, hd))
+    g = torch.ones(hd, device="cuda")
+    q = torch.zeros((R, 2, hd), device="cuda")
+    k = torch.zeros((R, 1, hd), device="cuda")
+    out = [torch.full_like(q, 5.0), torch.full_like(k, 5.0)]
+    pos = torch.arange(R, dtype=torch.int32, device="cuda")
+    pk.k_qk_norm_rope(q, k, g, g, cos, sin, pos, *out, eps=1e-5, stream=_stream())
+    assert all((o == 0).all() for o in out)  # 0 / sqrt(eps)
+    out = [torch.full_like(q, 5.0), torch.full_like(k, 5.0)]
+    pk.k_qk_norm_rope(q, k, g, g, cos, sin, pos - 100, *out, eps=1e-5, stream=_stream())
+    assert all((o == 5.0).all() for o in out)
+
+
+def test_norm_queries_only_and_large_values():
+    rng = np.random.default_rng(12)
+    _norm_case(rng, 6, 4, 0, 128, F32, F32)
+    R, hd = 3, 128
+    h = (rng.standard_normal((R, 2, hd)) * 1e15).astype(np.float32)
+    cos, sin = _tables(16, hd)
+    cu = lambda a: torch.from_numpy(a).cuda()
+    g = np.ones(hd, dtype=np.float32)
+    pos = np.array([0, 15, 7], dtype=np.int32)
+    q, k = cu(h), cu(h[:, :1].copy())
+    qo, ko = torch.zeros_like(q), torch.zeros_like(k)
+    pk.k_qk_norm_rope(q, k, cu(g), cu(g), cu(cos), cu(sin), cu(pos), qo, ko, stream=_stream())
+    want, mag = ref.norm_rope(h.astype(np.float64), g, 1e-5, cos[pos].astype(np.float64), sin[pos].astype(np.float64))
+    assert (np.abs(qo.double().cpu().numpy() - want) <= (hd / 2 + 8) * 2.0 ** -23 * mag + 2.0 ** -24 * np.abs(want)).all()
+
+
+def test_norm_rows_far_apart():
+    """Offsets beyond 32 bits: rows 2^30 elements apart."""
+    rng = np.random.default_rng(13)
+    R, nq, hd, ld = 3, 2, 64, 1 << 30
+    buf = torch.empty(ld * (R - 1) + 3 * hd, dtype=BF16, device="cuda")
+    q = torch.as_strided(buf, (R, nq, hd), (ld, hd, 1))
+    k = torch.as_strided(buf, (R, 1, hd), (ld, hd, 1), storage_offset=nq * hd)
+    h = rng.standard_normal((R, nq + 1, hd)).astype(np.float32)
+    q.copy_(torch.from_numpy(h[:, :nq]).cuda())
+    k.copy_(torch.from_numpy(h[:, nq:]).cuda())
+    cos, sin = _tables(8, hd)
+    g = np.ones(hd, dtype=np.float32)
+    cu = lambda a: torch.from_numpy(a).cuda()
+    pos = np.array([1, 2, 7], dtype=np.int32)
+    heads = q.double().cpu().numpy()
+    pk.k_qk_norm_rope(q, k, cu(g), cu(g), cu(cos), cu(sin), cu(pos), q, k, stream=_stream())
+    want, mag = ref.norm_rope(heads, g, 1e-5, cos[pos].astype(np.float64), sin[pos].astype(np.float64))
+    assert (np.abs(q.double().cpu().numpy() - want) <= (hd / 2 + 8) * 2.0 ** -23 * mag + 2.0 ** -8 * np.abs(want)).all()
+
+
+# ---- together ------------------------------------------------------------------------------------------------------
+class _Layer:
+    """The QKV step of one layer: rows -> e4m3 product with the fused matrix -> heads normed and rotated in place."""
+
+    def __init__(self, rng, R, d, nq, nkv, hd):
+        self.shape = (R, d, nq, nkv, hd)
+        self.w, self.ws = _weights(rng, (nq + 2 * nkv) * hd, d)
+        self.wd, self.wsd = _f8(self.w), torch.from_numpy(self.ws).cuda()
+        self.x = _activations(rng, R, d, BF16).cuda()
+        self.qkv = torch.zeros((R, (nq + 2 * nkv) * hd), device="cuda")
+        self.gq = (1 + 0.2 * torch.randn(hd)).cuda()
+        self.gk = (1 + 0.2 * torch.randn(hd)).cuda()
+        self.cos, self.sin = (torch.from_numpy(t).cuda() for t in _tables(64, hd))
+        self.pos = torch.arange(R, dtype=torch.int32, device="cuda") % 64
+        self.q = torch.zeros((R, nq, hd), dtype=BF16, device="cuda")
+        self.k = torch.zeros((R, nkv, hd), dtype=BF16, device="cuda")
+        self.work = torch.empty(pk.k_gemm_f8_workspace(d, R, BF16) + (8 << 20), dtype=torch.uint8, device="cuda")
+
+    def run(self):
+        R, d, nq, nkv, hd = self.shape
+        pk.k_gemm_f8(self.wd, self.wsd, self.x, self.qkv, workspace=self.work, stream=_stream())
+        pk.k_qk_norm_rope(self.qkv[:, : nq * hd].unflatten(1, (nq, hd)), self.qkv[:, nq * hd: (nq + nkv) * hd].unflatten(1, (nkv, hd)),
+                          self.gq, self.gk, self.cos, self.sin, self.pos, self.q, self.k, stream=_stream())
+
+    def check(self):
+        R, d, nq, nkv, hd = self.shape
+        qv, xs = ref.quantise(self.x.float().cpu().numpy())
+        want, mag = ref.product(qv, xs, self.w, self.ws)
+        got = self.qkv.double().cpu().numpy()
+        assert (np.abs(got - want) <= _product_tol(mag, want, ref.blocks(d), F32)).all()
+        at = self.pos.cpu().numpy()
+        c, s = self.cos.double().cpu().numpy()[at], self.sin.double().cpu().numpy()[at]
+        for lo, n, g, out in ((0, nq, self.gq, self.q), (nq, nkv, self.gk, self.k)):
+            h = got[:, lo * hd: (lo + n) * hd].reshape(R, n, hd)
+            w_, m_ = ref.norm_rope(h, g.double().cpu().numpy(), 1e-5, c, s)
+            assert (np.abs(out.double().cpu().numpy() - w_) <= (hd / 2 + 8) * 2.0 ** -23 * m_ + 2.0 ** -8 * np.abs(w_) + 1e-38).all()
+
+
+@pytest.mark.parametrize("R", [1, 9, 70, 300])
+def test_layer_step(R):
+    layer = _Layer(np.random.default_rng(R), R, 512, 8, 2, 64)
+    layer.run()
+    torch.cuda.synchronize()
+    layer.check()
+
+
+@pytest.mark.parametrize("R", [1, 40, 300])
+def test_layer_step_captured_and_replayed(R):
+    """A captured step gives the eager step's bits on every replay, with new rows and positions between replays and the
+    program's own work on the device around them."""
+    layer = _Layer(np.random.default_rng(R), R, 384, 4, 2, 128)
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        layer.run()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        layer.run()
+    for i in range(4):
+        layer.x.copy_(_activations(np.random.default_rng(100 + i), R, 384, BF16))
+        layer.pos.copy_((torch.arange(R, device="cuda", dtype=torch.int32) * (i + 3)) % 64)
+        for t in (layer.qkv, layer.q, layer.k):
+            t.fill_(-1)
+        layer.work.fill_(0x7f)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        seen = [t.clone() for t in (layer.qkv, layer.q, layer.k)]
+        junk = torch.randn(1 << 20, device="cuda").sum()
+        layer.run()
+        torch.cuda.synchronize()
+        assert torch.isfinite(junk)
+        for a, b in zip(seen, (layer.qkv, layer.q, layer.k)):
+            assert torch.equal(a, b)
+    layer.check()
+
+
+def test_two_streams_at_once():
+    layers = [_Layer(np.random.default_rng(s), 40 + 200 * s, 512, 8, 2, 64) for s in (0, 1)]
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for layer, st in zip(layers, streams):
+            with torch.cuda.stream(st):
+                layer.run()
+    torch.cuda.synchronize()
+    for layer in layers:
+        layer.check()
+
+
+def test_empty_calls_do_nothing():
+    w, ws = torch.zeros((32, 128), dtype=F8, device="cuda"), torch.ones((1, 1), device="cuda")
+    x, y = torch.zeros((0, 128), device="cuda"), torch.zeros((0, 32), device="cuda")
+    pk.k_gemm_f8(w, ws, x, y)
+    pk.k_quant_f8(x, torch.zeros((0, 128), dtype=F8, device="cuda"), torch.zeros((1, 0), device="cuda"))
+    h = torch.zeros((0, 2, 64), device="cuda")
+    c = torch.zeros((4, 32), device="cuda")
+    g = torch.ones(64, device="cuda")
+    pk.k_qk_norm_rope(h, h, g, g, c, c, torch.zeros(0, dtype=torch.int32, device="cuda"), h, h)
+    torch.cuda.synchronize()
+
+
+def test_small_workspace_is_refused():
+    x, y = torch.zeros((4, 256), device="cuda"), torch.zeros((4, 32), device="cuda")
+    w, ws = torch.zeros((32, 256), dtype=F8, device="cuda"), torch.ones((1, 2), device="cuda")
+    need = pk.k_gemm_f8_workspace(256, 4, F32)
+    assert need == 132 * 4 * 2
+    for work in (None, torch.zeros(need - 1, dtype=torch.uint8, device="cuda")):
+        with pytest.raises(pk.SpecError) as e:
+            pk.k_gemm_f8(w, ws, x, y, workspace=work)
+        assert e.value.code == binding.SPEC_EINVAL
+    pk.k_gemm_f8(w, ws, x, y, workspace=torch.zeros(need, dtype=torch.uint8, device="cuda"))
+    torch.cuda.synchronize()
