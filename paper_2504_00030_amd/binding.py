@@ -490,38 +490,51 @@ def k_accept_static(p_logits, q_logits, drafted, temperature: float, seed: int, 
 
 
 # ---- operators of an 8-bit checkpoint with normed heads (include/spec_ops.h) ------------------------------------------
+_KINDS = None
+
+
+def _kinds() -> Dict:
+    """Element types of torch -> as the library names them."""
+    global _KINDS
+    if _KINDS is None:
+        import torch
+        _KINDS = {torch.float32: SPEC_F32, torch.bfloat16: SPEC_BF16, torch.float8_e4m3fn: SPEC_F8, torch.uint8: SPEC_F8}
+    return _KINDS
+
+
 def _kind(t) -> int:
-    """Element type of a GPU tensor as the library names it."""
-    import torch
-    if t.dtype == torch.float32:
-        return SPEC_F32
-    if t.dtype == torch.bfloat16:
-        return SPEC_BF16
-    if t.dtype in (torch.float8_e4m3fn, torch.uint8):
-        return SPEC_F8
-    raise ValueError(f"unsupported element type {t.dtype}")
+    k = _kinds().get(t.dtype)
+    if k is None:
+        raise ValueError(f"unsupported element type {t.dtype}")
+    return k
 
 
-def _flat(t, name: str, shape, dtypes):
-    """t is a contiguous tensor of this shape and one of these types; only data_ptr() is taken."""
-    if tuple(t.shape) != tuple(shape) or t.dtype not in dtypes or not t.is_contiguous():
-        raise ValueError(f"{name} must be a contiguous {tuple(shape)} tensor of {dtypes}, not {tuple(t.shape)} of {t.dtype}")
+def _flat(t, name: str, shape, kind: int) -> int:
+    """Address of a contiguous tensor of this shape and element type."""
+    if t.shape != shape or _kinds().get(t.dtype) != kind or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {tuple(shape)} tensor, not {tuple(t.shape)} of {t.dtype}")
+    return t.data_ptr()
+
+
+def _i32(t, name: str, shape) -> int:
+    if t.shape != shape or str(t.dtype) != "torch.int32" or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous int32 {tuple(shape)} tensor, not {tuple(t.shape)} of {t.dtype}")
+    return t.data_ptr()
 
 
 def _here(*tensors):
     """The pointers belong to the current device."""
     import torch
-    dev = torch.cuda.current_device() if torch.cuda.is_available() else -1
-    for t in tensors:
-        if not t.is_cuda or t.device.index != dev:
-            raise ValueError("operands must be tensors on the current GPU")
+    dev = tensors[0].get_device()
+    if dev < 0 or any(t.get_device() != dev for t in tensors) or torch.cuda.current_device() != dev:
+        raise ValueError("operands must be tensors on the current GPU")
 
 
 def _rows(t, name: str) -> int:
     """Row stride of a [R][n] tensor whose rows are contiguous."""
-    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+    if t.dim() != 2 or (t.stride(1) != 1 and t.shape[1] > 1):
         raise ValueError(f"{name} must be two-dimensional with contiguous rows")
-    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
 
 
 def _ops_chk(rc: int, where: str):
@@ -532,20 +545,18 @@ def _ops_chk(rc: int, where: str):
 def k_quant_f8(x, q, scale, stream: int = 0):
     """Rows of x (fp32 or bf16 [R][K], any row stride) to e4m3: q [R][K] (float8_e4m3fn or uint8) and scale fp32
     [ceil(K / 128)][R]."""
-    import torch
-    R, K = x.shape
     ldx = _rows(x, "x")
-    _flat(q, "q", (R, K), (torch.float8_e4m3fn, torch.uint8))
-    _flat(scale, "scale", ((K + 127) // 128, R), (torch.float32,))
+    R, K = x.shape
+    qp, sp = _flat(q, "q", (R, K), SPEC_F8), _flat(scale, "scale", ((K + 127) // 128, R), SPEC_F32)
     _here(x, q, scale)
-    _ops_chk(load().spec_k_quant_f8(x.data_ptr(), _kind(x), ldx, R, K, q.data_ptr(), scale.data_ptr(), stream),
-             "spec_k_quant_f8")
+    _ops_chk(load().spec_k_quant_f8(x.data_ptr(), _kind(x), ldx, R, K, qp, sp, stream), "spec_k_quant_f8")
 
 
 def k_gemm_f8_workspace(K: int, R: int, x_dtype) -> int:
     """Bytes of workspace k_gemm_f8 needs for R rows of K elements of this torch type."""
-    import torch
-    n = load().spec_k_gemm_f8_workspace(K, R, _kind(torch.empty(0, dtype=x_dtype)))
+    if x_dtype not in _kinds():
+        raise ValueError(f"unsupported element type {x_dtype}")
+    n = load().spec_k_gemm_f8_workspace(K, R, _kinds()[x_dtype])
     if n < 0:
         raise SpecError(int(n), "spec_k_gemm_f8_workspace", load().spec_last_error(None).decode())
     return int(n)
@@ -555,55 +566,48 @@ def k_gemm_f8(w, w_scale, x, y, x_scale=None, workspace=None, stream: int = 0):
     """y [R][N] (fp32 or bf16, any row stride) = x . w^T with w e4m3 [N][K] and w_scale fp32 [ceil(N / 128)][ceil(K / 128)].
     x: e4m3 [R][K] with its x_scale as k_quant_f8 leaves them, or fp32 / bf16 rows, which the call quantises in
     `workspace` (a GPU tensor of at least k_gemm_f8_workspace() bytes; more, up to 32 MiB, lets K be shared out)."""
-    import torch
     N, K = w.shape
-    R = x.shape[0]
-    f8 = (torch.float8_e4m3fn, torch.uint8)
-    _flat(w, "w", (N, K), f8)
-    _flat(w_scale, "w_scale", ((N + 127) // 128, (K + 127) // 128), (torch.float32,))
-    if tuple(x.shape) != (R, K) or tuple(y.shape) != (R, N):
-        raise ValueError(f"x must be [R][{K}] and y [R][{N}], not {tuple(x.shape)} and {tuple(y.shape)}")
     ldx, ldy = _rows(x, "x"), _rows(y, "y")
+    R, KB = x.shape[0], (K + 127) // 128
+    if x.shape[1] != K or y.shape != (R, N):
+        raise ValueError(f"x must be [R][{K}] and y [R][{N}], not {tuple(x.shape)} and {tuple(y.shape)}")
+    wp, wsp = _flat(w, "w", (N, K), SPEC_F8), _flat(w_scale, "w_scale", ((N + 127) // 128, KB), SPEC_F32)
+    xp = x.data_ptr()
     _here(w, w_scale, x, y)
+    xsp = workp = None
+    work_bytes = 0
     if x_scale is not None:
-        _flat(x, "x", (R, K), f8)
-        _flat(x_scale, "x_scale", ((K + 127) // 128, R), (torch.float32,))
-        _here(x_scale)
-        ldx = K
-    nb = 0
+        xp, xsp = _flat(x, "x", (R, K), SPEC_F8), _flat(x_scale, "x_scale", (KB, R), SPEC_F32)
+        _here(x, x_scale)
     if workspace is not None:
-        _here(workspace)
         if not workspace.is_contiguous():
             raise ValueError("workspace must be contiguous")
-        nb = workspace.numel() * workspace.element_size()
-    _ops_chk(load().spec_k_gemm_f8(w.data_ptr(), w_scale.data_ptr(), N, K, x.data_ptr(), _kind(x), ldx,
-                                   None if x_scale is None else x_scale.data_ptr(), R, y.data_ptr(), _kind(y), ldy,
-                                   None if workspace is None else workspace.data_ptr(), nb, stream), "spec_k_gemm_f8")
+        _here(x, workspace)
+        workp, work_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    _ops_chk(load().spec_k_gemm_f8(wp, wsp, N, K, xp, _kind(x), ldx, xsp, R, y.data_ptr(), _kind(y), ldy, workp, work_bytes,
+                                   stream), "spec_k_gemm_f8")
 
 
 def _heads(t, name: str, R: int, hd: int) -> int:
     """Row stride of a [R][heads][hd] tensor whose rows hold their heads one after the other."""
-    if t.dim() != 3 or t.shape[0] != R or t.shape[2] != hd or (t.shape[1] > 1 and t.stride(1) != hd) or (hd > 1 and t.stride(2) != 1):
+    shape, stride = t.shape, t.stride()
+    if len(shape) != 3 or shape[0] != R or shape[2] != hd or (stride[1] != hd and shape[1] > 1) or (stride[2] != 1 and hd > 1):
         raise ValueError(f"{name} must be [{R}][heads][{hd}] with the heads of a row one after the other")
-    return t.stride(0) if R > 1 else max(t.stride(0), t.shape[1] * hd)
+    return stride[0] if R > 1 else shape[1] * hd
 
 
 def k_qk_norm_rope(q, k, q_norm, k_norm, cos, sin, pos, q_out, k_out, eps: float = 1e-5, stream: int = 0):
     """RMS norm (weights q_norm, k_norm fp32 [hd]) and rotation of the heads of q [R][nq][hd] and k [R][nkv][hd] (fp32 or
     bf16, views into fused rows included) into q_out, k_out (fp32 or bf16, may be the inputs).  cos, sin: fp32
     [n_pos][hd / 2]; pos: int32 [R], rows with a position outside the tables are left as they were."""
-    import torch
     R, nq, hd = q.shape
-    nkv = k.shape[1]
-    strides = [_heads(t, n, R, hd) for t, n in ((q, "q"), (k, "k"), (q_out, "q_out"), (k_out, "k_out"))]
+    ldq, ldk, ldqo, ldko = _heads(q, "q", R, hd), _heads(k, "k", R, hd), _heads(q_out, "q_out", R, hd), _heads(k_out, "k_out", R, hd)
     if q.dtype != k.dtype or q_out.dtype != k_out.dtype or q_out.shape != q.shape or k_out.shape != k.shape:
         raise ValueError("q and k must have one type, and the outputs theirs and the inputs' shapes")
-    n_pos = cos.shape[0]
-    for t, n, s in ((q_norm, "q_norm", (hd,)), (k_norm, "k_norm", (hd,)), (cos, "cos", (n_pos, hd // 2)), (sin, "sin", (n_pos, hd // 2))):
-        _flat(t, n, s, (torch.float32,))
-    _flat(pos, "pos", (R,), (torch.int32,))
+    n_pos, table = cos.shape[0], (cos.shape[0], hd // 2)
+    gq, gk = _flat(q_norm, "q_norm", (hd,), SPEC_F32), _flat(k_norm, "k_norm", (hd,), SPEC_F32)
+    cp, sp, pp = _flat(cos, "cos", table, SPEC_F32), _flat(sin, "sin", table, SPEC_F32), _i32(pos, "pos", (R,))
     _here(q, k, q_norm, k_norm, cos, sin, pos, q_out, k_out)
-    _ops_chk(load().spec_k_qk_norm_rope(q.data_ptr(), strides[0], nq, k.data_ptr(), strides[1], nkv, _kind(q), hd, R,
-                                        q_norm.data_ptr(), k_norm.data_ptr(), eps, cos.data_ptr(), sin.data_ptr(), n_pos,
-                                        pos.data_ptr(), q_out.data_ptr(), strides[2], k_out.data_ptr(), strides[3],
-                                        _kind(q_out), stream), "spec_k_qk_norm_rope")
+    _ops_chk(load().spec_k_qk_norm_rope(q.data_ptr(), ldq, nq, k.data_ptr(), ldk, k.shape[1], _kind(q), hd, R, gq, gk, eps, cp,
+                                        sp, n_pos, pp, q_out.data_ptr(), ldqo, k_out.data_ptr(), ldko, _kind(q_out), stream),
+             "spec_k_qk_norm_rope")

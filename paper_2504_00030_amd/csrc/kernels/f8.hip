@@ -2,12 +2,18 @@
 //
 //   y[r][n] = sum_b xs[b][r] ws[n / 128][b] sum_{k in block b} x[r][k] w[n][k],   blocks of 128 columns
 //
-// v_mfma_f32_16x16x128_f8f6f4 multiplies exactly one block: its result, started from zero, is the inner sum of 16 rows
-// of w by 16 rows of x, and one fused multiply-add per element adds it to the fp32 accumulators with the product of
-// the two scales.  w is the first operand, so a lane's four results are four neighbouring columns of one row of y:
-// they share one scale product, and they are stored together.  The instruction's k order inside a block is free as
-// long as both operands use the same one: lane l holds row l % 16 and the 16-byte chunks l / 16 and l / 16 + 4 of the
-// block's eight, so that each load of a wave covers whole halves of 128-byte lines of the row-major operands.
+// The matrix instructions sum one block from zero, 16 rows of w by 16 rows of x, and one fused multiply-add per element
+// adds the result to the fp32 accumulators with the product of the two scales.  w is the first operand, so a lane's four
+// results are four neighbouring columns of one row of y: they share one scale product, and they are stored together.  The
+// k order inside a block is free as long as both operands use the same one: lane l holds row l % 16 and the 16-byte
+// chunks l / 16 and l / 16 + 4 of the block's eight, so that each load of a wave covers whole halves of 128-byte lines of
+// the row-major operands.
+//
+// How the products of a block are summed.  v_mfma_f32_16x16x128_f8f6f4 takes the whole block at once, at twice the rate
+// of the 16-bit instructions, but inside each group of eight neighbouring products it drops what lies below 2^-13 of the
+// power of two of the largest one (measured: 2^16 + 2^3 comes out whole, 2^16 + 2^2 as 2^16).  Its results are 3e-5 off in
+// the 2-norm.  A bf16 result rounds by 2e-3, and the instruction serves it; an fp32 result is summed from the values as
+// fp16 (which holds every e4m3 value, so the products are exact) by v_mfma_f32_16x16x32_f16, and is 1e-7 off.
 #include "common.hpp"
 #include "params.hpp"
 
@@ -69,22 +75,33 @@ __device__ __forceinline__ void store_y4(OT *y, const f4_t v, int n, int N, bool
 }  // namespace
 
 // ---- quantiser -------------------------------------------------------------------------------------------------
-// Sixteen lanes per block of 128 columns, eight columns each.
+// Sixteen lanes per block of 128 columns, eight columns each: x is read once, and the block's largest is four shuffles
+// away.  VEC: the rows start on 16 bytes, so that the eight columns are one or two loads.
 template <typename T, bool VEC>
 __global__ __launch_bounds__(256) void quant_f8_k(const T *__restrict__ x, int64_t ldx, int R, int K, int KB,
                                                   uint8_t *__restrict__ q, float *__restrict__ scale) {
-    const int64_t grp = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4);
+    const uint32_t grp = blockIdx.x * 16 + (threadIdx.x >> 4);  // below 2^31 + 16: the host bounds R * KB
     const int sub = threadIdx.x & 15;
-    if (grp >= (int64_t)R * KB) return;
-    const int r = (int)(grp / KB), b = (int)(grp % KB);
+    const uint32_t r = grp / KB, b = grp % KB;
+    if (r >= (uint32_t)R) return;
     const int k = b * F8_BLOCK + sub * 8;
     float v[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = 0.f;
     if (k < K) {
         const T *p = x + (int64_t)r * ldx + k;
+        if constexpr (VEC && sizeof(T) == 4) {
+            const f4_t u0 = *reinterpret_cast<const f4_t *>(p), u1 = *reinterpret_cast<const f4_t *>(p + 4);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = (float)p[i];
+            for (int i = 0; i < 4; ++i) { v[i] = u0[i]; v[4 + i] = u1[i]; }
+        } else if constexpr (VEC) {
+            const u4_t u = *reinterpret_cast<const u4_t *>(p);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = i % 2 ? bf16_hi(u[i / 2]) : bf16_lo(u[i / 2]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = (float)p[i];
+        }
     }
     float a = F8_LEAST;
 #pragma unroll
@@ -92,20 +109,26 @@ __global__ __launch_bounds__(256) void quant_f8_k(const T *__restrict__ x, int64
 #pragma unroll
     for (int m = 8; m >= 1; m >>= 1) a = fmaxf(a, __shfl_xor(a, m, WAVE));
     const float f = F8_MAX / a;
-    if (k < K) {
-        *reinterpret_cast<uint2 *>(q + (int64_t)r * K + k) = make_uint2(quant4(v, f), quant4(v + 4, f));
-    }
+    if (k < K) *reinterpret_cast<uint2 *>(q + (int64_t)r * K + k) = make_uint2(quant4(v, f), quant4(v + 4, f));
     if (sub == 0) scale[(int64_t)b * R + r] = a / F8_MAX;
+}
+
+template <typename T>
+static void launch_quant_t(const void *x, int64_t ldx, int R, int K, int KB, void *q, float *scale, dim3 grid, hipStream_t s) {
+    const T *p = reinterpret_cast<const T *>(x);
+    uint8_t *o = reinterpret_cast<uint8_t *>(q);
+    if (reinterpret_cast<uintptr_t>(x) % 16 == 0 && ldx * sizeof(T) % 16 == 0)
+        hipLaunchKernelGGL((quant_f8_k<T, true>), grid, dim3(256), 0, s, p, ldx, R, K, KB, o, scale);
+    else
+        hipLaunchKernelGGL((quant_f8_k<T, false>), grid, dim3(256), 0, s, p, ldx, R, K, KB, o, scale);
 }
 
 hipError_t launch_quant_f8(const void *x, int dtype, int64_t ldx, int R, int K, void *q, float *scale, hipStream_t s) {
     const int KB = (K + F8_BLOCK - 1) / F8_BLOCK;
-    const int64_t wgs = ((int64_t)R * KB + 15) / 16;
-    if (wgs > 0x7fffffff) return hipErrorInvalidValue;
-    const dim3 grid((unsigned)wgs), block(256);
-    uint8_t *qo = reinterpret_cast<uint8_t *>(q);
-    if (dtype == DT_F32) hipLaunchKernelGGL((quant_f8_k<float, false>), grid, block, 0, s, reinterpret_cast<const float *>(x), ldx, R, K, KB, qo, scale);
-    else hipLaunchKernelGGL((quant_f8_k<__bf16, false>), grid, block, 0, s, reinterpret_cast<const __bf16 *>(x), ldx, R, K, KB, qo, scale);
+    if ((int64_t)R * KB > 0x7fffffff) return hipErrorInvalidValue;
+    const dim3 grid((unsigned)(((int64_t)R * KB + 15) / 16));
+    if (dtype == DT_F32) launch_quant_t<float>(x, ldx, R, K, KB, q, scale, grid, s);
+    else launch_quant_t<__bf16>(x, ldx, R, K, KB, q, scale, grid, s);
     return hipGetLastError();
 }
 
@@ -278,11 +301,197 @@ static hipError_t launch_stream(const F8Args &a, hipStream_t s) {
     return hipGetLastError();
 }
 
+// ---- product: tiles in LDS -------------------------------------------------------------------------------------
+// A workgroup computes TN columns by TR rows of y with PN x PR waves.  A stage of LDS holds one block of k of both
+// operands; two stages alternate, and while one multiplies, the next is on its way from memory straight into the other
+// (16 bytes a lane, no registers).  The two stages are two arrays, and the loop is unrolled over them: the compiler then
+// sees that fragment reads do not touch the stage in flight and does not wait for it.  A row of a stage is 128 bytes,
+// eight chunks; position p of row i holds chunk p ^ (i / 2 % 8), which spreads the sixteen rows a fragment read touches
+// over all banks.
+// F16: the fragments are turned into fp16 (exact sums), otherwise multiplied as e4m3.
+template <typename OT, bool F16, int TN, int TR, int PN, int PR>
+__global__ __launch_bounds__(64 * PN * PR, 2) void f8_tile_k(const F8Args a, const int n_tiles, const int r_tiles) {
+    constexpr int NT = 64 * PN * PR, WN = TN / PN / 16, WR = TR / PR / 16;
+    constexpr int LW = TN * 8 / NT, LX = TR * 8 / NT;  // 16-byte chunks a thread moves per stage
+    constexpr int LAG = 2;                             // matrix instructions between a tile's own and its additions
+    __shared__ __attribute__((aligned(16))) uint8_t stage0[(TN + TR) * F8_BLOCK];
+    __shared__ __attribute__((aligned(16))) uint8_t stage1[(TN + TR) * F8_BLOCK];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int sub = lane & 15, g = lane >> 4;
+    const int wn = wave % PN, wr = wave / PN;
+    // consecutive workgroups go round the eight XCDs: each takes one run of tiles, in bands of eight tiles of rows, so that
+    // the tiles it works on together share rows of w and x in its L2
+    const int total = n_tiles * r_tiles, per = (total + 7) >> 3;
+    const int t = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
+    if (t >= total) return;
+    const int band = t / (8 * n_tiles), in_band = t % (8 * n_tiles), rows_in_band = min(8, r_tiles - band * 8);
+    const int n0 = in_band / rows_in_band * TN, r0 = (band * 8 + in_band % rows_in_band) * TR;
+    const int K = a.K, KB = a.KB;
+    const uint8_t *wb = a.w + (int64_t)n0 * K, *xb = reinterpret_cast<const uint8_t *>(a.x) + (int64_t)r0 * K;
+
+    // a thread moves chunk `chunk` of rows row + i NT / 8; in the tiles at the edge rows past the last repeat it
+    const int row = tid >> 3, chunk = (tid & 7) ^ ((tid >> 4) & 7);
+    const bool edge_n = n0 + TN > a.N, edge_r = r0 + TR > a.R;
+    const uint32_t own = (uint32_t)row * (uint32_t)K;
+    auto copy = [&](const uint8_t *from, uint32_t o, uint8_t *to) {  // 16 bytes a lane, to 1 KiB of LDS per wave
+        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(from + o),
+                                         (__attribute__((address_space(3))) void *)to, 16, 0, 0);
+    };
+    auto issue = [&](int b, uint8_t *to) {
+        // a chunk past the end of the rows reads the block's first one; it is zeroed before the block is multiplied
+        const uint32_t c = b * F8_BLOCK + chunk * 16 < K ? chunk * 16 : 0;
+        const uint8_t *w = wb + b * F8_BLOCK, *x = xb + b * F8_BLOCK;
+        to += wave * 1024;
+        if (!edge_n) {
+#pragma unroll
+            for (int i = 0; i < LW; ++i) copy(w + (int64_t)i * (NT / 8) * K, own + c, to + i * NT * 16);
+        } else {
+#pragma unroll
+            for (int i = 0; i < LW; ++i) copy(w, (uint32_t)min(row + i * (NT / 8), a.N - 1 - n0) * (uint32_t)K + c, to + i * NT * 16);
+        }
+        to += TN * F8_BLOCK;
+        if (!edge_r) {
+#pragma unroll
+            for (int i = 0; i < LX; ++i) copy(x + (int64_t)i * (NT / 8) * K, own + c, to + i * NT * 16);
+        } else {
+#pragma unroll
+            for (int i = 0; i < LX; ++i) copy(x, (uint32_t)min(row + i * (NT / 8), a.R - 1 - r0) * (uint32_t)K + c, to + i * NT * 16);
+        }
+    };
+    f4_t acc[WN][WR];
+#pragma unroll
+    for (int i = 0; i < WN; ++i)
+#pragma unroll
+        for (int j = 0; j < WR; ++j) acc[i][j] = f4_t{0.f, 0.f, 0.f, 0.f};
+    uint32_t so[WR];
+#pragma unroll
+    for (int j = 0; j < WR; ++j) so[j] = min(r0 + (wr * WR + j) * 16 + sub, a.R - 1);
+    const float *wsp = a.ws + (int64_t)(min(n0 + wn * WN * 16, a.N - 1) / F8_BLOCK) * KB;
+    float xs[WR], ws;
+    auto scales = [&](int b) {
+        const float *p = a.xs + (int64_t)b * a.R;
+#pragma unroll
+        for (int j = 0; j < WR; ++j) xs[j] = p[so[j]];
+        ws = wsp[b];
+    };
+    const int f0 = sub * F8_BLOCK + ((g ^ (sub >> 1)) * 16), f1 = f0 ^ 64;
+    auto frag = [&](const uint8_t *p, u4_t &c0, u4_t &c1) {
+        c0 = *reinterpret_cast<const u4_t *>(p + f0);
+        c1 = *reinterpret_cast<const u4_t *>(p + f1);
+    };
+    auto add = [&](int i, int j, const f4_t t, float sc) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[i][j][e] = fmaf(t[e], sc, acc[i][j][e]);
+        asm volatile("" : "+v"(acc[i][j]));  // no instruction: keeps the additions in front of the barrier at the step's end
+    };
+    auto step = [&](int b, uint8_t *cur, uint8_t *nxt) {
+        float sc[WR];
+#pragma unroll
+        for (int j = 0; j < WR; ++j) sc[j] = xs[j] * ws;
+        if (b + 1 < KB) issue(b + 1, nxt);
+        scales(min(b + 1, KB - 1));
+        if ((b + 1) * F8_BLOCK > K) {  // the last block is short: the missing columns of x count as zeros
+            if (b * F8_BLOCK + chunk * 16 >= K) {
+#pragma unroll
+                for (int i = 0; i < LX; ++i) *reinterpret_cast<u4_t *>(cur + TN * F8_BLOCK + (i * NT + tid) * 16) = u4_t{0, 0, 0, 0};
+            }
+            __syncthreads();
+        }
+        const uint8_t *lw = cur + wn * WN * 16 * F8_BLOCK, *lx = cur + (TN + wr * WR * 16) * F8_BLOCK;
+        // Matrix instructions and vector instructions of one wave alternate (the scheduler would group them, and each
+        // unit would wait for the other): the additions of a tile follow matrix instructions issued after its own.
+        if constexpr (F16) {
+            h8_t hx[WR][4], hw[2][4];
+            f4_t t[2][WR];
+            auto wide = [&](const uint8_t *p, h8_t (&h)[4]) {
+                u4_t c0, c1;
+                frag(p, c0, c1);
+                h[0] = to_f16(c0[0], c0[1]); h[1] = to_f16(c0[2], c0[3]);
+                h[2] = to_f16(c1[0], c1[1]); h[3] = to_f16(c1[2], c1[3]);
+            };
+#pragma unroll
+            for (int j = 0; j < WR; ++j) wide(lx + j * 16 * F8_BLOCK, hx[j]);
+            wide(lw, hw[0]);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int i = 0; i < WN; ++i) {
+                if (i + 1 < WN) wide(lw + (i + 1) * 16 * F8_BLOCK, hw[(i + 1) & 1]);
+#pragma unroll
+                for (int j = 0; j < WR; ++j) t[i & 1][j] = f4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+#pragma unroll
+                    for (int j = 0; j < WR; ++j)
+                        t[i & 1][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(hw[i & 1][q], hx[j][q], t[i & 1][j], 0, 0, 0);
+                if (i > 0) {
+#pragma unroll
+                    for (int j = 0; j < WR; ++j) add(i - 1, j, t[(i - 1) & 1][j], sc[j]);
+                }
+#pragma unroll
+                for (int q = 0; q < 4 * WR; ++q) {
+                    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);  // one matrix instruction
+                    __builtin_amdgcn_sched_group_barrier(0x002, 2, 0);  // two vector instructions
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+#pragma unroll
+            for (int j = 0; j < WR; ++j) add(WN - 1, j, t[(WN - 1) & 1][j], sc[j]);
+        } else {
+            u4_t x0[WR], x1[WR], w0[2], w1[2];
+            f4_t t[4];
+            frag(lw, w0[0], w1[0]);
+#pragma unroll
+            for (int j = 0; j < WR; ++j) frag(lx + j * 16 * F8_BLOCK, x0[j], x1[j]);
+#pragma unroll
+            for (int u = 0; u < WN * WR; ++u) {
+                const int i = u / WR, j = u % WR;
+                if (j == 0 && i + 1 < WN) frag(lw + (i + 1) * 16 * F8_BLOCK, w0[(i + 1) & 1], w1[(i + 1) & 1]);
+                t[u & 3] = mfma_f8(w0[i & 1], w1[i & 1], x0[j], x1[j]);
+                __builtin_amdgcn_sched_barrier(0);
+                if (u >= LAG) add((u - LAG) / WR, (u - LAG) % WR, t[(u - LAG) & 3], sc[(u - LAG) % WR]);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+#pragma unroll
+            for (int u = WN * WR - LAG; u < WN * WR; ++u) add(u / WR, u % WR, t[u & 3], sc[u % WR]);
+        }
+        __syncthreads();
+    };
+    issue(0, stage0);
+    scales(0);
+    __syncthreads();
+    for (int b = 0; b < KB; b += 2) {
+        step(b, stage0, stage1);
+        if (b + 1 < KB) step(b + 1, stage1, stage0);
+    }
+    OT *y = reinterpret_cast<OT *>(a.y);
+    const bool aligned = a.ldy % 4 == 0 && reinterpret_cast<uintptr_t>(a.y) % (4 * sizeof(OT)) == 0;
+#pragma unroll
+    for (int j = 0; j < WR; ++j) {
+        const int r = r0 + (wr * WR + j) * 16 + sub;
+        if (r >= a.R) continue;
+#pragma unroll
+        for (int i = 0; i < WN; ++i) store_y4(y + (int64_t)r * a.ldy, acc[i][j], n0 + (wn * WN + i) * 16 + 4 * g, a.N, aligned);
+    }
+}
+
+template <typename OT, bool F16, int TN, int TR, int PN, int PR>
+static hipError_t launch_tile(const F8Args &a, hipStream_t s) {
+    const int64_t n_tiles = (a.N + TN - 1) / TN, r_tiles = (a.R + TR - 1) / TR;
+    if (n_tiles * r_tiles > 0x7ffffff0 || 8 * n_tiles > 0x7fffffff) return hipErrorInvalidValue;
+    const int64_t per = (n_tiles * r_tiles + 7) / 8;
+    hipLaunchKernelGGL((f8_tile_k<OT, F16, TN, TR, PN, PR>), dim3((unsigned)(8 * per)), dim3(64 * PN * PR), 0, s, a, (int)n_tiles,
+                       (int)r_tiles);
+    return hipGetLastError();
+}
+
 template <typename OT>
 static hipError_t launch_gemm_f8_t(const F8Args &a, hipStream_t s) {
     if (a.R <= 16) return launch_stream<OT, 1, 1, 8, 1, X_F8>(a, s);
     if (a.R <= 32) return launch_stream<OT, 1, 2, 8, 1, X_F8>(a, s);
-    return launch_stream<OT, 2, 4, 8, 1, X_F8>(a, s);
+    auto tiles = [&](int64_t t) { return (a.N + t - 1) / t * ((a.R + t - 1) / t); };
+    if (sizeof(OT) == 4) return tiles(128) >= 256 ? launch_tile<OT, true, 128, 128, 2, 2>(a, s) : launch_tile<OT, true, 64, 64, 2, 2>(a, s);
+    if (tiles(256) >= 256) return launch_tile<OT, false, 256, 256, 2, 4>(a, s);
+    return tiles(128) >= 256 ? launch_tile<OT, false, 128, 128, 2, 2>(a, s) : launch_tile<OT, false, 64, 64, 2, 2>(a, s);
 }
 
 hipError_t launch_gemm_f8(const F8Args &a, hipStream_t s) {

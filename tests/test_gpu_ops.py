@@ -4,7 +4,10 @@ Tolerances, derived from the number formats.  A sum of n fp32 terms in any order
 sum of their magnitudes (2^-24 a rounding to nearest, twice that where an adder truncates).
   product: 128 terms inside a block, the scale product and its multiplication (3 roundings), one addition per block:
            (128 + 3 + blocks) 2^-23 of the sum of magnitudes, then half a step of the output type (bf16: 2^-8 of the value,
-           fp32: 2^-24);
+           fp32: 2^-24).  For a bf16 result the kernels may sum each group of eight products in the e4m3 matrix
+           instruction, which drops what lies below 2^-13 of the power of two of the group's largest product: each of the
+           other seven loses less than 2^-13 of that product, and that product is at most the sum of the group's magnitudes, so
+           the loss is below 7 2^-13 of the sum of magnitudes;
   norm:    the mean of hd squares is off by (hd + 1) 2^-23 of itself, its root by half that; then the division, the two
            products and the two rotations round 6 times: (hd / 2 + 8) 2^-23 of the magnitudes of the two terms, then half a
            step of the output type;
@@ -48,7 +51,8 @@ def _activations(rng, R, K, dtype):
 
 
 def _product_tol(mag, y, KB, dtype):
-    return (128 + 3 + KB) * 2.0 ** -23 * mag + HALF_STEP[dtype] * np.abs(y) + 1e-38
+    sums = (128 + 3 + KB) * 2.0 ** -23 + (7 * 2.0 ** -13 if dtype == BF16 else 0.0)
+    return sums * mag * (1 + HALF_STEP[dtype]) + HALF_STEP[dtype] * np.abs(y) + 1e-38
 
 
 def _gemm_case(rng, R, N, K, x_kind, y_dtype, ldy_extra=0):
