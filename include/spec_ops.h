@@ -28,13 +28,13 @@ enum { SPEC_F8 = 3 };
  *     a = max(max |x|, 2^-96),  scale = a / 448,  q = e4m3(x * (448 / a)),
  * quotients and product in fp32, each rounded to nearest even.  x: device, dtype SPEC_F32 or SPEC_BF16, row r at element
  * r * ldx (ldx >= K), any alignment of its element type; q: device e4m3 [R][K], 16-byte aligned; scale: device fp32 [ceil(K / 128)][R]
- * (the product reads the scales of a block of columns together).  K >= 16, K % 16 == 0.  A NaN stays a NaN in its
+ * (the product reads the scales of a block of columns together).  16 <= K <= 2^22, K % 16 == 0.  A NaN stays a NaN in its
  * place; a block with an infinity gets an infinite scale, and products over it are NaN. */
 int spec_k_quant_f8(const void *x, int32_t dtype, int64_t ldx, int32_t R, int32_t K, void *q, float *scale, void *stream);
 
 /* y[r][n] = sum over blocks b of x_scale[b][r] * w_scale[n / 128][b] * sum over k in block b of x[r][k] * w[n][k].
  * w: device e4m3 [N][K] row-major as a checkpoint holds it, 16-byte aligned; w_scale: device fp32 [ceil(N / 128)][ceil(K /
- * 128)]; N >= 1, K >= 16, K % 16 == 0.  y: device, y_dtype SPEC_F32 or SPEC_BF16, row r at element r * ldy (ldy >= N),
+ * 128)]; N >= 1, 16 <= K <= 2^22, K % 16 == 0.  y: device, y_dtype SPEC_F32 or SPEC_BF16, row r at element r * ldy (ldy >= N),
  * columns N .. ldy - 1 are left alone.  Sums are held in fp32.
  *  - x_dtype SPEC_F8: x e4m3 [R][K] (ldx == K), 16-byte aligned, with x_scale device fp32 [ceil(K / 128)][R], both as
  *    spec_k_quant_f8 leaves them.

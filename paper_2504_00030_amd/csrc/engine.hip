@@ -1687,7 +1687,8 @@ static size_t width(int32_t dtype) { return dtype == SPEC_F32 ? 4 : 2; }
 
 int spec_k_quant_f8(const void *x, int32_t dtype, int64_t ldx, int32_t R, int32_t K, void *q, float *scale, void *stream) {
     if (!wide(dtype)) return refuse(SPEC_EINVAL, "quant_f8: x must be fp32 or bf16");
-    if (R < 0 || K < 16 || K % 16 || ldx < K) return refuse(SPEC_EINVAL, "quant_f8: R < 0, K not a positive multiple of 16, or ldx < K");
+    if (R < 0 || K < 16 || K > F8_K_MAX || K % 16 || ldx < K)
+        return refuse(SPEC_EINVAL, "quant_f8: R < 0, K not a multiple of 16 in 16 .. 2^22, or ldx < K");
     if (R == 0) return SPEC_OK;
     if (!x || !q || !scale) return refuse(SPEC_EINVAL, "quant_f8: null pointer");
     if (off(x, width(dtype)) || off(q, 16) || off(scale, 4)) return refuse(SPEC_EINVAL, "quant_f8: misaligned pointer");
@@ -1695,8 +1696,8 @@ int spec_k_quant_f8(const void *x, int32_t dtype, int64_t ldx, int32_t R, int32_
 }
 
 int64_t spec_k_gemm_f8_workspace(int32_t K, int32_t R, int32_t x_dtype) {
-    if (K < 16 || K % 16 || R < 0 || (x_dtype != SPEC_F8 && !wide(x_dtype)))
-        return refuse(SPEC_EINVAL, "gemm_f8_workspace: R < 0, K not a positive multiple of 16, or unknown type of x");
+    if (K < 16 || K > F8_K_MAX || K % 16 || R < 0 || (x_dtype != SPEC_F8 && !wide(x_dtype)))
+        return refuse(SPEC_EINVAL, "gemm_f8_workspace: R < 0, K not a multiple of 16 in 16 .. 2^22, or unknown type of x");
     return x_dtype == SPEC_F8 ? 0 : (int64_t)132 * R * ((K + 127) / 128);
 }
 
@@ -1705,8 +1706,8 @@ int spec_k_gemm_f8(const void *w, const float *w_scale, int32_t N, int32_t K, co
                    int64_t workspace_bytes, void *stream) {
     const bool f8 = x_dtype == SPEC_F8;
     if ((!f8 && !wide(x_dtype)) || !wide(y_dtype)) return refuse(SPEC_EINVAL, "gemm_f8: x must be e4m3, fp32 or bf16, y fp32 or bf16");
-    if (N < 1 || K < 16 || K % 16 || R < 0 || ldx < K || ldy < N || workspace_bytes < 0 || (f8 && ldx != K))
-        return refuse(SPEC_EINVAL, "gemm_f8: N < 1, R < 0, K not a positive multiple of 16, or a row stride that does not fit");
+    if (N < 1 || K < 16 || K > F8_K_MAX || K % 16 || R < 0 || ldx < K || ldy < N || workspace_bytes < 0 || (f8 && ldx != K))
+        return refuse(SPEC_EINVAL, "gemm_f8: N < 1, R < 0, K not a multiple of 16 in 16 .. 2^22, or a row stride that does not fit");
     if (R == 0) return SPEC_OK;
     if (!w || !w_scale || !x || !y || (f8 ? !x_scale : x_scale != nullptr))
         return refuse(SPEC_EINVAL, "gemm_f8: null pointer (x_scale goes with e4m3 rows, and only with them)");
@@ -1725,6 +1726,12 @@ int spec_k_gemm_f8(const void *w, const float *w_scale, int32_t N, int32_t K, co
         const int rc = launched(launch_quant_f8(x, x_dtype, ldx, R, K, q, scale, st), "gemm_f8: launch failed");
         if (rc != SPEC_OK) return rc;
         a.x = q; a.xs = scale; a.ldx = K; a.x_type = 0;
+    }
+    // what the quantised rows leave of the workspace is for partial sums
+    const int64_t used = (need + 255) & ~(int64_t)255;
+    if (workspace && workspace_bytes > used) {
+        a.part = reinterpret_cast<float *>(reinterpret_cast<uint8_t *>(workspace) + used);
+        a.part_bytes = workspace_bytes - used;
     }
     return launched(launch_gemm_f8(a, st), "gemm_f8: launch failed");
 }

@@ -18,6 +18,7 @@
 #include "params.hpp"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace sd {
 
@@ -49,6 +50,18 @@ __device__ __forceinline__ h8_t to_f16(uint32_t lo, uint32_t hi) {
     const h2_t a = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.f, false), b = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.f, true);
     const h2_t c = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.f, false), d = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.f, true);
     return h8_t{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+
+// a lane's 32 values of a fragment as fp16, and the two of its dwords `v` of them alone
+__device__ __forceinline__ void widen(const u4_t &c0, const u4_t &c1, h8_t (&h)[4]) {
+    h[0] = to_f16(c0[0], c0[1]); h[1] = to_f16(c0[2], c0[3]);
+    h[2] = to_f16(c1[0], c1[1]); h[3] = to_f16(c1[2], c1[3]);
+}
+__device__ __forceinline__ void widen2(const u4_t &c0, const u4_t &c1, h8_t (&h)[4], int v) {
+    const uint32_t d = v < 4 ? c0[v] : c1[v - 4];
+    const h2_t a = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(d, 1.f, false), b = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(d, 1.f, true);
+    h[v >> 1][(v & 1) * 4] = a[0]; h[v >> 1][(v & 1) * 4 + 1] = a[1];
+    h[v >> 1][(v & 1) * 4 + 2] = b[0]; h[v >> 1][(v & 1) * 4 + 3] = b[1];
 }
 
 // four values scaled and rounded to e4m3
@@ -310,7 +323,7 @@ static hipError_t launch_stream(const F8Args &a, hipStream_t s) {
 // over all banks.
 // F16: the fragments are turned into fp16 (exact sums), otherwise multiplied as e4m3.
 template <typename OT, bool F16, int TN, int TR, int PN, int PR>
-__global__ __launch_bounds__(64 * PN * PR, 2) void f8_tile_k(const F8Args a, const int n_tiles, const int r_tiles) {
+__global__ __launch_bounds__(64 * PN * PR, 2) void f8_tile_k(const F8Args a, const int n_tiles, const int r_tiles, const int shares) {
     constexpr int NT = 64 * PN * PR, WN = TN / PN / 16, WR = TR / PR / 16;
     constexpr int LW = TN * 8 / NT, LX = TR * 8 / NT;  // 16-byte chunks a thread moves per stage
     constexpr int LAG = 2;                             // matrix instructions between a tile's own and its additions
@@ -321,57 +334,49 @@ __global__ __launch_bounds__(64 * PN * PR, 2) void f8_tile_k(const F8Args a, con
     const int wn = wave % PN, wr = wave / PN;
     // consecutive workgroups go round the eight XCDs: each takes one run of tiles, in bands of eight tiles of rows, so that
     // the tiles it works on together share rows of w and x in its L2
-    const int total = n_tiles * r_tiles, per = (total + 7) >> 3;
-    const int t = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
-    if (t >= total) return;
-    const int band = t / (8 * n_tiles), in_band = t % (8 * n_tiles), rows_in_band = min(8, r_tiles - band * 8);
+    // (a tile's shares of K stand side by side: they run together)
+    const int total = n_tiles * r_tiles * shares, per = (total + 7) >> 3;
+    const int id = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
+    if (id >= total || (int)(blockIdx.x >> 3) >= per) return;
+    const int tile = id / shares, share = id % shares;
+    const int band = tile / (8 * n_tiles), in_band = tile % (8 * n_tiles), rows_in_band = min(8, r_tiles - band * 8);
     const int n0 = in_band / rows_in_band * TN, r0 = (band * 8 + in_band % rows_in_band) * TR;
-    const int K = a.K, KB = a.KB;
-    const uint8_t *wb = a.w + (int64_t)n0 * K, *xb = reinterpret_cast<const uint8_t *>(a.x) + (int64_t)r0 * K;
+    // this share's blocks of K; from here on K and KB are those of the share
+    const int b_share = (int)((int64_t)a.KB * share / shares);
+    const int KB = (int)((int64_t)a.KB * (share + 1) / shares) - b_share, ld = a.K, K = min(ld - b_share * F8_BLOCK, KB * F8_BLOCK);
+    const uint8_t *wb = a.w + (int64_t)n0 * ld + b_share * F8_BLOCK;
+    const uint8_t *xb = reinterpret_cast<const uint8_t *>(a.x) + (int64_t)r0 * ld + b_share * F8_BLOCK;
 
-    // a thread moves chunk `chunk` of rows row + i NT / 8; in the tiles at the edge rows past the last repeat it
+    // copy i of a thread moves chunk `chunk` of row `row` + i NT / 8 of w, or of x for i >= LW; rows past the last repeat it
     const int row = tid >> 3, chunk = (tid & 7) ^ ((tid >> 4) & 7);
-    const bool edge_n = n0 + TN > a.N, edge_r = r0 + TR > a.R;
-    const uint32_t own = (uint32_t)row * (uint32_t)K;
-    auto copy = [&](const uint8_t *from, uint32_t o, uint8_t *to) {  // 16 bytes a lane, to 1 KiB of LDS per wave
-        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(from + o),
-                                         (__attribute__((address_space(3))) void *)to, 16, 0, 0);
-    };
-    auto issue = [&](int b, uint8_t *to) {
+    const int last_n = a.N - 1 - n0, last_r = a.R - 1 - r0;
+    // the rows of this tile as buffers (a tile's rows span less than 2^31 bytes: the host bounds K)
+    const __amdgpu_buffer_rsrc_t wbuf = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(wb), 0, min(TN - 1, last_n) * ld + K, 0x27000);
+    const __amdgpu_buffer_rsrc_t xbuf = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(xb), 0, min(TR - 1, last_r) * ld + K, 0x27000);
+    auto copy = [&](int b, int i, uint8_t *stage) {  // 16 bytes a lane, 1 KiB of LDS a wave
         // a chunk past the end of the rows reads the block's first one; it is zeroed before the block is multiplied
         const uint32_t c = b * F8_BLOCK + chunk * 16 < K ? chunk * 16 : 0;
-        const uint8_t *w = wb + b * F8_BLOCK, *x = xb + b * F8_BLOCK;
-        to += wave * 1024;
-        if (!edge_n) {
-#pragma unroll
-            for (int i = 0; i < LW; ++i) copy(w + (int64_t)i * (NT / 8) * K, own + c, to + i * NT * 16);
-        } else {
-#pragma unroll
-            for (int i = 0; i < LW; ++i) copy(w, (uint32_t)min(row + i * (NT / 8), a.N - 1 - n0) * (uint32_t)K + c, to + i * NT * 16);
-        }
-        to += TN * F8_BLOCK;
-        if (!edge_r) {
-#pragma unroll
-            for (int i = 0; i < LX; ++i) copy(x + (int64_t)i * (NT / 8) * K, own + c, to + i * NT * 16);
-        } else {
-#pragma unroll
-            for (int i = 0; i < LX; ++i) copy(x, (uint32_t)min(row + i * (NT / 8), a.R - 1 - r0) * (uint32_t)K + c, to + i * NT * 16);
-        }
+        const int ii = i < LW ? i : i - LW;
+        int own = row;
+        asm volatile("" : "+v"(own));  // no instruction: keeps the compiler from holding the offset of every copy in a register
+        const uint32_t o = __umul24(min(own + ii * (NT / 8), i < LW ? last_n : last_r), ld) + c;
+        uint8_t *to = stage + (i < LW ? 0 : TN * F8_BLOCK) + ii * NT * 16 + wave * 1024;
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(i < LW ? wbuf : xbuf, (__attribute__((address_space(3))) void *)to, 16, o,
+                                                 b * F8_BLOCK, 0, 0);
     };
     f4_t acc[WN][WR];
 #pragma unroll
     for (int i = 0; i < WN; ++i)
 #pragma unroll
         for (int j = 0; j < WR; ++j) acc[i][j] = f4_t{0.f, 0.f, 0.f, 0.f};
-    uint32_t so[WR];
-#pragma unroll
-    for (int j = 0; j < WR; ++j) so[j] = min(r0 + (wr * WR + j) * 16 + sub, a.R - 1);
-    const float *wsp = a.ws + (int64_t)(min(n0 + wn * WN * 16, a.N - 1) / F8_BLOCK) * KB;
+    const float *wsp = a.ws + (int64_t)(min(n0 + wn * WN * 16, a.N - 1) / F8_BLOCK) * a.KB + b_share;
     float xs[WR], ws;
     auto scales = [&](int b) {
-        const float *p = a.xs + (int64_t)b * a.R;
+        const char *p = reinterpret_cast<const char *>(a.xs + (int64_t)(b_share + b) * a.R + r0);
+        int own = wr * WR * 16 + sub;
+        asm volatile("" : "+v"(own));
 #pragma unroll
-        for (int j = 0; j < WR; ++j) xs[j] = p[so[j]];
+        for (int j = 0; j < WR; ++j) xs[j] = *reinterpret_cast<const float *>(p + (uint32_t)min(own + j * 16, last_r) * 4);
         ws = wsp[b];
     };
     const int f0 = sub * F8_BLOCK + ((g ^ (sub >> 1)) * 16), f1 = f0 ^ 64;
@@ -379,91 +384,143 @@ __global__ __launch_bounds__(64 * PN * PR, 2) void f8_tile_k(const F8Args a, con
         c0 = *reinterpret_cast<const u4_t *>(p + f0);
         c1 = *reinterpret_cast<const u4_t *>(p + f1);
     };
+    auto add1 = [&](int i, int j, int e, const f4_t t, float sc) {
+        acc[i][j][e] = fmaf(t[e], sc, acc[i][j][e]);
+        asm volatile("" : "+v"(acc[i][j][e]));  // no instruction: keeps the addition in front of the step's end
+    };
     auto add = [&](int i, int j, const f4_t t, float sc) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) acc[i][j][e] = fmaf(t[e], sc, acc[i][j][e]);
         asm volatile("" : "+v"(acc[i][j]));  // no instruction: keeps the additions in front of the barrier at the step's end
     };
-    auto step = [&](int b, uint8_t *cur, uint8_t *nxt) {
-        float sc[WR];
-#pragma unroll
-        for (int j = 0; j < WR; ++j) sc[j] = xs[j] * ws;
-        if (b + 1 < KB) issue(b + 1, nxt);
-        scales(min(b + 1, KB - 1));
-        if ((b + 1) * F8_BLOCK > K) {  // the last block is short: the missing columns of x count as zeros
+    // the last block may be short: its missing columns of x count as zeros
+    auto trim = [&](int b, uint8_t *stage) {
+        if ((b + 1) * F8_BLOCK > K) {
             if (b * F8_BLOCK + chunk * 16 >= K) {
 #pragma unroll
-                for (int i = 0; i < LX; ++i) *reinterpret_cast<u4_t *>(cur + TN * F8_BLOCK + (i * NT + tid) * 16) = u4_t{0, 0, 0, 0};
+                for (int i = 0; i < LX; ++i) *reinterpret_cast<u4_t *>(stage + TN * F8_BLOCK + (i * NT + tid) * 16) = u4_t{0, 0, 0, 0};
             }
             __syncthreads();
         }
-        const uint8_t *lw = cur + wn * WN * 16 * F8_BLOCK, *lx = cur + (TN + wr * WR * 16) * F8_BLOCK;
-        // Matrix instructions and vector instructions of one wave alternate (the scheduler would group them, and each
-        // unit would wait for the other): the additions of a tile follow matrix instructions issued after its own.
+    };
+    const int lw = wn * WN * 16 * F8_BLOCK, lx = (TN + wr * WR * 16) * F8_BLOCK;
+    u4_t x0[WR], x1[WR], w0[2], w1[2];
+    h8_t hx[F16 ? WR : 1][4], hw[2][4];  // fp16 fragments
+    // Step b multiplies the stage `cur` while block b + 1 is copied into `nxt`, CPR copies a row of tiles (all at once they
+    // would hold up the matrix instructions behind them).  Fragments are read a row of tiles ahead; in front of the last
+    // row, whose fragments are in registers by then, the workgroup meets: `nxt` is complete and nobody reads `cur` any
+    // more, and the first fragments of `nxt` are read behind the last row's instructions.
+    // Matrix and vector instructions of a wave alternate (left alone, the scheduler groups them, and each unit waits for
+    // the other): a tile's additions follow matrix instructions issued after its own.
+    constexpr int CPR = (LW + LX + WN / 2 - 1) / (WN / 2);
+    float sc[WR], nsc[WR];  // scales of this step and of the one to come
+    f4_t t[4];              // the last results; those of a step's last tiles are added in the next one
+#pragma unroll
+    for (int u = 0; u < 4; ++u) t[u] = f4_t{0.f, 0.f, 0.f, 0.f};
+    auto step = [&](int b, uint8_t *cur, uint8_t *nxt, auto more) {
+        float old[LAG];
+#pragma unroll
+        for (int q = 0; q < LAG; ++q) old[q] = sc[WR - LAG + q];
+#pragma unroll
+        for (int j = 0; j < WR; ++j) sc[j] = nsc[j];
+        auto meet = [&] {
+            __syncthreads();
+            trim(b + 1, nxt);
+            frag(nxt + lw, w0[0], w1[0]);
+#pragma unroll
+            for (int q = 0; q < WR; ++q) nsc[q] = xs[q] * ws;
+        };
         if constexpr (F16) {
-            h8_t hx[WR][4], hw[2][4];
-            f4_t t[2][WR];
-            auto wide = [&](const uint8_t *p, h8_t (&h)[4]) {
-                u4_t c0, c1;
-                frag(p, c0, c1);
-                h[0] = to_f16(c0[0], c0[1]); h[1] = to_f16(c0[2], c0[3]);
-                h[2] = to_f16(c1[0], c1[1]); h[3] = to_f16(c1[2], c1[3]);
-            };
 #pragma unroll
-            for (int j = 0; j < WR; ++j) wide(lx + j * 16 * F8_BLOCK, hx[j]);
-            wide(lw, hw[0]);
+            for (int j = 0; j < WR; ++j) widen(x0[j], x1[j], hx[j]);
             __builtin_amdgcn_sched_barrier(0);
+            // two tiles at a time: four matrix instructions each, in turn
 #pragma unroll
-            for (int i = 0; i < WN; ++i) {
-                if (i + 1 < WN) wide(lw + (i + 1) * 16 * F8_BLOCK, hw[(i + 1) & 1]);
+            for (int p = 0; p < WN * WR / 2; ++p) {
+                const int i = p / (WR / 2), jp = p % (WR / 2);
+                if (jp == 0 && i + 1 < WN) frag(cur + lw + (i + 1) * 16 * F8_BLOCK, w0[0], w1[0]);
+                if constexpr (more) {
+                    if (jp == 0 && i + 1 == WN) {
+                        meet();
 #pragma unroll
-                for (int j = 0; j < WR; ++j) t[i & 1][j] = f4_t{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int q = 0; q < 4; ++q)
-#pragma unroll
-                    for (int j = 0; j < WR; ++j)
-                        t[i & 1][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(hw[i & 1][q], hx[j][q], t[i & 1][j], 0, 0, 0);
-                if (i > 0) {
-#pragma unroll
-                    for (int j = 0; j < WR; ++j) add(i - 1, j, t[(i - 1) & 1][j], sc[j]);
-                }
-#pragma unroll
-                for (int q = 0; q < 4 * WR; ++q) {
-                    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);  // one matrix instruction
-                    __builtin_amdgcn_sched_group_barrier(0x002, 2, 0);  // two vector instructions
+                        for (int j = 0; j < WR; ++j) frag(nxt + lx + j * 16 * F8_BLOCK, x0[j], x1[j]);
+                    }
+                    if (jp == 0 && i == WN / 2 - 1) scales(b + 1);
                 }
                 __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int v = 0; v < 8; ++v) {
+                    const int q = v >> 1, u = 2 * p + (v & 1), j = u % WR;
+                    const f4_t z = {0.f, 0.f, 0.f, 0.f};
+                    t[u & 3] = __builtin_amdgcn_mfma_f32_16x16x32_f16(hw[i & 1][q], hx[j][q], q == 0 ? z : t[u & 3], 0, 0, 0);
+                    __builtin_amdgcn_sched_barrier(0);
+                    if constexpr (more) {
+                        const int k = i * CPR + jp * 8 + v;
+                        if (jp * 8 + v < CPR && i < WN / 2 && k < LW + LX) copy(b + 1, k, nxt);
+                    }
+                    const int d = u - 2;  // the pair before, one element of each tile at a time
+                    if (d >= 0) add1(d / WR, d % WR, q, t[d & 3], sc[d % WR]);
+                    else add1(WN - 1, WR + d, q, t[d & 3], old[LAG + d]);
+                    if (jp == WR / 2 - 1 && (i + 1 < WN || more)) widen2(w0[0], w1[0], hw[(i + 1) & 1], v);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
             }
-#pragma unroll
-            for (int j = 0; j < WR; ++j) add(WN - 1, j, t[(WN - 1) & 1][j], sc[j]);
         } else {
-            u4_t x0[WR], x1[WR], w0[2], w1[2];
-            f4_t t[4];
-            frag(lw, w0[0], w1[0]);
-#pragma unroll
-            for (int j = 0; j < WR; ++j) frag(lx + j * 16 * F8_BLOCK, x0[j], x1[j]);
 #pragma unroll
             for (int u = 0; u < WN * WR; ++u) {
                 const int i = u / WR, j = u % WR;
-                if (j == 0 && i + 1 < WN) frag(lw + (i + 1) * 16 * F8_BLOCK, w0[(i + 1) & 1], w1[(i + 1) & 1]);
+                if (j == 0 && i + 1 < WN) frag(cur + lw + (i + 1) * 16 * F8_BLOCK, w0[(i + 1) & 1], w1[(i + 1) & 1]);
+                if constexpr (more) {
+                    if (j == 0 && i + 1 == WN) meet();
+                    if (j == 0 && i == WN / 2 - 1) scales(b + 1);
+                }
+                __builtin_amdgcn_sched_barrier(0);
                 t[u & 3] = mfma_f8(w0[i & 1], w1[i & 1], x0[j], x1[j]);
                 __builtin_amdgcn_sched_barrier(0);
+                if constexpr (more) {
+                    if (i + 1 == WN) frag(nxt + lx + j * 16 * F8_BLOCK, x0[j], x1[j]);
+                    if (j % (WR / 2) == 0) {
+#pragma unroll
+                        for (int q = 0; q < (CPR + 1) / 2; ++q) {
+                            const int k = i * CPR + j / (WR / 2) * ((CPR + 1) / 2) + q;
+                            if (k < (i + 1) * CPR && k < LW + LX) copy(b + 1, k, nxt);
+                        }
+                    }
+                }
                 if (u >= LAG) add((u - LAG) / WR, (u - LAG) % WR, t[(u - LAG) & 3], sc[(u - LAG) % WR]);
+                else add(WN - 1, WR - LAG + u, t[(u - LAG) & 3], old[u]);
                 __builtin_amdgcn_sched_barrier(0);
             }
-#pragma unroll
-            for (int u = WN * WR - LAG; u < WN * WR; ++u) add(u / WR, u % WR, t[u & 3], sc[u % WR]);
         }
-        __syncthreads();
     };
-    issue(0, stage0);
+    static_assert(WN % 2 == 0 && WR % 2 == 0 && WN * WR % 4 == 0 && WR >= LAG, "the fragments of w alternate over whole steps");
+#pragma unroll
+    for (int i = 0; i < LW + LX; ++i) copy(0, i, stage0);
     scales(0);
     __syncthreads();
-    for (int b = 0; b < KB; b += 2) {
-        step(b, stage0, stage1);
-        if (b + 1 < KB) step(b + 1, stage1, stage0);
+    trim(0, stage0);
+#pragma unroll
+    for (int j = 0; j < WR; ++j) { nsc[j] = xs[j] * ws; sc[j] = 0.f; }
+    frag(stage0 + lw, w0[0], w1[0]);
+#pragma unroll
+    for (int j = 0; j < WR; ++j) frag(stage0 + lx + j * 16 * F8_BLOCK, x0[j], x1[j]);
+    if constexpr (F16) widen(w0[0], w1[0], hw[0]);
+    const std::true_type yes;
+    const std::false_type no;
+    int b = 0;
+    for (; b + 2 < KB; b += 2) {
+        step(b, stage0, stage1, yes);
+        step(b + 1, stage1, stage0, yes);
     }
-    OT *y = reinterpret_cast<OT *>(a.y);
+    if (b + 1 < KB) {
+        step(b, stage0, stage1, yes);
+        step(b + 1, stage1, stage0, no);
+    } else {
+        step(b, stage0, stage1, no);
+    }
+#pragma unroll
+    for (int q = 0; q < LAG; ++q) add(WN - 1, WR - LAG + q, t[(q - LAG) & 3], sc[WR - LAG + q]);
+    OT *y = reinterpret_cast<OT *>(a.y) + (int64_t)share * a.R * a.ldy;  // several shares: slabs of partial sums
     const bool aligned = a.ldy % 4 == 0 && reinterpret_cast<uintptr_t>(a.y) % (4 * sizeof(OT)) == 0;
 #pragma unroll
     for (int j = 0; j < WR; ++j) {
@@ -474,24 +531,73 @@ __global__ __launch_bounds__(64 * PN * PR, 2) void f8_tile_k(const F8Args a, con
     }
 }
 
+// y = sum of the shares' slabs, in their order
+template <typename OT>
+__global__ __launch_bounds__(256) void f8_sum_k(const float *__restrict__ part, int shares, int R, int N, OT *__restrict__ y, int64_t ldy) {
+    const int64_t slab = (int64_t)R * N;
+    const int n4 = (N + 3) >> 2;
+    const bool whole = N % 4 == 0, aligned = ldy % 4 == 0 && reinterpret_cast<uintptr_t>(y) % (4 * sizeof(OT)) == 0;
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i >= (int64_t)R * n4) return;
+    const int r = (int)(i / n4), n = (int)(i % n4) * 4;
+    const float *p = part + (int64_t)r * N + n;
+    f4_t v = {0.f, 0.f, 0.f, 0.f};
+    for (int s = 0; s < shares; ++s, p += slab) {
+        if (whole) {
+            v += *reinterpret_cast<const f4_t *>(p);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (n + e < N) v[e] += p[e];
+        }
+    }
+    store_y4(y + (int64_t)r * ldy, v, n, N, aligned);
+}
+
 template <typename OT, bool F16, int TN, int TR, int PN, int PR>
-static hipError_t launch_tile(const F8Args &a, hipStream_t s) {
-    const int64_t n_tiles = (a.N + TN - 1) / TN, r_tiles = (a.R + TR - 1) / TR;
-    if (n_tiles * r_tiles > 0x7ffffff0 || 8 * n_tiles > 0x7fffffff) return hipErrorInvalidValue;
-    const int64_t per = (n_tiles * r_tiles + 7) / 8;
-    hipLaunchKernelGGL((f8_tile_k<OT, F16, TN, TR, PN, PR>), dim3((unsigned)(8 * per)), dim3(64 * PN * PR), 0, s, a, (int)n_tiles,
-                       (int)r_tiles);
+static hipError_t launch_tile(const F8Args &a, int shares, hipStream_t s) {
+    const int64_t n_tiles = (a.N + TN - 1) / TN, r_tiles = (a.R + TR - 1) / TR, total = n_tiles * r_tiles * shares;
+    if (total > 0x7ffffff0 || 8 * n_tiles > 0x7fffffff) return hipErrorInvalidValue;
+    const dim3 grid((unsigned)((total + 7) / 8 * 8)), block(64 * PN * PR);
+    if (shares == 1) {
+        hipLaunchKernelGGL((f8_tile_k<OT, F16, TN, TR, PN, PR>), grid, block, 0, s, a, (int)n_tiles, (int)r_tiles, 1);
+        return hipGetLastError();
+    }
+    F8Args p = a;  // partial sums: [shares][R][N]
+    p.y = a.part; p.ldy = a.N;
+    hipLaunchKernelGGL((f8_tile_k<float, F16, TN, TR, PN, PR>), grid, block, 0, s, p, (int)n_tiles, (int)r_tiles, shares);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    const int64_t items = (int64_t)a.R * ((a.N + 3) / 4);
+    hipLaunchKernelGGL((f8_sum_k<OT>), dim3((unsigned)((items + 255) / 256)), dim3(256), 0, s, a.part, shares, a.R, a.N,
+                       reinterpret_cast<OT *>(a.y), a.ldy);
     return hipGetLastError();
+}
+
+// Shares of K for a grid of `tiles` tiles that should be `wanted` workgroups: at most eight, eight blocks of k each, and the
+// partial sums have to fit the scratch.
+static int pick_shares(const F8Args &a, int64_t tiles, int64_t wanted) {
+    const int64_t slab = (int64_t)a.R * a.N * 4;
+    const int64_t fit = a.part == nullptr ? 1 : a.part_bytes / slab;
+    return (int)std::max<int64_t>(1, std::min({wanted / tiles, (int64_t)8, (int64_t)a.KB / 8, fit}));
 }
 
 template <typename OT>
 static hipError_t launch_gemm_f8_t(const F8Args &a, hipStream_t s) {
     if (a.R <= 16) return launch_stream<OT, 1, 1, 8, 1, X_F8>(a, s);
-    if (a.R <= 32) return launch_stream<OT, 1, 2, 8, 1, X_F8>(a, s);
-    auto tiles = [&](int64_t t) { return (a.N + t - 1) / t * ((a.R + t - 1) / t); };
-    if (sizeof(OT) == 4) return tiles(128) >= 256 ? launch_tile<OT, true, 128, 128, 2, 2>(a, s) : launch_tile<OT, true, 64, 64, 2, 2>(a, s);
-    if (tiles(256) >= 256) return launch_tile<OT, false, 256, 256, 2, 4>(a, s);
-    return tiles(128) >= 256 ? launch_tile<OT, false, 128, 128, 2, 2>(a, s) : launch_tile<OT, false, 64, 64, 2, 2>(a, s);
+    if (a.R <= 32 && a.N <= 8192) return launch_stream<OT, 1, 2, 8, 1, X_F8>(a, s);
+    auto tiles = [&](int64_t tn, int64_t tr) { return (a.N + tn - 1) / tn * ((a.R + tr - 1) / tr); };
+    // A tile's time is its steps times a latency that the workgroups sharing a compute unit hide, so a product with few
+    // tiles takes smaller ones and shares K out.
+    constexpr bool F16 = sizeof(OT) == 4;
+    if constexpr (F16) {
+        const int64_t t = tiles(128, 128);
+        if (t >= 128) return launch_tile<OT, true, 128, 128, 2, 2>(a, pick_shares(a, t, 384), s);
+    } else {
+        if (tiles(256, 256) >= 192) return launch_tile<OT, false, 256, 256, 2, 4>(a, 1, s);
+        if (tiles(128, 64) >= 384) return launch_tile<OT, false, 128, 64, 4, 1>(a, 1, s);
+    }
+    return launch_tile<OT, F16, 64, 64, 2, 2>(a, pick_shares(a, tiles(64, 64), 768), s);
 }
 
 hipError_t launch_gemm_f8(const F8Args &a, hipStream_t s) {

@@ -192,6 +192,8 @@ struct AcceptArgs {
     int32_t *A_dev, *y_dev;     // [B] device copies
 };
 
+constexpr int F8_K_MAX = 1 << 22;  // longest row: a tile of 256 rows spans less than 2^31 bytes, and row offsets are 24-bit products
+
 // e4m3 product with block scales (f8.hip): y [R][N] = x [R][K] . w [N][K]^T
 struct F8Args {
     const uint8_t *w;     // e4m3 [N][K]
@@ -203,6 +205,8 @@ struct F8Args {
     void *y;              // y_dtype, row stride ldy
     int64_t ldy;
     int32_t y_dtype, N, K, KB, R;  // KB = ceil(K / 128)
+    float *part;          // scratch for partial sums, part_bytes of it
+    int64_t part_bytes;
 };
 
 // Norm and rotation of query and key heads (headnorm.hip); strides in elements.
