@@ -490,75 +490,80 @@ def k_accept_static(p_logits, q_logits, drafted, temperature: float, seed: int, 
 
 
 # ---- operators of an 8-bit checkpoint with normed heads (include/spec_ops.h) ------------------------------------------
-_KINDS = None
+# These calls take a few microseconds on the GPU, so the checks are written for speed: one pass over the tensors' attributes.
+_KINDS: Dict = {}   # element types of torch -> as the library names them
+_F32T = _I32T = _current_device = None
 
 
-def _kinds() -> Dict:
-    """Element types of torch -> as the library names them."""
-    global _KINDS
-    if _KINDS is None:
-        import torch
-        _KINDS = {torch.float32: SPEC_F32, torch.bfloat16: SPEC_BF16, torch.float8_e4m3fn: SPEC_F8, torch.uint8: SPEC_F8}
-    return _KINDS
+def _setup():
+    global _F32T, _I32T, _current_device
+    import torch
+    _F32T, _I32T, _current_device = torch.float32, torch.int32, torch.cuda.current_device
+    _KINDS.update({torch.float32: SPEC_F32, torch.bfloat16: SPEC_BF16, torch.float8_e4m3fn: SPEC_F8, torch.uint8: SPEC_F8})
 
 
-def _kind(t) -> int:
-    k = _kinds().get(t.dtype)
+def _kind(t, name: str) -> int:
+    k = _KINDS.get(t.dtype)
     if k is None:
-        raise ValueError(f"unsupported element type {t.dtype}")
+        raise ValueError(f"{name}: unsupported element type {t.dtype}")
     return k
 
 
-def _flat(t, name: str, shape, kind: int) -> int:
-    """Address of a contiguous tensor of this shape and element type."""
-    if t.shape != shape or _kinds().get(t.dtype) != kind or not t.is_contiguous():
-        raise ValueError(f"{name} must be a contiguous {tuple(shape)} tensor, not {tuple(t.shape)} of {t.dtype}")
-    return t.data_ptr()
+def _need(t, name: str, what: str):
+    raise ValueError(f"{name} must be {what}, not {tuple(t.shape)} of {t.dtype} with strides {t.stride()} on {t.device}")
 
 
-def _i32(t, name: str, shape) -> int:
-    if t.shape != shape or str(t.dtype) != "torch.int32" or not t.is_contiguous():
-        raise ValueError(f"{name} must be a contiguous int32 {tuple(shape)} tensor, not {tuple(t.shape)} of {t.dtype}")
-    return t.data_ptr()
+def _on(dev: int, t):
+    """The library takes the address as one on the current device."""
+    if dev < 0 or dev != _current_device():
+        raise ValueError(f"operands must be tensors on the current GPU, not on {t.device}")
 
 
-def _here(*tensors):
-    """The pointers belong to the current device."""
-    import torch
-    dev = tensors[0].get_device()
-    if dev < 0 or any(t.get_device() != dev for t in tensors) or torch.cuda.current_device() != dev:
-        raise ValueError("operands must be tensors on the current GPU")
+def _elsewhere(*tensors):
+    raise ValueError(f"operands on different devices: {[str(t.device) for t in tensors]}")
 
 
 def _rows(t, name: str) -> int:
     """Row stride of a [R][n] tensor whose rows are contiguous."""
-    if t.dim() != 2 or (t.stride(1) != 1 and t.shape[1] > 1):
-        raise ValueError(f"{name} must be two-dimensional with contiguous rows")
-    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+    stride = t.stride()
+    if len(stride) != 2 or (stride[1] != 1 and t.shape[1] > 1):
+        _need(t, name, "two-dimensional with contiguous rows")
+    return stride[0] if t.shape[0] > 1 else t.shape[1]
 
 
-def _ops_chk(rc: int, where: str):
-    if rc != 0:
-        raise SpecError(rc, where, load().spec_last_error(None).decode())
+def _refused(rc: int, where: str):
+    raise SpecError(rc, where, load().spec_last_error(None).decode())
 
 
 def k_quant_f8(x, q, scale, stream: int = 0):
     """Rows of x (fp32 or bf16 [R][K], any row stride) to e4m3: q [R][K] (float8_e4m3fn or uint8) and scale fp32
     [ceil(K / 128)][R]."""
+    if not _KINDS:
+        _setup()
     ldx = _rows(x, "x")
     R, K = x.shape
-    qp, sp = _flat(q, "q", (R, K), SPEC_F8), _flat(scale, "scale", ((K + 127) // 128, R), SPEC_F32)
-    _here(x, q, scale)
-    _ops_chk(load().spec_k_quant_f8(x.data_ptr(), _kind(x), ldx, R, K, qp, sp, stream), "spec_k_quant_f8")
+    if q.shape != x.shape or _KINDS.get(q.dtype) != SPEC_F8 or not q.is_contiguous():
+        _need(q, "q", f"a contiguous e4m3 tensor of {R} x {K}")
+    if scale.shape != ((K + 127) // 128, R) or scale.dtype is not _F32T or not scale.is_contiguous():
+        _need(scale, "scale", f"a contiguous fp32 tensor of {(K + 127) // 128} x {R}")
+    dev = x.get_device()
+    if q.get_device() != dev or scale.get_device() != dev:
+        _elsewhere(x, q, scale)
+    _on(dev, x)
+    rc = load().spec_k_quant_f8(x.data_ptr(), _kind(x, "x"), ldx, R, K, q.data_ptr(), scale.data_ptr(), stream)
+    if rc != 0:
+        _refused(rc, "spec_k_quant_f8")
 
 
 def k_gemm_f8_workspace(K: int, R: int, x_dtype) -> int:
     """Bytes of workspace k_gemm_f8 needs for R rows of K elements of this torch type."""
-    if x_dtype not in _kinds():
+    if not _KINDS:
+        _setup()
+    if x_dtype not in _KINDS:
         raise ValueError(f"unsupported element type {x_dtype}")
-    n = load().spec_k_gemm_f8_workspace(K, R, _kinds()[x_dtype])
+    n = load().spec_k_gemm_f8_workspace(K, R, _KINDS[x_dtype])
     if n < 0:
-        raise SpecError(int(n), "spec_k_gemm_f8_workspace", load().spec_last_error(None).decode())
+        _refused(int(n), "spec_k_gemm_f8_workspace")
     return int(n)
 
 
@@ -566,48 +571,77 @@ def k_gemm_f8(w, w_scale, x, y, x_scale=None, workspace=None, stream: int = 0):
     """y [R][N] (fp32 or bf16, any row stride) = x . w^T with w e4m3 [N][K] and w_scale fp32 [ceil(N / 128)][ceil(K / 128)].
     x: e4m3 [R][K] with its x_scale as k_quant_f8 leaves them, or fp32 / bf16 rows, which the call quantises in
     `workspace` (a GPU tensor of at least k_gemm_f8_workspace() bytes; more, up to 32 MiB, lets K be shared out)."""
+    if not _KINDS:
+        _setup()
     N, K = w.shape
     ldx, ldy = _rows(x, "x"), _rows(y, "y")
     R, KB = x.shape[0], (K + 127) // 128
-    if x.shape[1] != K or y.shape != (R, N):
-        raise ValueError(f"x must be [R][{K}] and y [R][{N}], not {tuple(x.shape)} and {tuple(y.shape)}")
-    wp, wsp = _flat(w, "w", (N, K), SPEC_F8), _flat(w_scale, "w_scale", ((N + 127) // 128, KB), SPEC_F32)
-    xp = x.data_ptr()
-    _here(w, w_scale, x, y)
-    xsp = workp = None
+    if x.shape[1] != K:
+        _need(x, "x", f"of {K} columns")
+    if y.shape != (R, N):
+        _need(y, "y", f"of {R} x {N}")
+    if _KINDS.get(w.dtype) != SPEC_F8 or not w.is_contiguous():
+        _need(w, "w", "a contiguous e4m3 matrix")
+    if w_scale.shape != ((N + 127) // 128, KB) or w_scale.dtype is not _F32T or not w_scale.is_contiguous():
+        _need(w_scale, "w_scale", f"a contiguous fp32 tensor of {(N + 127) // 128} x {KB}")
+    dev = x.get_device()
+    if w.get_device() != dev or w_scale.get_device() != dev or y.get_device() != dev:
+        _elsewhere(w, w_scale, x, y)
+    _on(dev, x)
+    scales = work = None
     work_bytes = 0
     if x_scale is not None:
-        xp, xsp = _flat(x, "x", (R, K), SPEC_F8), _flat(x_scale, "x_scale", (KB, R), SPEC_F32)
-        _here(x, x_scale)
+        if _KINDS.get(x.dtype) != SPEC_F8 or not x.is_contiguous():
+            _need(x, "x", "a contiguous e4m3 matrix where x_scale is given")
+        if x_scale.shape != (KB, R) or x_scale.dtype is not _F32T or not x_scale.is_contiguous():
+            _need(x_scale, "x_scale", f"a contiguous fp32 tensor of {KB} x {R}")
+        if x_scale.get_device() != dev:
+            _elsewhere(x, x_scale)
+        scales, ldx = x_scale.data_ptr(), K
     if workspace is not None:
-        if not workspace.is_contiguous():
-            raise ValueError("workspace must be contiguous")
-        _here(x, workspace)
-        workp, work_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
-    _ops_chk(load().spec_k_gemm_f8(wp, wsp, N, K, xp, _kind(x), ldx, xsp, R, y.data_ptr(), _kind(y), ldy, workp, work_bytes,
-                                   stream), "spec_k_gemm_f8")
+        if workspace.get_device() != dev or not workspace.is_contiguous():
+            _need(workspace, "workspace", "contiguous, on the device of the operands")
+        work, work_bytes = workspace.data_ptr(), workspace.nbytes
+    rc = load().spec_k_gemm_f8(w.data_ptr(), w_scale.data_ptr(), N, K, x.data_ptr(), _kind(x, "x"), ldx, scales, R, y.data_ptr(),
+                               _kind(y, "y"), ldy, work, work_bytes, stream)
+    if rc != 0:
+        _refused(rc, "spec_k_gemm_f8")
 
 
-def _heads(t, name: str, R: int, hd: int) -> int:
-    """Row stride of a [R][heads][hd] tensor whose rows hold their heads one after the other."""
+def _heads(t, name: str, R: int, hd: int):
+    """Row stride and heads of a [R][heads][hd] tensor whose rows hold their heads one after the other."""
     shape, stride = t.shape, t.stride()
     if len(shape) != 3 or shape[0] != R or shape[2] != hd or (stride[1] != hd and shape[1] > 1) or (stride[2] != 1 and hd > 1):
-        raise ValueError(f"{name} must be [{R}][heads][{hd}] with the heads of a row one after the other")
-    return stride[0] if R > 1 else shape[1] * hd
+        _need(t, name, f"[{R}][heads][{hd}] with the heads of a row one after the other")
+    return (stride[0] if R > 1 else shape[1] * hd), shape[1]
 
 
 def k_qk_norm_rope(q, k, q_norm, k_norm, cos, sin, pos, q_out, k_out, eps: float = 1e-5, stream: int = 0):
     """RMS norm (weights q_norm, k_norm fp32 [hd]) and rotation of the heads of q [R][nq][hd] and k [R][nkv][hd] (fp32 or
     bf16, views into fused rows included) into q_out, k_out (fp32 or bf16, may be the inputs).  cos, sin: fp32
     [n_pos][hd / 2]; pos: int32 [R], rows with a position outside the tables are left as they were."""
-    R, nq, hd = q.shape
-    ldq, ldk, ldqo, ldko = _heads(q, "q", R, hd), _heads(k, "k", R, hd), _heads(q_out, "q_out", R, hd), _heads(k_out, "k_out", R, hd)
-    if q.dtype != k.dtype or q_out.dtype != k_out.dtype or q_out.shape != q.shape or k_out.shape != k.shape:
+    if not _KINDS:
+        _setup()
+    R, hd = q.shape[0], q.shape[-1]
+    ldq, nq = _heads(q, "q", R, hd)
+    ldk, nkv = _heads(k, "k", R, hd)
+    ldqo, nqo = _heads(q_out, "q_out", R, hd)
+    ldko, nko = _heads(k_out, "k_out", R, hd)
+    if q.dtype is not k.dtype or q_out.dtype is not k_out.dtype or nqo != nq or nko != nkv:
         raise ValueError("q and k must have one type, and the outputs theirs and the inputs' shapes")
-    n_pos, table = cos.shape[0], (cos.shape[0], hd // 2)
-    gq, gk = _flat(q_norm, "q_norm", (hd,), SPEC_F32), _flat(k_norm, "k_norm", (hd,), SPEC_F32)
-    cp, sp, pp = _flat(cos, "cos", table, SPEC_F32), _flat(sin, "sin", table, SPEC_F32), _i32(pos, "pos", (R,))
-    _here(q, k, q_norm, k_norm, cos, sin, pos, q_out, k_out)
-    _ops_chk(load().spec_k_qk_norm_rope(q.data_ptr(), ldq, nq, k.data_ptr(), ldk, k.shape[1], _kind(q), hd, R, gq, gk, eps, cp,
-                                        sp, n_pos, pp, q_out.data_ptr(), ldqo, k_out.data_ptr(), ldko, _kind(q_out), stream),
-             "spec_k_qk_norm_rope")
+    n_pos = cos.shape[0]
+    for t, name, n in ((q_norm, "q_norm", hd), (k_norm, "k_norm", hd), (cos, "cos", n_pos * (hd // 2)), (sin, "sin", n_pos * (hd // 2))):
+        if t.dtype is not _F32T or t.numel() != n or not t.is_contiguous():
+            _need(t, name, f"a contiguous fp32 tensor of {n} elements")
+    if pos.dtype is not _I32T or pos.numel() != R or not pos.is_contiguous():
+        _need(pos, "pos", f"a contiguous int32 tensor of {R} elements")
+    dev = q.get_device()
+    if not (k.get_device() == q_norm.get_device() == k_norm.get_device() == cos.get_device() == sin.get_device() ==
+            pos.get_device() == q_out.get_device() == k_out.get_device() == dev):
+        _elsewhere(q, k, q_norm, k_norm, cos, sin, pos, q_out, k_out)
+    _on(dev, q)
+    rc = load().spec_k_qk_norm_rope(q.data_ptr(), ldq, nq, k.data_ptr(), ldk, nkv, _kind(q, "q"), hd, R, q_norm.data_ptr(),
+                                    k_norm.data_ptr(), eps, cos.data_ptr(), sin.data_ptr(), n_pos, pos.data_ptr(),
+                                    q_out.data_ptr(), ldqo, k_out.data_ptr(), ldko, _kind(q_out, "q_out"), stream)
+    if rc != 0:
+        _refused(rc, "spec_k_qk_norm_rope")

@@ -1720,7 +1720,7 @@ int spec_k_gemm_f8(const void *w, const float *w_scale, int32_t N, int32_t K, co
     a.w = reinterpret_cast<const uint8_t *>(w); a.ws = w_scale; a.N = N; a.K = K; a.KB = (K + 127) / 128; a.R = R;
     a.y = y; a.y_dtype = y_dtype; a.ldy = ldy;
     a.x = x; a.xs = x_scale; a.ldx = ldx; a.x_type = f8 ? 0 : (x_dtype == SPEC_F32 ? 1 : 2);
-    if (!f8) {
+    if (!f8 && !gemm_f8_takes_wide(a)) {
         uint8_t *q = reinterpret_cast<uint8_t *>(workspace);
         float *scale = reinterpret_cast<float *>(q + (int64_t)128 * R * a.KB);
         const int rc = launched(launch_quant_f8(x, x_dtype, ldx, R, K, q, scale, st), "gemm_f8: launch failed");

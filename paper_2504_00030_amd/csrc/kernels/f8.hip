@@ -574,6 +574,18 @@ static hipError_t launch_tile(const F8Args &a, int shares, hipStream_t s) {
     return hipGetLastError();
 }
 
+// ---- which kernel runs ---------------------------------------------------------------------------------------------
+// Times below: rows as fp32 or bf16 with fresh weights from HBM for every call, in microseconds.
+
+// Whether the product quantises fp32 / bf16 rows itself, in every workgroup anew, instead of by a launch of the quantiser
+// in front: for a few rows of a small matrix (1 x 2048 x 2048: 4.9 against 5.6 with both launches in a graph, 4 x 4096 x
+// 4096: 8.1 against 9.1; but 1 x 6144 x 4096: 12.0 against 10.4, 1 x 4096 x 14336: 20.0 against 14.6).
+bool gemm_f8_takes_wide(const F8Args &a) {
+    const int64_t size = a.x_type == X_F32 ? 4 : 2;
+    return a.R <= 8 && a.K <= 4096 && (int64_t)a.N * a.K <= 4096 * 4096 && reinterpret_cast<uintptr_t>(a.x) % 16 == 0 &&
+           a.ldx * size % 16 == 0;
+}
+
 // Shares of K for a grid of `tiles` tiles that should be `wanted` workgroups: at most eight, eight blocks of k each, and the
 // partial sums have to fit the scratch.
 static int pick_shares(const F8Args &a, int64_t tiles, int64_t wanted) {
@@ -582,18 +594,34 @@ static int pick_shares(const F8Args &a, int64_t tiles, int64_t wanted) {
     return (int)std::max<int64_t>(1, std::min({wanted / tiles, (int64_t)8, (int64_t)a.KB / 8, fit}));
 }
 
+// Up to 16 rows: the stream, sixteen waves once each has two blocks of k (1 x 28672 x 4096: 23.8 against 25.6 with eight;
+// 1 x 128256 x 2048: 61 against 42).
+template <typename OT, int XIN>
+static hipError_t launch_few(const F8Args &a, hipStream_t s) {
+    return a.KB >= 32 ? launch_stream<OT, 1, 1, 16, 1, XIN>(a, s) : launch_stream<OT, 1, 1, 8, 1, XIN>(a, s);
+}
+
 template <typename OT>
 static hipError_t launch_gemm_f8_t(const F8Args &a, hipStream_t s) {
-    if (a.R <= 16) return launch_stream<OT, 1, 1, 8, 1, X_F8>(a, s);
-    if (a.R <= 32 && a.N <= 8192) return launch_stream<OT, 1, 2, 8, 1, X_F8>(a, s);
+    if (a.x_type == X_F32) return launch_few<OT, X_F32>(a, s);
+    if (a.x_type == X_BF16) return launch_few<OT, X_BF16>(a, s);
+    if (a.R <= 16) return launch_few<OT, X_F8>(a, s);
+    if (a.R <= 32) {
+        // wider column tiles read x less often, and need more columns to give every compute unit one (24 x 4096 x 4096: 9.6 / 11.0 / 15.8
+        // with 16 / 32 / 64 columns, 32 x 6144 x 4096: 16.3 / 12.5 / 17.1, 32 x 28672 x 4096: 49.7 / 43.5 / 35.9)
+        if (a.N > 8192) return launch_stream<OT, 4, 2, 4, 1, X_F8>(a, s);
+        if (a.N > 4096) return launch_stream<OT, 2, 2, 4, 2, X_F8>(a, s);
+        return launch_stream<OT, 1, 2, 8, 1, X_F8>(a, s);
+    }
     auto tiles = [&](int64_t tn, int64_t tr) { return (a.N + tn - 1) / tn * ((a.R + tr - 1) / tr); };
     // A tile's time is its steps times a latency that the workgroups sharing a compute unit hide, so a product with few
-    // tiles takes smaller ones and shares K out.
+    // tiles takes smaller ones and shares K out (137 x 4096 x 11008: 64 with one share of 64 x 64 tiles, 29 with four).
     constexpr bool F16 = sizeof(OT) == 4;
     if constexpr (F16) {
-        const int64_t t = tiles(128, 128);
+        const int64_t t = tiles(128, 128);  // 512 x 6144 x 4096: 45 with two shares, 48 with 64 x 64 tiles
         if (t >= 128) return launch_tile<OT, true, 128, 128, 2, 2>(a, pick_shares(a, t, 384), s);
     } else {
+        // 512 x 28672 x 4096: 77 / 92 / 111 / 126 with 256 x 256 / 128 x 128 / 128 x 64 / 64 x 64; 1024 x 6144 x 4096: 65 / 46 / 45 / 60
         if (tiles(256, 256) >= 192) return launch_tile<OT, false, 256, 256, 2, 4>(a, 1, s);
         if (tiles(128, 64) >= 384) return launch_tile<OT, false, 128, 64, 4, 1>(a, 1, s);
     }

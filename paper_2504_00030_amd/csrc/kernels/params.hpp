@@ -266,6 +266,7 @@ hipError_t launch_copy(const void *src, void *dst, int64_t bytes, hipStream_t s)
 hipError_t launch_cast_to_bf16(const float *src, uint16_t *dst, int64_t lo_off, int64_t n, hipStream_t s);
 hipError_t launch_cast_to_f32(const void *src, int dtype, float *dst, int64_t n, hipStream_t s);
 hipError_t launch_quant_f8(const void *x, int dtype, int64_t ldx, int R, int K, void *q, float *scale, hipStream_t s);
+bool gemm_f8_takes_wide(const F8Args &a);  // whether the product quantises fp32 / bf16 rows itself
 hipError_t launch_gemm_f8(const F8Args &a, hipStream_t s);
 hipError_t launch_head_norm(const HeadNormArgs &a, hipStream_t s);
 
