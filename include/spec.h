@@ -24,7 +24,8 @@
  *  - Models are Llama-style decoders: RMSNorm, rotary embedding with
  *    rotate-half pairing (element j pairs with j + head_dim/2, angle
  *    pos * theta^(-2j/head_dim)), grouped-query attention (query head h reads
- *    kv head h / (n_q_heads / n_kv_heads)), SwiGLU MLP, no biases.
+ *    kv head h / (n_q_heads / n_kv_heads)), SwiGLU MLP, no biases; optionally
+ *    with normed query and key heads (spec_set_qk_norm()).
  */
 #ifndef SPEC_H
 #define SPEC_H
@@ -157,6 +158,13 @@ int spec_accept(spec_ctx *ctx, int32_t *n_accepted, int32_t *next_token, int32_t
  * (the last value repeats beyond n).  Only used with SPEC_ACCEPT_FORCED.  In forced mode the
  * confidence seen by early stopping is the synthetic clamp(alpha[g] + (0.5 - Philox(g, 0, FORCED, b)) / 2, 0, 1). */
 int spec_set_forced_alpha(spec_ctx *ctx, const float *alpha, int32_t n);
+
+/* Normed heads: from here on the model's (0 draft, 1 target) query and key heads are RMS-normed with rms_eps before the
+ * rotation, h <- h / sqrt(mean(h^2) + eps) * norm, as in spec_k_qk_norm_rope() (spec_ops.h).  q_norm, k_norm: host arrays of
+ * n_layers device pointers to [head_dim] weights, element type as the model's other norm weights; copied by the call.
+ * Both NULL: back to the rotation alone.  head_dim up to 512.  The caches then hold nothing: the next call must be
+ * spec_prefill*().  Synchronises. */
+int spec_set_qk_norm(spec_ctx *ctx, int32_t model, const void *const *q_norm, const void *const *k_norm);
 
 /* GammaTune+ threshold: stop drafting when the draft's top probability
  * max softmax(logits / T_eff), T_eff = T > 0 ? T : 1, is below tau.  tau <= 0 disables. */

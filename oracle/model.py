@@ -9,6 +9,8 @@ ones both sides implement independently:
   * RMSNorm: y = x * rsqrt(mean(x^2) + eps) * g
   * RoPE, rotate-half pairing: element j pairs with j + hd/2, angle
     pos * theta**(-2j/hd); no frequency rescaling
+  * models with "q_norm" / "k_norm" weights ([hd] per layer) apply RMSNorm to
+    every query / key head before the rotation
   * attention: softmax(q k^T / sqrt(hd)) v with a causal mask on absolute
     positions; query head h reads kv head h // (n_q / n_kv)
   * MLP: W_down( silu(W_gate m) * (W_up m) ), no biases
@@ -101,7 +103,7 @@ def forward(shape: Shape, W: Dict, tokens, cache: Optional[KVCache] = None) -> n
 
     W keys: tok_embed [V,d], lm_head [V,d], final_norm [d], and per-layer lists
     wq [nq*hd,d], wk, wv [nkv*hd,d], wo [d,nq*hd], w_gate, w_up [ffn,d],
-    w_down [d,ffn], attn_norm [d], ffn_norm [d].
+    w_down [d,ffn], attn_norm [d], ffn_norm [d], optionally q_norm, k_norm [hd].
     """
     tokens = np.asarray(tokens, dtype=np.int64).reshape(-1)
     n = tokens.shape[0]
@@ -118,6 +120,9 @@ def forward(shape: Shape, W: Dict, tokens, cache: Optional[KVCache] = None) -> n
         q = (a @ as_f64(W["wq"][l]).T).reshape(n, nq, hd)
         k = (a @ as_f64(W["wk"][l]).T).reshape(n, nkv, hd)
         v = (a @ as_f64(W["wv"][l]).T).reshape(n, nkv, hd)
+        if "q_norm" in W:
+            q = rmsnorm(q, as_f64(W["q_norm"][l]), shape.rms_eps)
+            k = rmsnorm(k, as_f64(W["k_norm"][l]), shape.rms_eps)
         q = rope(q, pos, shape.rope_theta)
         k = rope(k, pos, shape.rope_theta)
         if shape.kv_bf16:

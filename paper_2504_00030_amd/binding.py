@@ -25,7 +25,7 @@ GT_EXPAND_A, GT_LITERAL, GT_SHORT_TERM = 0, 1, 2
 # every symbol the headers in include/ declare
 EXPORTS = [
     "spec_init", "spec_prefill", "spec_prefill_ragged", "spec_debug_set_step", "spec_draft", "spec_draft_batch", "spec_verify", "spec_accept",
-    "spec_set_forced_alpha", "spec_set_early_stop", "spec_generate", "spec_read_tokens", "spec_debug_logits",
+    "spec_set_forced_alpha", "spec_set_early_stop", "spec_set_qk_norm", "spec_generate", "spec_read_tokens", "spec_debug_logits",
     "spec_debug_drafted", "spec_debug_read", "spec_debug_fill_kv", "spec_debug_write_kv", "spec_debug_set_block_table", "spec_device_bytes", "spec_profile_kernel", "spec_profile_read", "spec_profile_read_class", "spec_debug_verify_rows", "spec_destroy",
     "spec_strerror", "spec_last_error", "spec_k_gemv", "spec_k_gemv_tiled", "spec_k_gemm_tiled", "spec_k_retile_q8", "spec_k_gemv_tiled_q8", "spec_k_gemm_tiled_q8", "spec_k_retile", "spec_k_copy", "spec_k_philox", "spec_k_accept", "spec_k_accept_static",
     "spec_k_quant_f8", "spec_k_gemm_f8", "spec_k_gemm_f8_workspace", "spec_k_qk_norm_rope",
@@ -97,6 +97,7 @@ def load() -> C.CDLL:
     lib.spec_accept.argtypes = [C.c_void_p, i32p, i32p, i32p]
     lib.spec_set_forced_alpha.argtypes = [C.c_void_p, f32p, C.c_int32]
     lib.spec_set_early_stop.argtypes = [C.c_void_p, C.c_float]
+    lib.spec_set_qk_norm.argtypes = [C.c_void_p, C.c_int32, _PP, _PP]
     lib.spec_read_tokens.argtypes = [C.c_void_p, C.c_int32, i32p, C.c_int32, i32p]
     lib.spec_debug_logits.argtypes = [C.c_void_p, C.c_int32, f32p, C.c_int64, i32p]
     lib.spec_debug_drafted.argtypes = [C.c_void_p, C.c_int32, i32p, C.c_int32, i32p]
@@ -230,6 +231,10 @@ class SpecEngine:
         rc = self._lib.spec_init(C.byref(ts), C.byref(tw), C.byref(ds), C.byref(dw), C.byref(cfg), C.byref(self._ctx))
         if rc != 0:
             raise SpecError(rc, "spec_init", self._lib.spec_last_error(None).decode())
+        self._shapes = (draft_shape, target_shape)
+        for model, W in enumerate((draft_w, target_w)):  # models with normed heads
+            if "q_norm" in W or "k_norm" in W:
+                self.set_qk_norm(model, W.get("q_norm"), W.get("k_norm"))
 
     def _chk(self, rc: int, where: str):
         if rc != 0:
@@ -290,6 +295,20 @@ class SpecEngine:
 
     def set_early_stop(self, tau: float):
         self._chk(self._lib.spec_set_early_stop(self._ctx, float(tau)), "spec_set_early_stop")
+
+    def set_qk_norm(self, model: int, q_norm, k_norm):
+        """q_norm, k_norm: one [head_dim] GPU tensor per layer of the model (0 draft, 1 target), of the type of its norm
+        weights; None, None: no head norms.  The next call must be a prefill."""
+        def arr(ts):
+            if ts is None:
+                return None
+            ms = self._shapes[model]
+            kind = "torch.float32" if ms.dtype == "fp32" else "torch.bfloat16"
+            if len(ts) != ms.n_layers or any(tuple(t.shape) != (ms.head_dim,) or str(t.dtype) != kind or not t.is_cuda or
+                                             not t.is_contiguous() for t in ts):
+                raise ValueError(f"head norms must be {ms.n_layers} contiguous GPU tensors of {ms.head_dim} x {kind}")
+            return (C.c_void_p * len(ts))(*[t.data_ptr() for t in ts])
+        self._chk(self._lib.spec_set_qk_norm(self._ctx, model, arr(q_norm), arr(k_norm)), "spec_set_qk_norm")
 
     def set_block_table(self, table: np.ndarray):
         t = np.ascontiguousarray(table, dtype=np.int32)

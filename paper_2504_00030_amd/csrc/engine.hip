@@ -19,6 +19,7 @@
 #include <chrono>
 #include <map>
 #include <mutex>
+#include <new>
 #include <string>
 #include <vector>
 
@@ -39,6 +40,9 @@ struct ModelRT {
     std::vector<const void *> wq, wk, wv, wo, wg, wu, wd;
     std::vector<float *> attn_norm, ffn_norm;
     float *final_norm = nullptr;
+    std::vector<float *> q_norm, k_norm;  // per-head norm weights (empty: the heads are rotated only)
+    std::vector<float *> norm_copies;     // their memory, two per layer once allocated
+    float *qkv = nullptr;                 // plain result of the QKV projection in front of the head norms, [Rmax][qd + 2 kvd]
     const void *embed = nullptr, *lm_head = nullptr;
     // re-tiled bf16 copies for the matrix-core path (empty when unused)
     std::vector<void *> t_qkv, t_wo, t_gu, t_wd;
@@ -547,7 +551,7 @@ int forward(spec_ctx *c, ModelRT &m, const RowPlan &plan, const LogitsPlan &lp, 
     const int kvd = s.n_kv_heads * s.head_dim;
     const bool tiled = m.mfma_ok;
     for (int l = 0; l < s.n_layers; ++l) {
-        {   // fused QKV projection + RoPE + KV write
+        if (m.q_norm.empty()) {   // fused QKV projection + RoPE + KV write
             GemvArgs a = base(d, m.xg, m.xgb, xgb_lo);
             a.w0 = m.wq[l]; a.w1 = m.wk[l]; a.w2 = m.wv[l];
             a.n0 = qd; a.n1 = a.n2 = kvd;
@@ -557,6 +561,31 @@ int forward(spec_ctx *c, ModelRT &m, const RowPlan &plan, const LogitsPlan &lp, 
             a.kv = kv_of(c, m, l); a.kv_dtype = s.dtype;
             a.wscale = tiled ? m.sc_qkv[l] : nullptr;
             TRY(launch_proj(c, m, a, EPI_QKV, tiled ? m.t_qkv[l] : nullptr, qd + 2 * kvd, nullptr, nullptr));
+        } else {   // QKV projection, then norm + RoPE of the heads and KV write
+            const size_t Rq = (size_t)m.Rmax * qd, Rk = (size_t)m.Rmax * kvd;
+            auto plain = [&](const void *w, const void *t, int N, float *y) {
+                GemvArgs a = base(d, m.xg, m.xgb, xgb_lo);
+                a.w0 = w; a.n0 = N;
+                a.ssq_in = m.ssq; a.ssq_in_slots = slots;
+                a.y = y;
+                a.wscale = tiled ? m.sc_qkv[l] : nullptr;
+                return launch_proj(c, m, a, EPI_PLAIN, t, N, nullptr, nullptr, 1);
+            };
+            if (tiled) {
+                TRY(plain(nullptr, m.t_qkv[l], qd + 2 * kvd, m.qkv));
+            } else {
+                TRY(plain(m.wq[l], nullptr, qd, m.qkv));
+                TRY(plain(m.wk[l], nullptr, kvd, m.qkv + Rq));
+                TRY(plain(m.wv[l], nullptr, kvd, m.qkv + Rq + Rk));
+            }
+            QkvNormArgs n{};
+            n.q_in = m.qkv; n.k_in = m.qkv + Rq; n.v_in = m.qkv + Rq + Rk; n.packed = tiled;
+            n.ldq = tiled ? qd + 2 * kvd : qd; n.ldkv = kvd;
+            n.R = R; n.nq = s.n_q_heads; n.nkv = s.n_kv_heads; n.hd = s.head_dim;
+            n.q_norm = m.q_norm[l]; n.k_norm = m.k_norm[l]; n.eps = s.rms_eps;
+            n.rope_cos = m.rope_cos; n.rope_sin = m.rope_sin; n.row_pos = m.row_pos; n.row_seq = m.row_seq;
+            n.q = m.q; n.qb = m.qb; n.qb_lo = qb_lo; n.kv = kv_of(c, m, l); n.kv_dtype = s.dtype; n.active = active;
+            HIPCHK(c, launch_qkv_norm(n, st));
         }
         {
             AttnArgs t{};
@@ -1061,6 +1090,52 @@ int spec_set_early_stop(spec_ctx *c, float tau) {
     c->g_draft.clear();
     for (auto &kv : c->g_pass) (void)hipGraphExecDestroy(kv.second);
     c->g_pass.clear();
+    return SPEC_OK;
+}
+
+int spec_set_qk_norm(spec_ctx *c, int32_t model, const void *const *q_norm, const void *const *k_norm) {
+    if (!c) return SPEC_EINVAL;
+    try {
+        if (model != 0 && model != 1) return fail(c, SPEC_EINVAL, "set_qk_norm: model must be 0 (draft) or 1 (target)");
+        if ((q_norm == nullptr) != (k_norm == nullptr)) return fail(c, SPEC_EINVAL, "set_qk_norm: one of the two arrays is null");
+        ModelRT &m = model ? c->tgt : c->drf;
+        const int hd = m.s.head_dim;
+        if (q_norm != nullptr) {
+            if (hd > 512) return fail(c, SPEC_EINVAL, "set_qk_norm: head_dim beyond 512");
+            for (int l = 0; l < m.s.n_layers; ++l)
+                if (!q_norm[l] || !k_norm[l]) return fail(c, SPEC_EINVAL, "set_qk_norm: null layer weight");
+        }
+        HIPCHK(c, hipDeviceSynchronize());  // whatever produced the weights, and this context's own work
+        std::vector<float *> qn, kn;
+        if (q_norm != nullptr) {
+            if (m.qkv == nullptr) TRY(dalloc(c, &m.qkv, (size_t)m.Rmax * (m.s.n_q_heads + 2 * m.s.n_kv_heads) * hd));
+            // the copies of an earlier call serve again
+            while (m.norm_copies.size() < 2 * (size_t)m.s.n_layers) {
+                float *p = nullptr;
+                TRY(dalloc(c, &p, hd));
+                m.norm_copies.push_back(p);
+            }
+            for (int l = 0; l < m.s.n_layers; ++l) {
+                qn.push_back(m.norm_copies[2 * l]);
+                kn.push_back(m.norm_copies[2 * l + 1]);
+                HIPCHK(c, launch_cast_to_f32(q_norm[l], m.s.dtype, qn[l], hd, c->stream));
+                HIPCHK(c, launch_cast_to_f32(k_norm[l], m.s.dtype, kn[l], hd, c->stream));
+            }
+            HIPCHK(c, hipStreamSynchronize(c->stream));
+        }
+        // captured graphs hold the other form of the layers, and the caches hold keys made by it
+        for (auto &kv : c->g_draft) (void)hipGraphExecDestroy(kv.second);
+        for (auto &kv : c->g_verify) (void)hipGraphExecDestroy(kv.second.exec);
+        for (auto &kv : c->g_pass) (void)hipGraphExecDestroy(kv.second);
+        c->g_draft.clear();
+        c->g_verify.clear();
+        c->g_pass.clear();
+        m.q_norm.swap(qn);
+        m.k_norm.swap(kn);
+        c->phase = 0;
+    } catch (const std::bad_alloc &) {
+        return SPEC_ENOMEM;
+    }
     return SPEC_OK;
 }
 

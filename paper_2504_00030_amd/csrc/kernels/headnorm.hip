@@ -6,6 +6,7 @@
 // and the whole sum of squares stay in registers and a head is read and written once.  What bounds the kernel is memory
 // (large calls) or the launch (small ones).
 #include "common.hpp"
+#include "kv.hpp"
 #include "params.hpp"
 
 #include <algorithm>
@@ -51,6 +52,21 @@ __device__ __forceinline__ void store4(T *p, int l, int half, const f4_t v) {
     }
 }
 
+// One head: its norm and rotation; u, v hold this lane's elements of the two halves.
+template <int LPH, bool VEC>
+__device__ __forceinline__ void norm_rotate(f4_t &u, f4_t &v, const float *g, float eps, int hd, const f4_t c, const f4_t s, int l) {
+    float ss = 0.f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) ss += u[e] * u[e] + v[e] * v[e];
+#pragma unroll
+    for (int m = LPH / 2; m >= 1; m >>= 1) ss += __shfl_xor(ss, m, WAVE);
+    const float inv = 1.f / sqrtf(ss / (float)hd + eps);
+    const f4_t x = u * inv * load4<float, LPH, VEC>(g, l, hd >> 1);
+    const f4_t y = v * inv * load4<float, LPH, VEC>(g + (hd >> 1), l, hd >> 1);
+    u = x * c - y * s;
+    v = y * c + x * s;
+}
+
 }  // namespace
 
 // HB: heads of one row a group of lanes takes, one after the other (their loads are issued together, and the rotation
@@ -86,16 +102,9 @@ __global__ __launch_bounds__(256) void head_norm_k(const HeadNormArgs a) {
         const float *gw = is_q ? a.q_norm : a.k_norm;
         OT *dst = is_q ? reinterpret_cast<OT *>(a.q_out) + (int64_t)r * a.ldqo + (int64_t)hh * a.hd
                        : reinterpret_cast<OT *>(a.k_out) + (int64_t)r * a.ldko + (int64_t)(hh - a.nq) * a.hd;
-        float ss = 0.f;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) ss += u[i][e] * u[i][e] + v[i][e] * v[i][e];
-#pragma unroll
-        for (int m = LPH / 2; m >= 1; m >>= 1) ss += __shfl_xor(ss, m, WAVE);
-        const float inv = 1.f / sqrtf(ss / (float)a.hd + a.eps);
-        const f4_t x = u[i] * inv * load4<float, LPH, VEC>(gw, l, half);
-        const f4_t y = v[i] * inv * load4<float, LPH, VEC>(gw + half, l, half);
-        store4<OT, LPH, VEC>(dst, l, half, x * c - y * s);
-        store4<OT, LPH, VEC>(dst + half, l, half, y * c + x * s);
+        norm_rotate<LPH, VEC>(u[i], v[i], gw, a.eps, a.hd, c, s, l);
+        store4<OT, LPH, VEC>(dst, l, half, u[i]);
+        store4<OT, LPH, VEC>(dst + half, l, half, v[i]);
     }
 }
 
@@ -131,6 +140,69 @@ static hipError_t launch_head_norm_t(const HeadNormArgs &a, hipStream_t s) {
 hipError_t launch_head_norm(const HeadNormArgs &a, hipStream_t s) {
     if (a.dtype == DT_F32) return a.out_dtype == DT_F32 ? launch_head_norm_t<float, float>(a, s) : launch_head_norm_t<float, __bf16>(a, s);
     return a.out_dtype == DT_F32 ? launch_head_norm_t<__bf16, float>(a, s) : launch_head_norm_t<__bf16, __bf16>(a, s);
+}
+
+// The engine's form: the plain result of a layer's QKV projection -> queries (fp32 and two bf16 terms) and the paged
+// cache, what the QKV epilogue writes for models without head norms.  A group of lanes per head, value heads included.
+template <int LPH>
+__global__ __launch_bounds__(256) void qkv_norm_k(const QkvNormArgs a) {
+    if (a.active != nullptr && *a.active == 0) return;
+    constexpr int GPB = 256 / LPH;
+    const int half = a.hd >> 1, nh = a.nq + 2 * a.nkv;
+    const int item = blockIdx.x * GPB + threadIdx.x / LPH, l = threadIdx.x % LPH;
+    const int r = item / nh, hh = item % nh;
+    if (r >= a.R) return;
+    const int j = 4 * l, pos = a.row_pos[r], seq = a.row_seq[r];
+    f4_t u = {0.f, 0.f, 0.f, 0.f}, v = u, c = u, s = u;
+    if (j < half) {
+        if (a.packed) {  // columns of the re-tiled matrix: eight first elements of pairs, then their eight partners
+            const int P = hh * half + j;
+            const float *p = a.q_in + (size_t)r * a.ldq + (P >> 3) * 16 + (P & 7);
+            u = *reinterpret_cast<const f4_t *>(p);
+            v = *reinterpret_cast<const f4_t *>(p + 8);
+        } else {
+            const float *p = hh < a.nq ? a.q_in + (size_t)r * a.ldq + hh * a.hd
+                                       : (hh < a.nq + a.nkv ? a.k_in : a.v_in) + (size_t)r * a.ldkv + (hh - a.nq) % a.nkv * a.hd;
+            u = *reinterpret_cast<const f4_t *>(p + j);
+            v = *reinterpret_cast<const f4_t *>(p + half + j);
+        }
+    }
+    if (hh < a.nq + a.nkv) {
+        c = load4<float, LPH, true>(a.rope_cos + (size_t)pos * half, l, half);
+        s = load4<float, LPH, true>(a.rope_sin + (size_t)pos * half, l, half);
+        norm_rotate<LPH, true>(u, v, hh < a.nq ? a.q_norm : a.k_norm, a.eps, a.hd, c, s, l);
+    }
+    if (j >= half) return;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        if (hh < a.nq) {
+            const size_t o = ((size_t)r * a.nq + hh) * a.hd + j + e;
+            a.q[o] = u[e];
+            a.q[o + half] = v[e];
+            store_split_bf16(a.qb, o, a.qb_lo, u[e]);
+            store_split_bf16(a.qb, o + half, a.qb_lo, v[e]);
+        } else {
+            const bool is_k = hh < a.nq + a.nkv;
+            const int kvh = hh - a.nq - (is_k ? 0 : a.nkv);
+            kv_store(a.kv, a.kv_dtype, is_k, seq, pos, kvh, j + e, u[e]);
+            kv_store(a.kv, a.kv_dtype, is_k, seq, pos, kvh, j + e + half, v[e]);
+        }
+    }
+}
+
+hipError_t launch_qkv_norm(const QkvNormArgs &a, hipStream_t s) {
+    if (a.hd % 8 || a.hd > 512 || (a.packed && a.hd % 16)) return hipErrorInvalidValue;
+    const int need = (a.hd / 2 + 3) / 4, lph = need <= 8 ? 8 : (need <= 16 ? 16 : (need <= 32 ? 32 : 64));
+    const int64_t wgs = ((int64_t)a.R * (a.nq + 2 * a.nkv) + 256 / lph - 1) / (256 / lph);
+    if (wgs * (256 / lph) > 0x7fffffff) return hipErrorInvalidValue;
+    const dim3 grid((unsigned)wgs), block(256);
+    switch (lph) {
+        case 8: hipLaunchKernelGGL((qkv_norm_k<8>), grid, block, 0, s, a); break;
+        case 16: hipLaunchKernelGGL((qkv_norm_k<16>), grid, block, 0, s, a); break;
+        case 32: hipLaunchKernelGGL((qkv_norm_k<32>), grid, block, 0, s, a); break;
+        default: hipLaunchKernelGGL((qkv_norm_k<64>), grid, block, 0, s, a); break;
+    }
+    return hipGetLastError();
 }
 
 }  // namespace sd

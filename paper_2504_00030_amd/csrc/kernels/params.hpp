@@ -224,6 +224,24 @@ struct HeadNormArgs {
     int32_t out_dtype;
 };
 
+// The engine's form of it: the QKV projection's plain result -> queries and paged cache.
+struct QkvNormArgs {
+    // packed: q_in holds all columns in the order of the re-tiled matrix; otherwise q, k and v rows of their own
+    const float *q_in, *k_in, *v_in;
+    int64_t ldq, ldkv;
+    int32_t packed, R, nq, nkv, hd;
+    const float *q_norm, *k_norm;  // [hd]
+    float eps;
+    const float *rope_cos, *rope_sin;
+    const int32_t *row_pos, *row_seq;
+    float *q;
+    uint16_t *qb;
+    int64_t qb_lo;
+    KVCache kv;
+    int32_t kv_dtype;
+    const int32_t *active;
+};
+
 // ---- launchers (defined next to the kernels) -----------------------------------------------------
 hipError_t launch_begin_draft(const State &st, const int32_t *gamma_plan, hipStream_t s);
 hipError_t launch_embed(const EmbedArgs &a, hipStream_t s);
@@ -269,5 +287,6 @@ hipError_t launch_quant_f8(const void *x, int dtype, int64_t ldx, int R, int K, 
 bool gemm_f8_takes_wide(const F8Args &a);  // whether the product quantises fp32 / bf16 rows itself
 hipError_t launch_gemm_f8(const F8Args &a, hipStream_t s);
 hipError_t launch_head_norm(const HeadNormArgs &a, hipStream_t s);
+hipError_t launch_qkv_norm(const QkvNormArgs &a, hipStream_t s);
 
 }  // namespace sd
