@@ -628,11 +628,11 @@ def k_gemm_f8(w, w_scale, x, y, x_scale=None, workspace=None, stream: int = 0):
 
 
 def _heads(t, name: str, R: int, hd: int):
-    """Row stride and heads of a [R][heads][hd] tensor whose rows hold their heads one after the other."""
+    """Row stride of a [R][heads][hd] tensor whose rows hold their heads one after the other."""
     shape, stride = t.shape, t.stride()
     if len(shape) != 3 or shape[0] != R or shape[2] != hd or (stride[1] != hd and shape[1] > 1) or (stride[2] != 1 and hd > 1):
         _need(t, name, f"[{R}][heads][{hd}] with the heads of a row one after the other")
-    return (stride[0] if R > 1 else shape[1] * hd), shape[1]
+    return stride[0] if R > 1 else shape[1] * hd
 
 
 def k_qk_norm_rope(q, k, q_norm, k_norm, cos, sin, pos, q_out, k_out, eps: float = 1e-5, stream: int = 0):
@@ -641,17 +641,22 @@ def k_qk_norm_rope(q, k, q_norm, k_norm, cos, sin, pos, q_out, k_out, eps: float
     [n_pos][hd / 2]; pos: int32 [R], rows with a position outside the tables are left as they were."""
     if not _KINDS:
         _setup()
-    R, hd = q.shape[0], q.shape[-1]
-    ldq, nq = _heads(q, "q", R, hd)
-    ldk, nkv = _heads(k, "k", R, hd)
-    ldqo, nqo = _heads(q_out, "q_out", R, hd)
-    ldko, nko = _heads(k_out, "k_out", R, hd)
-    if q.dtype is not k.dtype or q_out.dtype is not k_out.dtype or nqo != nq or nko != nkv:
+    qs, ks = q.shape, k.shape
+    R, hd = qs[0], qs[-1]
+    if q.dtype is not k.dtype or q_out.dtype is not k_out.dtype or q_out.shape != qs or k_out.shape != ks:
         raise ValueError("q and k must have one type, and the outputs theirs and the inputs' shapes")
+    ldq, ldk, ldqo, ldko = _heads(q, "q", R, hd), _heads(k, "k", R, hd), _heads(q_out, "q_out", R, hd), _heads(k_out, "k_out", R, hd)
+    nq, nkv = qs[1], ks[1]
     n_pos = cos.shape[0]
-    for t, name, n in ((q_norm, "q_norm", hd), (k_norm, "k_norm", hd), (cos, "cos", n_pos * (hd // 2)), (sin, "sin", n_pos * (hd // 2))):
-        if t.dtype is not _F32T or t.numel() != n or not t.is_contiguous():
-            _need(t, name, f"a contiguous fp32 tensor of {n} elements")
+    n = n_pos * (hd // 2)
+    if q_norm.dtype is not _F32T or q_norm.numel() != hd or not q_norm.is_contiguous():
+        _need(q_norm, "q_norm", f"a contiguous fp32 tensor of {hd} elements")
+    if k_norm.dtype is not _F32T or k_norm.numel() != hd or not k_norm.is_contiguous():
+        _need(k_norm, "k_norm", f"a contiguous fp32 tensor of {hd} elements")
+    if cos.dtype is not _F32T or cos.numel() != n or not cos.is_contiguous():
+        _need(cos, "cos", f"a contiguous fp32 tensor of {n_pos} x {hd // 2}")
+    if sin.dtype is not _F32T or sin.numel() != n or not sin.is_contiguous():
+        _need(sin, "sin", f"a contiguous fp32 tensor of {n_pos} x {hd // 2}")
     if pos.dtype is not _I32T or pos.numel() != R or not pos.is_contiguous():
         _need(pos, "pos", f"a contiguous int32 tensor of {R} elements")
     dev = q.get_device()
