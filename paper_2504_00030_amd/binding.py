@@ -627,14 +627,6 @@ def k_gemm_f8(w, w_scale, x, y, x_scale=None, workspace=None, stream: int = 0):
         _refused(rc, "spec_k_gemm_f8")
 
 
-def _heads(t, name: str, R: int, hd: int):
-    """Row stride of a [R][heads][hd] tensor whose rows hold their heads one after the other."""
-    shape, stride = t.shape, t.stride()
-    if len(shape) != 3 or shape[0] != R or shape[2] != hd or (stride[1] != hd and shape[1] > 1) or (stride[2] != 1 and hd > 1):
-        _need(t, name, f"[{R}][heads][{hd}] with the heads of a row one after the other")
-    return stride[0] if R > 1 else shape[1] * hd
-
-
 def k_qk_norm_rope(q, k, q_norm, k_norm, cos, sin, pos, q_out, k_out, eps: float = 1e-5, stream: int = 0):
     """RMS norm (weights q_norm, k_norm fp32 [hd]) and rotation of the heads of q [R][nq][hd] and k [R][nkv][hd] (fp32 or
     bf16, views into fused rows included) into q_out, k_out (fp32 or bf16, may be the inputs).  cos, sin: fp32
@@ -645,8 +637,19 @@ def k_qk_norm_rope(q, k, q_norm, k_norm, cos, sin, pos, q_out, k_out, eps: float
     R, hd = qs[0], qs[-1]
     if q.dtype is not k.dtype or q_out.dtype is not k_out.dtype or q_out.shape != qs or k_out.shape != ks:
         raise ValueError("q and k must have one type, and the outputs theirs and the inputs' shapes")
-    ldq, ldk, ldqo, ldko = _heads(q, "q", R, hd), _heads(k, "k", R, hd), _heads(q_out, "q_out", R, hd), _heads(k_out, "k_out", R, hd)
+    if len(qs) != 3 or len(ks) != 3 or ks[0] != R or ks[2] != hd:
+        _need(k, "k", f"[{R}][heads][{hd}]")
     nq, nkv = qs[1], ks[1]
+    ldq, hq, eq = q.stride()
+    ldk, hk, ek = k.stride()
+    ldqo, hqo, eqo = q_out.stride()
+    ldko, hko, eko = k_out.stride()
+    if not (hq == hk == hqo == hko == hd and eq == ek == eqo == eko == 1):
+        for t, name in ((q, "q"), (k, "k"), (q_out, "q_out"), (k_out, "k_out")):
+            if (t.stride(1) != hd and t.shape[1] > 1) or t.stride(2) != 1:  # (the stride of a single head says nothing)
+                _need(t, name, f"[{R}][heads][{hd}] with the heads of a row one after the other")
+    if R < 2:  # nor does the row stride of a single row
+        ldq, ldk, ldqo, ldko = nq * hd, nkv * hd, nq * hd, nkv * hd
     n_pos = cos.shape[0]
     n = n_pos * (hd // 2)
     if q_norm.dtype is not _F32T or q_norm.numel() != hd or not q_norm.is_contiguous():
