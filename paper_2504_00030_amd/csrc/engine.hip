@@ -1762,8 +1762,8 @@ static size_t width(int32_t dtype) { return dtype == SPEC_F32 ? 4 : 2; }
 
 int spec_k_quant_f8(const void *x, int32_t dtype, int64_t ldx, int32_t R, int32_t K, void *q, float *scale, void *stream) {
     if (!wide(dtype)) return refuse(SPEC_EINVAL, "quant_f8: x must be fp32 or bf16");
-    if (R < 0 || K < 16 || K > F8_K_MAX || K % 16 || ldx < K)
-        return refuse(SPEC_EINVAL, "quant_f8: R < 0, K not a multiple of 16 in 16 .. 2^22, or ldx < K");
+    if (R < 0 || R > F8_ROWS_MAX || K < 16 || K > F8_K_MAX || K % 16 || ldx < K)
+        return refuse(SPEC_EINVAL, "quant_f8: R outside 0 .. 2^30, K not a multiple of 16 in 16 .. 2^22, or ldx < K");
     if (R == 0) return SPEC_OK;
     if (!x || !q || !scale) return refuse(SPEC_EINVAL, "quant_f8: null pointer");
     if (off(x, width(dtype)) || off(q, 16) || off(scale, 4)) return refuse(SPEC_EINVAL, "quant_f8: misaligned pointer");
@@ -1771,8 +1771,8 @@ int spec_k_quant_f8(const void *x, int32_t dtype, int64_t ldx, int32_t R, int32_
 }
 
 int64_t spec_k_gemm_f8_workspace(int32_t K, int32_t R, int32_t x_dtype) {
-    if (K < 16 || K > F8_K_MAX || K % 16 || R < 0 || (x_dtype != SPEC_F8 && !wide(x_dtype)))
-        return refuse(SPEC_EINVAL, "gemm_f8_workspace: R < 0, K not a multiple of 16 in 16 .. 2^22, or unknown type of x");
+    if (K < 16 || K > F8_K_MAX || K % 16 || R < 0 || R > F8_ROWS_MAX || (x_dtype != SPEC_F8 && !wide(x_dtype)))
+        return refuse(SPEC_EINVAL, "gemm_f8_workspace: R outside 0 .. 2^30, K not a multiple of 16 in 16 .. 2^22, or unknown type of x");
     return x_dtype == SPEC_F8 ? 0 : (int64_t)132 * R * ((K + 127) / 128);
 }
 
@@ -1781,8 +1781,8 @@ int spec_k_gemm_f8(const void *w, const float *w_scale, int32_t N, int32_t K, co
                    int64_t workspace_bytes, void *stream) {
     const bool f8 = x_dtype == SPEC_F8;
     if ((!f8 && !wide(x_dtype)) || !wide(y_dtype)) return refuse(SPEC_EINVAL, "gemm_f8: x must be e4m3, fp32 or bf16, y fp32 or bf16");
-    if (N < 1 || K < 16 || K > F8_K_MAX || K % 16 || R < 0 || ldx < K || ldy < N || workspace_bytes < 0 || (f8 && ldx != K))
-        return refuse(SPEC_EINVAL, "gemm_f8: N < 1, R < 0, K not a multiple of 16 in 16 .. 2^22, or a row stride that does not fit");
+    if (N < 1 || N > F8_ROWS_MAX || K < 16 || K > F8_K_MAX || K % 16 || R < 0 || R > F8_ROWS_MAX || ldx < K || ldy < N || workspace_bytes < 0 || (f8 && ldx != K))
+        return refuse(SPEC_EINVAL, "gemm_f8: N outside 1 .. 2^30, R outside 0 .. 2^30, K not a multiple of 16 in 16 .. 2^22, or a row stride that does not fit");
     if (R == 0) return SPEC_OK;
     if (!w || !w_scale || !x || !y || (f8 ? !x_scale : x_scale != nullptr))
         return refuse(SPEC_EINVAL, "gemm_f8: null pointer (x_scale goes with e4m3 rows, and only with them)");
@@ -1817,8 +1817,9 @@ int spec_k_qk_norm_rope(const void *q, int64_t ldq, int32_t nq, const void *k, i
                         int64_t ldko, int32_t out_dtype, void *stream) {
     if (!wide(dtype) || !wide(out_dtype)) return refuse(SPEC_EINVAL, "qk_norm_rope: heads must be fp32 or bf16");
     if (hd < 2 || hd > 512 || hd % 2) return refuse(SPEC_EINVAL, "qk_norm_rope: hd must be even, 2 to 512");
-    if (nq < 0 || nkv < 0 || (int64_t)nq + nkv < 1 || (int64_t)nq + nkv > 0x7fffffff || R < 0 || n_pos < 1 || !(eps >= 0.f))
-        return refuse(SPEC_EINVAL, "qk_norm_rope: no heads, R < 0, n_pos < 1 or eps < 0");
+    if (nq < 0 || nkv < 0 || (int64_t)nq + nkv < 1 || (int64_t)nq + nkv > 0x7fffffff || R < 0 || R > F8_ROWS_MAX ||
+        (int64_t)R * ((int64_t)nq + nkv) > 0x7fffffff || n_pos < 1 || !(eps >= 0.f))
+        return refuse(SPEC_EINVAL, "qk_norm_rope: no heads, R < 0, R * heads beyond 2^31, n_pos < 1 or eps < 0");
     if ((nq && (ldq < (int64_t)nq * hd || ldqo < (int64_t)nq * hd)) || (nkv && (ldk < (int64_t)nkv * hd || ldko < (int64_t)nkv * hd)))
         return refuse(SPEC_EINVAL, "qk_norm_rope: row stride below the heads' width");
     if (R == 0) return SPEC_OK;

@@ -315,6 +315,9 @@ static hipError_t launch_stream(const F8Args &a, hipStream_t s) {
 }
 
 // ---- product: tiles in LDS -------------------------------------------------------------------------------------
+// This wave's copies into LDS have landed: vmcnt(0), the other counters as they are.  A barrier alone is no promise of it.
+__device__ __forceinline__ void copies_done() { __builtin_amdgcn_s_waitcnt(0x0f70); }
+
 // A workgroup computes TN columns by TR rows of y with PN x PR waves.  A stage of LDS holds one block of k of both
 // operands; two stages alternate, and while one multiplies, the next is on its way from memory straight into the other
 // (16 bytes a lane, no registers).  The two stages are two arrays, and the loop is unrolled over them: the compiler then
@@ -424,6 +427,7 @@ __global__ __launch_bounds__(64 * PN * PR, 2) void f8_tile_k(const F8Args a, con
 #pragma unroll
         for (int j = 0; j < WR; ++j) sc[j] = nsc[j];
         auto meet = [&] {
+            copies_done();
             __syncthreads();
             trim(b + 1, nxt);
             frag(nxt + lw, w0[0], w1[0]);
@@ -497,6 +501,7 @@ __global__ __launch_bounds__(64 * PN * PR, 2) void f8_tile_k(const F8Args a, con
 #pragma unroll
     for (int i = 0; i < LW + LX; ++i) copy(0, i, stage0);
     scales(0);
+    copies_done();
     __syncthreads();
     trim(0, stage0);
 #pragma unroll

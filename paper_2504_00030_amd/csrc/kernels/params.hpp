@@ -193,6 +193,7 @@ struct AcceptArgs {
 };
 
 constexpr int F8_K_MAX = 1 << 22;  // longest row: a tile of 256 rows spans less than 2^31 bytes, and row offsets are 24-bit products
+constexpr int F8_ROWS_MAX = 1 << 30;  // rows of x and of w: indexes a tile past the last one stay 32-bit
 
 // e4m3 product with block scales (f8.hip): y [R][N] = x [R][K] . w [N][K]^T
 struct F8Args {

@@ -220,6 +220,70 @@ def test_product_repeats_bit_for_bit():
         assert torch.equal(ys[0], ys[1]) and torch.equal(ys[0], ys[2])
 
 
+@pytest.mark.parametrize("R,N,K", [(1, 2048, 2048), (4, 4096, 4096), (8, 130, 400), (8, 64, 14336), (12, 300, 272), (30, 520, 1040), (300, 384, 640)])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_product_of_rows_equals_quantiser_and_product(R, N, K, dtype):
+    """Rows quantised by the call, wherever it does that, give the bits of the two calls."""
+    rng = np.random.default_rng(R + N + K)
+    w, ws = _weights(rng, N, K)
+    wd, wsd, x = _f8(w), torch.from_numpy(ws).cuda(), _activations(rng, R, K, dtype).cuda()
+    work = torch.empty(pk.k_gemm_f8_workspace(K, R, dtype) + (32 << 20), dtype=torch.uint8, device="cuda")
+    one, two = torch.zeros((R, N), device="cuda"), torch.zeros((R, N), device="cuda")
+    pk.k_gemm_f8(wd, wsd, x, one, workspace=work, stream=_stream())
+    q, xs = torch.zeros((R, K), dtype=F8, device="cuda"), torch.zeros((ref.blocks(K), R), device="cuda")
+    pk.k_quant_f8(x, q, xs, stream=_stream())
+    pk.k_gemm_f8(wd, wsd, q, two, x_scale=xs, workspace=work, stream=_stream())
+    assert torch.equal(one, two)
+
+
+@pytest.mark.parametrize("x_kind", [F8, F32, BF16])
+@pytest.mark.parametrize("R,N,K", [(2, 96, 400), (20, 96, 400), (90, 200, 272), (700, 300, 144)])
+def test_product_operands_at_sixteen_byte_offsets(R, N, K, x_kind):
+    """Operands that start 16 bytes into an allocation, rows of an odd number of 16-byte units, x with a row stride."""
+    rng = np.random.default_rng(R + K)
+    w, ws = _weights(rng, N, K)
+    x = _activations(rng, R, K, F32 if x_kind == F8 else x_kind)
+    q, xs = ref.quantise(x.float().numpy())
+    wbuf = torch.zeros(N * K + 16, dtype=torch.uint8, device="cuda")
+    wbuf[16:].copy_(_f8(w).view(torch.uint8).flatten())
+    wd = wbuf[16:].view(N, K)
+    y = torch.zeros((R, N), device="cuda")
+    work = torch.empty(132 * R * ref.blocks(K), dtype=torch.uint8, device="cuda")
+    wsd = torch.from_numpy(ws).cuda()
+    if x_kind == F8:
+        xbuf = torch.zeros(R * K + 16, dtype=torch.uint8, device="cuda")
+        xbuf[16:].copy_(_f8(q).view(torch.uint8).flatten())
+        pk.k_gemm_f8(wd, wsd, xbuf[16:].view(R, K), y, x_scale=torch.from_numpy(xs).cuda(), stream=_stream())
+    else:
+        for extra, shift in ((8, 8), (3, 1)):
+            flat = torch.full((R * (K + extra) + shift,), 1e30, dtype=x_kind, device="cuda")
+            view = flat[shift:].view(R, K + extra)[:, :K]
+            view.copy_(x)
+            y.zero_()
+            pk.k_gemm_f8(wd, wsd, view, y, workspace=work, stream=_stream())
+            want, mag = ref.product(q, xs, w, ws)
+            assert (np.abs(y.double().cpu().numpy() - want) <= _product_tol(mag, want, ref.blocks(K), F32)).all()
+    want, mag = ref.product(q, xs, w, ws)
+    assert (np.abs(y.double().cpu().numpy() - want) <= _product_tol(mag, want, ref.blocks(K), F32)).all()
+
+
+@pytest.mark.parametrize("y_dtype", [F32, BF16])
+@pytest.mark.parametrize("R,N,K", [(140, 2100, 2064), (260, 6200, 400), (1030, 12300, 272), (40, 128, 16400)])
+def test_product_launch_shapes(R, N, K, y_dtype):
+    """Sizes that take the large tiles and shares of K, with edges in every direction."""
+    rng = np.random.default_rng(R)
+    w, ws = _weights(rng, N, K)
+    q, xs = ref.quantise(_activations(rng, R, K, F32).numpy())
+    work = torch.empty(32 << 20, dtype=torch.uint8, device="cuda")
+    buf = torch.full((R, N + 4), 7.0, dtype=y_dtype, device="cuda")
+    pk.k_gemm_f8(_f8(w), torch.from_numpy(ws).cuda(), _f8(q), buf[:, :N], x_scale=torch.from_numpy(xs).cuda(), workspace=work,
+                 stream=_stream())
+    got = buf.double().cpu().numpy()
+    want, mag = ref.product(q, xs, w, ws)
+    assert (np.abs(got[:, :N] - want) <= _product_tol(mag, want, ref.blocks(K), y_dtype)).all()
+    assert (got[:, N:] == 7.0).all()
+
+
 # ---- norm and rotation -------------------------------------------------------------------------------------------
 def _tables(n_pos, hd):
     ang = np.arange(n_pos)[:, None] * 10000.0 ** (-2.0 * np.arange(hd // 2) / hd)[None, :]

@@ -80,6 +80,26 @@ def test_long_prompt_through_the_ingestion_kernels():
     _run(synth.pair("small-bf16"), prompt_len=1100, n_generate=8, temperature=0.0)
 
 
+@pytest.mark.parametrize("pair_name,batch", [("1b", 1), ("8b", 3)])
+def test_full_widths_at_reduced_depth(pair_name, batch):
+    """The large pairs' widths, two target layers and one draft layer deep, drawn at a temperature in graphs."""
+    from oracle import model as om
+    cfg = synth.shrink(synth.pair(pair_name), 2, 1)
+    Wt, Wd = synth.make_pair_weights(cfg, 0, device="cuda")
+    cpu = lambda W: {k: W[k] for k in ("q_norm", "k_norm")}
+    gpu = lambda W, extra: dict(W, **{k: [t.cuda() for t in v] for k, v in extra.items()})
+    Wt, Wd = gpu(Wt, cpu(_with_norms({}, cfg.target, 1))), gpu(Wd, cpu(_with_norms({}, cfg.draft, 2)))
+    torch.cuda.synchronize()
+    widen = lambda W: {k: ([om.as_f64(a) for a in v] if isinstance(v, list) else om.as_f64(v))
+                       for k, v in synth.to_numpy_weights(W).items()}
+    eng = pk.SpecEngine(cfg.target, Wt, cfg.draft, Wd, batch=batch, max_seq=512, gamma_max=4, temperature=0.0, seed=0, use_graphs=True)
+    prompts = synth.make_prompts(batch, 60, cfg.target.vocab, 7)
+    c = run_lockstep(eng, cfg, widen(Wt), widen(Wd), prompts, 6, controller="fixed3", temperature=0.0, seed=0)
+    eng.close()
+    assert not c.failures, "\n".join(c.failures[:10])
+    assert c.max_logit_err <= TOL["bf16"] and c.coverage >= 0.7
+
+
 def test_switching_the_norms_on_and_off():
     """Without the norms again, the engine gives the bits it gave before; and a change asks for a new prompt."""
     cfg = synth.pair("small-bf16")

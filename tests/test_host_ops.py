@@ -27,7 +27,7 @@ def _norm(q=P, ldq=256, nq=2, k=P, ldk=128, nkv=1, dtype=0, hd=128, R=4, gq=P, g
 
 
 @pytest.mark.parametrize("bad", [dict(x=None), dict(q=None), dict(scale=None), dict(dtype=2), dict(dtype=3), dict(dtype=-1), dict(R=-1),
-                                 dict(K=0), dict(K=8), dict(K=120), dict(ldx=127), dict(ldx=-128), dict(x=P + 2), dict(q=P + 8),
+                                 dict(K=0), dict(K=8), dict(K=120), dict(K=2**22 + 16, ldx=2**23), dict(R=2**30 + 1), dict(ldx=127), dict(ldx=-128), dict(x=P + 2), dict(q=P + 8),
                                  dict(scale=P + 2)])
 def test_quantiser_refuses(bad):
     assert _quant(**bad) == E
@@ -35,7 +35,7 @@ def test_quantiser_refuses(bad):
 
 
 @pytest.mark.parametrize("bad", [dict(w=None), dict(ws=None), dict(x=None), dict(xs=None), dict(y=None), dict(N=0), dict(N=-5), dict(K=0),
-                                 dict(K=136), dict(R=-1), dict(ldx=129), dict(ldx=100), dict(ldy=31), dict(xt=2), dict(xt=4), dict(yt=3),
+                                 dict(K=136), dict(K=2**22 + 16, ldx=2**22 + 16), dict(R=-1), dict(R=2**30 + 1), dict(N=2**30 + 1, ldy=2**31), dict(ldx=129), dict(ldx=100), dict(ldy=31), dict(xt=2), dict(xt=4), dict(yt=3),
                                  dict(yt=2), dict(w=P + 8), dict(x=P + 4), dict(xs=P + 1), dict(y=P + 2), dict(ws=P + 2), dict(nb=-1),
                                  dict(xt=0), dict(xt=0, xs=None), dict(xt=1, xs=None, work=P, nb=527), dict(xt=1, xs=None, work=P + 8, nb=4096),
                                  dict(xt=1, xs=None, work=None, nb=4096), dict(xt=0, xs=None, x=P + 2, work=P, nb=4096)])
@@ -48,7 +48,7 @@ def test_workspace_sizes_and_refusals():
     f = pk.load().spec_k_gemm_f8_workspace
     assert f(128, 4, 3) == 0 and f(128, 4, 0) == 528 and f(1040, 3, 1) == 132 * 3 * 9
     assert f(14336, 1 << 20, 1) == 132 * (1 << 20) * 112  # beyond 32 bits
-    for bad in [(0, 4, 0), (120, 4, 0), (128, -1, 0), (128, 4, 2), (128, 4, 7)]:
+    for bad in [(0, 4, 0), (120, 4, 0), (2**22 + 16, 4, 0), (128, -1, 0), (128, 2**30 + 1, 0), (128, 4, 2), (128, 4, 7)]:
         assert f(*bad) == E
     with pytest.raises(pk.SpecError):
         pk.k_gemm_f8_workspace(120, 4, torch.float32)
@@ -60,7 +60,7 @@ def test_workspace_sizes_and_refusals():
                                  dict(qo=None), dict(ko=None), dict(dtype=2), dict(ot=3), dict(hd=0), dict(hd=127), dict(hd=514),
                                  dict(nq=0, nkv=0), dict(nq=-1), dict(nkv=-1), dict(R=-1), dict(n_pos=0), dict(eps=-1.0),
                                  dict(eps=float("nan")), dict(ldq=255), dict(ldk=127), dict(ldqo=255), dict(ldko=127), dict(q=P + 2),
-                                 dict(ko=P + 1), dict(gq=P + 2), dict(pos=P + 2), dict(c=P + 1), dict(nq=2**31 - 1, nkv=2**31 - 1)])
+                                 dict(ko=P + 1), dict(gq=P + 2), dict(pos=P + 2), dict(c=P + 1), dict(nq=2**31 - 1, nkv=2**31 - 1), dict(R=2**30 + 1), dict(R=2**30, nq=2, nkv=1)])
 def test_norm_refuses(bad):
     assert _norm(**bad) == E
     assert _said().startswith("qk_norm_rope:")
