@@ -7,7 +7,8 @@
  * pointers belong to the current device; work is enqueued on `stream` (a hipStream_t, NULL: the null stream), nothing
  * synchronises or allocates, and every call may be captured into a graph (kernel launches only).  The library keeps no
  * state between calls: calls on different streams may overlap as long as their outputs and workspaces differ.  Inputs,
- * outputs and workspaces must not overlap unless stated otherwise.  R == 0 is a call without work; R is at most 2^30.
+ * outputs and workspaces must not overlap unless stated otherwise.  R == 0 is a call without work; R is at most 2^30, and
+ * R * ceil(K / 128) stays below 2^31.
  */
 #ifndef SPEC_OPS_H
 #define SPEC_OPS_H

@@ -302,6 +302,8 @@ class SpecEngine:
         def arr(ts):
             if ts is None:
                 return None
+            if model not in (0, 1):
+                raise ValueError("model must be 0 (draft) or 1 (target)")
             ms = self._shapes[model]
             kind = "torch.float32" if ms.dtype == "fp32" else "torch.bfloat16"
             if len(ts) != ms.n_layers or any(tuple(t.shape) != (ms.head_dim,) or str(t.dtype) != kind or not t.is_cuda or
@@ -550,6 +552,11 @@ def _rows(t, name: str) -> int:
     return stride[0] if t.shape[0] > 1 else t.shape[1]
 
 
+def _too_long(*sizes):
+    """Sizes go to the library as 32-bit integers."""
+    raise ValueError(f"sizes beyond 2^31: {sizes}")
+
+
 def _refused(rc: int, where: str):
     raise SpecError(rc, where, load().spec_last_error(None).decode())
 
@@ -561,6 +568,8 @@ def k_quant_f8(x, q, scale, stream: int = 0):
         _setup()
     ldx = _rows(x, "x")
     R, K = x.shape
+    if (R | K) >> 31:
+        _too_long(R, K)
     if q.shape != x.shape or _KINDS.get(q.dtype) != SPEC_F8 or not q.is_contiguous():
         _need(q, "q", f"a contiguous e4m3 tensor of {R} x {K}")
     if scale.shape != ((K + 127) // 128, R) or scale.dtype is not _F32T or not scale.is_contiguous():
@@ -580,6 +589,8 @@ def k_gemm_f8_workspace(K: int, R: int, x_dtype) -> int:
         _setup()
     if x_dtype not in _KINDS:
         raise ValueError(f"unsupported element type {x_dtype}")
+    if (K | R) >> 31:
+        _too_long(K, R)
     n = load().spec_k_gemm_f8_workspace(K, R, _KINDS[x_dtype])
     if n < 0:
         _refused(int(n), "spec_k_gemm_f8_workspace")
@@ -595,6 +606,8 @@ def k_gemm_f8(w, w_scale, x, y, x_scale=None, workspace=None, stream: int = 0):
     N, K = w.shape
     ldx, ldy = _rows(x, "x"), _rows(y, "y")
     R, KB = x.shape[0], (K + 127) // 128
+    if (N | K | R) >> 31:
+        _too_long(N, K, R)
     if x.shape[1] != K:
         _need(x, "x", f"of {K} columns")
     if y.shape != (R, N):
@@ -652,6 +665,8 @@ def k_qk_norm_rope(q, k, q_norm, k_norm, cos, sin, pos, q_out, k_out, eps: float
         ldq, ldk, ldqo, ldko = nq * hd, nkv * hd, nq * hd, nkv * hd
     n_pos = cos.shape[0]
     n = n_pos * (hd // 2)
+    if (R | nq | nkv | hd | n_pos) >> 31:
+        _too_long(R, nq, nkv, hd, n_pos)
     if q_norm.dtype is not _F32T or q_norm.numel() != hd or not q_norm.is_contiguous():
         _need(q_norm, "q_norm", f"a contiguous fp32 tensor of {hd} elements")
     if k_norm.dtype is not _F32T or k_norm.numel() != hd or not k_norm.is_contiguous():

@@ -8,6 +8,13 @@ namespace sd {
 
 constexpr int WAVE = 64;
 
+// One axis of a grid holds less than 2^32 threads: from 2^20 workgroups on a long grid goes on along y, and the kernel
+// leaves out the ones past its last.
+inline dim3 grid_of(int64_t workgroups) {
+    return workgroups <= 1 << 20 ? dim3((unsigned)workgroups) : dim3(1 << 20, (unsigned)((workgroups + (1 << 20) - 1) >> 20));
+}
+__device__ __forceinline__ uint32_t workgroup() { return blockIdx.x + (blockIdx.y << 20); }
+
 typedef uint16_t bf16_t;  // raw bfloat16 bits
 
 __device__ __forceinline__ float bf16_lo(uint32_t u) { return __uint_as_float(u << 16); }

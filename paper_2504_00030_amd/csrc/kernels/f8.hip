@@ -93,7 +93,7 @@ __device__ __forceinline__ void store_y4(OT *y, const f4_t v, int n, int N, bool
 template <typename T, bool VEC>
 __global__ __launch_bounds__(256) void quant_f8_k(const T *__restrict__ x, int64_t ldx, int R, int K, int KB,
                                                   uint8_t *__restrict__ q, float *__restrict__ scale) {
-    const uint32_t grp = blockIdx.x * 16 + (threadIdx.x >> 4);  // below 2^31 + 16: the host bounds R * KB
+    const uint32_t grp = workgroup() * 16 + (threadIdx.x >> 4);  // below 2^32: the host bounds R * KB
     const int sub = threadIdx.x & 15;
     const uint32_t r = grp / KB, b = grp % KB;
     if (r >= (uint32_t)R) return;
@@ -139,7 +139,7 @@ static void launch_quant_t(const void *x, int64_t ldx, int R, int K, int KB, voi
 hipError_t launch_quant_f8(const void *x, int dtype, int64_t ldx, int R, int K, void *q, float *scale, hipStream_t s) {
     const int KB = (K + F8_BLOCK - 1) / F8_BLOCK;
     if ((int64_t)R * KB > 0x7fffffff) return hipErrorInvalidValue;
-    const dim3 grid((unsigned)(((int64_t)R * KB + 15) / 16));
+    const dim3 grid = grid_of(((int64_t)R * KB + 15) / 16);
     if (dtype == DT_F32) launch_quant_t<float>(x, ldx, R, K, KB, q, scale, grid, s);
     else launch_quant_t<__bf16>(x, ldx, R, K, KB, q, scale, grid, s);
     return hipGetLastError();
@@ -195,7 +195,9 @@ __global__ __launch_bounds__(64 * NW) void f8_stream_k(const F8Args a) {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int sub = lane & 15, g = lane >> 4;
     const int n_tiles = (a.N + 16 * NG - 1) / (16 * NG);
-    const int n0 = (blockIdx.x % n_tiles) * 16 * NG, r0 = (blockIdx.x / n_tiles) * 16 * RB;
+    const uint32_t wg = workgroup();
+    const int n0 = (wg % n_tiles) * 16 * NG, r0 = (wg / n_tiles) * 16 * RB;
+    if (r0 >= a.R) return;
     const int K = a.K, KB = a.KB;
     constexpr int XB = XIN == X_F32 ? 4 : (XIN == X_BF16 ? 2 : 1);  // bytes of an element of x
     const uint8_t *wp[NG], *xp[RB];
@@ -309,8 +311,7 @@ __global__ __launch_bounds__(64 * NW) void f8_stream_k(const F8Args a) {
 template <typename OT, int NG, int RB, int NW, int D, int XIN>
 static hipError_t launch_stream(const F8Args &a, hipStream_t s) {
     const int64_t wgs = (int64_t)((a.N + 16 * NG - 1) / (16 * NG)) * ((a.R + 16 * RB - 1) / (16 * RB));
-    if (wgs > 0x7fffffff) return hipErrorInvalidValue;
-    hipLaunchKernelGGL((f8_stream_k<OT, NG, RB, NW, D, XIN>), dim3((unsigned)wgs), dim3(64 * NW), 0, s, a);
+    hipLaunchKernelGGL((f8_stream_k<OT, NG, RB, NW, D, XIN>), grid_of(wgs), dim3(64 * NW), 0, s, a);  // R <= 32: below 2^28
     return hipGetLastError();
 }
 
@@ -339,8 +340,8 @@ __global__ __launch_bounds__(64 * PN * PR, 2) void f8_tile_k(const F8Args a, con
     // the tiles it works on together share rows of w and x in its L2
     // (a tile's shares of K stand side by side: they run together)
     const int total = n_tiles * r_tiles * shares, per = (total + 7) >> 3;
-    const int id = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
-    if (id >= total || (int)(blockIdx.x >> 3) >= per) return;
+    const int wg = (int)workgroup(), id = (wg & 7) * per + (wg >> 3);
+    if (id >= total || (wg >> 3) >= per) return;
     const int tile = id / shares, share = id % shares;
     const int band = tile / (8 * n_tiles), in_band = tile % (8 * n_tiles), rows_in_band = min(8, r_tiles - band * 8);
     const int n0 = in_band / rows_in_band * TN, r0 = (band * 8 + in_band % rows_in_band) * TR;
@@ -560,20 +561,22 @@ __global__ __launch_bounds__(256) void f8_sum_k(const float *__restrict__ part, 
 }
 
 template <typename OT, bool F16, int TN, int TR, int PN, int PR>
-static hipError_t launch_tile(const F8Args &a, int shares, hipStream_t s) {
+static hipError_t launch_tile(const F8Args &a, hipStream_t s, int shares = 1) {
     const int64_t n_tiles = (a.N + TN - 1) / TN, r_tiles = (a.R + TR - 1) / TR, total = n_tiles * r_tiles * shares;
-    if (total > 0x7ffffff0 || 8 * n_tiles > 0x7fffffff) return hipErrorInvalidValue;
-    const dim3 grid((unsigned)((total + 7) / 8 * 8)), block(64 * PN * PR);
-    if (shares == 1) {
-        hipLaunchKernelGGL((f8_tile_k<OT, F16, TN, TR, PN, PR>), grid, block, 0, s, a, (int)n_tiles, (int)r_tiles, 1);
-        return hipGetLastError();
-    }
+    if (total > 1 << 30) return hipErrorInvalidValue;  // beyond any memory: N and R are at most 2^30 each
+    hipLaunchKernelGGL((f8_tile_k<OT, F16, TN, TR, PN, PR>), grid_of((total + 7) / 8 * 8), dim3(64 * PN * PR), 0, s, a, (int)n_tiles,
+                       (int)r_tiles, shares);
+    return hipGetLastError();
+}
+
+template <typename OT, bool F16, int TN, int TR, int PN, int PR>
+static hipError_t launch_shared(const F8Args &a, int shares, hipStream_t s) {
+    if (shares == 1) return launch_tile<OT, F16, TN, TR, PN, PR>(a, s);
     F8Args p = a;  // partial sums: [shares][R][N]
     p.y = a.part; p.ldy = a.N;
-    hipLaunchKernelGGL((f8_tile_k<float, F16, TN, TR, PN, PR>), grid, block, 0, s, p, (int)n_tiles, (int)r_tiles, shares);
-    const hipError_t e = hipGetLastError();
+    const hipError_t e = launch_tile<float, F16, TN, TR, PN, PR>(p, s, shares);
     if (e != hipSuccess) return e;
-    const int64_t items = (int64_t)a.R * ((a.N + 3) / 4);
+    const int64_t items = (int64_t)a.R * ((a.N + 3) / 4);  // few tiles share: far below 2^32
     hipLaunchKernelGGL((f8_sum_k<OT>), dim3((unsigned)((items + 255) / 256)), dim3(256), 0, s, a.part, shares, a.R, a.N,
                        reinterpret_cast<OT *>(a.y), a.ldy);
     return hipGetLastError();
@@ -624,13 +627,13 @@ static hipError_t launch_gemm_f8_t(const F8Args &a, hipStream_t s) {
     constexpr bool F16 = sizeof(OT) == 4;
     if constexpr (F16) {
         const int64_t t = tiles(128, 128);  // 512 x 6144 x 4096: 45 with two shares, 48 with 64 x 64 tiles
-        if (t >= 128) return launch_tile<OT, true, 128, 128, 2, 2>(a, pick_shares(a, t, 384), s);
+        if (t >= 128) return launch_shared<OT, true, 128, 128, 2, 2>(a, pick_shares(a, t, 384), s);
     } else {
         // 512 x 28672 x 4096: 77 / 92 / 111 / 126 with 256 x 256 / 128 x 128 / 128 x 64 / 64 x 64; 1024 x 6144 x 4096: 65 / 46 / 45 / 60
-        if (tiles(256, 256) >= 192) return launch_tile<OT, false, 256, 256, 2, 4>(a, 1, s);
-        if (tiles(128, 64) >= 384) return launch_tile<OT, false, 128, 64, 4, 1>(a, 1, s);
+        if (tiles(256, 256) >= 192) return launch_tile<OT, false, 256, 256, 2, 4>(a, s);
+        if (tiles(128, 64) >= 384) return launch_tile<OT, false, 128, 64, 4, 1>(a, s);
     }
-    return launch_tile<OT, F16, 64, 64, 2, 2>(a, pick_shares(a, tiles(64, 64), 768), s);
+    return launch_shared<OT, F16, 64, 64, 2, 2>(a, pick_shares(a, tiles(64, 64), 768), s);
 }
 
 hipError_t launch_gemm_f8(const F8Args &a, hipStream_t s) {

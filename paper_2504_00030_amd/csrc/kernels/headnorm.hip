@@ -102,7 +102,7 @@ __global__ __launch_bounds__(256) void head_norm_k(const HeadNormArgs a) {
     constexpr int GPB = 256 / LPH;
     const uint32_t nh = a.nq + a.nkv;
     const int half = a.hd >> 1;
-    const uint32_t item = blockIdx.x * GPB + threadIdx.x / LPH;  // below 2^31 + GPB: the host bounds R * nh
+    const uint32_t item = workgroup() * GPB + threadIdx.x / LPH;  // below 2^32: the host bounds R * nh
     const uint32_t r = item / nh;
     const int hh = (int)(item % nh);
     if (r >= (uint32_t)a.R) return;  // whole groups of lanes leave: the sums below stay inside a group
@@ -128,8 +128,8 @@ __global__ __launch_bounds__(256) void head_norm_k(const HeadNormArgs a) {
 
 template <typename T, typename OT, int LPH, bool VEC, int W>
 static hipError_t launch_one(const HeadNormArgs &a, hipStream_t s) {
-    const unsigned wgs = (unsigned)(((int64_t)a.R * (a.nq + a.nkv) + 256 / LPH - 1) / (256 / LPH));
-    hipLaunchKernelGGL((head_norm_k<T, OT, LPH, VEC, W>), dim3(wgs), dim3(256), 0, s, a);
+    const int64_t wgs = ((int64_t)a.R * (a.nq + a.nkv) + 256 / LPH - 1) / (256 / LPH);
+    hipLaunchKernelGGL((head_norm_k<T, OT, LPH, VEC, W>), grid_of(wgs), dim3(256), 0, s, a);
     return hipGetLastError();
 }
 
@@ -140,8 +140,10 @@ static hipError_t launch_lanes(const HeadNormArgs &a, hipStream_t s) {
     if (need <= 4) return launch_one<T, OT, 4, VEC, W>(a, s);
     if (need <= 8) return launch_one<T, OT, 8, VEC, W>(a, s);
     if (need <= 16) return launch_one<T, OT, 16, VEC, W>(a, s);
-    if (need <= 32) return launch_one<T, OT, 32, VEC, W>(a, s);
-    return launch_one<T, OT, 64, VEC, W>(a, s);
+    if constexpr (W == 1) {  // eight pairs a lane: 512 elements are 32 lanes
+        if (need > 32) return launch_one<T, OT, 64, VEC, W>(a, s);
+    }
+    return launch_one<T, OT, 32, VEC, W>(a, s);
 }
 
 template <typename T, typename OT>

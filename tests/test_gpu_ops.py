@@ -387,6 +387,50 @@ def test_norm_rows_far_apart():
     assert (np.abs(q.double().cpu().numpy() - want) <= (hd / 2 + 8) * 2.0 ** -23 * mag + 2.0 ** -8 * np.abs(want)).all()
 
 
+# ---- grids past the threads one axis holds (2^32) --------------------------------------------------------------------
+def test_quantiser_of_very_many_rows():
+    """2^28 blocks and more, sixteen lanes each: 4099 rows over and over, against one call for them alone."""
+    times = 65536
+    base = torch.randn((4099, 16), device="cuda").to(BF16)
+    x = base.repeat(times, 1)
+    q = torch.zeros(x.shape, dtype=torch.uint8, device="cuda")
+    scale = torch.zeros((1, x.shape[0]), device="cuda")
+    pk.k_quant_f8(x, q, scale, stream=_stream())
+    want, want_s = torch.zeros((4099, 16), dtype=torch.uint8, device="cuda"), torch.zeros((1, 4099), device="cuda")
+    pk.k_quant_f8(base, want, want_s, stream=_stream())
+    assert bool((q.view(times, 4099, 16) == want).all()) and bool((scale.view(times, 4099) == want_s).all())
+
+
+def test_product_of_very_many_columns():
+    """2^23 workgroups of 512 threads and more; the scales are powers of two, so every block repeats the first one's bits."""
+    rng = np.random.default_rng(17)
+    blocks = (1 << 20) + 3
+    w, _ = _weights(rng, 128, 16)
+    first = _f8(w)
+    x = _activations(rng, 2, 16, F32).cuda()
+    q, qs = torch.zeros((2, 16), dtype=F8, device="cuda"), torch.zeros((1, 2), device="cuda")
+    pk.k_quant_f8(x, q, qs, stream=_stream())
+    ws = 2.0 ** (torch.arange(blocks, device="cuda") % 11 - 5).float()[:, None]
+    y, want = torch.zeros((2, 128 * blocks), device="cuda"), torch.zeros((2, 128), device="cuda")
+    pk.k_gemm_f8(first.view(torch.uint8).repeat(blocks, 1), ws, q, y, qs, stream=_stream())
+    pk.k_gemm_f8(first, torch.ones((1, 1), device="cuda"), q, want, qs, stream=_stream())
+    assert bool((y.view(2, blocks, 128) == want[:, None] * ws).all())
+
+
+def test_norm_of_very_many_heads():
+    """2^30 heads and more, four lanes each: seven rows over and over."""
+    times, nq, hd = 149797, 1023, 2
+    heads = torch.randn((7, nq + 1, hd), device="cuda").to(BF16)
+    cos, sin = (torch.from_numpy(t).cuda() for t in _tables(7, hd))
+    g = torch.tensor([1.25, 0.75], device="cuda")
+    pos = torch.arange(7, dtype=torch.int32, device="cuda")
+    want = torch.zeros_like(heads)
+    pk.k_qk_norm_rope(heads[:, :nq], heads[:, nq:], g, g, cos, sin, pos, want[:, :nq], want[:, nq:], stream=_stream())
+    rows = heads.repeat(times, 1, 1)
+    pk.k_qk_norm_rope(rows[:, :nq], rows[:, nq:], g, g, cos, sin, pos.repeat(times), rows[:, :nq], rows[:, nq:], stream=_stream())
+    assert bool((rows.view(times, 7, nq + 1, hd) == want).all())
+
+
 # ---- together ------------------------------------------------------------------------------------------------------
 class _Layer:
     """The QKV step of one layer: rows -> e4m3 product with the fused matrix -> heads normed and rotated in place."""

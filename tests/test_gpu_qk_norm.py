@@ -154,3 +154,16 @@ def test_refusals():
     assert eng._lib.spec_set_qk_norm(eng._ctx, 2, None, None) == binding.SPEC_EINVAL
     assert eng._lib.spec_set_qk_norm(None, 1, None, None) == binding.SPEC_EINVAL
     eng.close()
+
+
+@pytest.mark.parametrize("model", [-1, 2])
+def test_norms_of_no_model_are_refused(model):
+    cfg = synth.pair("tiny")
+    Wt, Wd = synth.make_pair_weights(cfg, 3)
+    eng = _engine(cfg, Wt, Wd, 16, 8, 1)
+    g = [torch.ones(cfg.target.head_dim, device="cuda") for _ in range(cfg.target.n_layers)]
+    with pytest.raises(ValueError, match="model"):
+        eng.set_qk_norm(model, g, g)
+    with pytest.raises(pk.SpecError):
+        eng.set_qk_norm(model, None, None)
+    eng.close()

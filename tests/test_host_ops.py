@@ -94,3 +94,20 @@ def test_wrappers_refuse_tensors_that_do_not_fit():
         a = dict(h=h, g=g, c=c, pos=pos, o=h) | bad
         with pytest.raises(ValueError):
             pk.k_qk_norm_rope(a["h"], a["h"], a["g"], a["g"], a["c"], a["c"], a["pos"], a["o"], a.get("o2", a["o"]))
+
+
+def test_wrappers_refuse_sizes_beyond_32_bits():
+    """Sizes that a 32-bit argument would cut to a small one (tensors without memory)."""
+    new = lambda shape, dtype=torch.float32: torch.empty(shape, dtype=dtype, device="meta")
+    f8, long = torch.float8_e4m3fn, 2**32 + 16
+    with pytest.raises(ValueError, match="beyond"):
+        pk.k_quant_f8(new((long, 16)), new((long, 16), f8), new((1, long)))
+    with pytest.raises(ValueError, match="beyond"):
+        pk.k_gemm_f8_workspace(128, long, torch.float32)
+    for R, N, K in [(long, 32, 16), (4, long, 16), (4, 32, long)]:
+        with pytest.raises(ValueError, match="beyond"):
+            pk.k_gemm_f8(new((N, K), f8), new(((N + 127) // 128, (K + 127) // 128)), new((R, K)), new((R, N)))
+    for R, n_pos in [(long, 8), (4, long)]:
+        h, c = new((R, 1, 2)), new((n_pos, 1))
+        with pytest.raises(ValueError, match="beyond"):
+            pk.k_qk_norm_rope(h, h, new(2), new(2), c, c, new(R, torch.int32), h, h)
