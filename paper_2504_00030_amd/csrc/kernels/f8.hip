@@ -255,39 +255,45 @@ __global__ __launch_bounds__(64 * NW) void f8_stream_k(const F8Args a) {
 #pragma unroll
         for (int j = 0; j < RB; ++j) load_x(st[d], b, j);
     }
-    for (int b0 = wave; b0 < KB; b0 += D * NW) {
+    // multiplies block b, which `s` holds; `more`: `s` is loaded anew, each register as soon as its values have been converted
+    auto step = [&](Stage &s, int b, auto more) {
+        const int nb = b + D * NW;
+        h8_t hw[NG][4];
 #pragma unroll
-        for (int d = 0; d < D; ++d) {
-            const int b = b0 + d * NW;
-            if (b >= KB) break;
-            Stage &s = st[d];
-            // each register set is reloaded as soon as its values have been converted
-            const int nb = min(b + D * NW, KB - 1);
-            h8_t hw[NG][4];
+        for (int i = 0; i < NG; ++i) widen(s.w[i][0], s.w[i][1], hw[i]);
+        const float sw = s.sw;
+        if constexpr (more) load_w(s, nb);
+        const bool part = (b + 1) * F8_BLOCK > K;
+        const bool dead0 = part && b * F8_BLOCK + g * 16 >= K, dead1 = part && b * F8_BLOCK + 64 + g * 16 >= K;
+#pragma unroll
+        for (int j = 0; j < RB; ++j) {
+            h8_t hx[4];
+            const float sc = sw * take_x<XIN>(s.x[j], s.sx[j], dead0, dead1, hx);
+            if constexpr (more) load_x(s, nb, j);
 #pragma unroll
             for (int i = 0; i < NG; ++i) {
-                hw[i][0] = to_f16(s.w[i][0][0], s.w[i][0][1]); hw[i][1] = to_f16(s.w[i][0][2], s.w[i][0][3]);
-                hw[i][2] = to_f16(s.w[i][1][0], s.w[i][1][1]); hw[i][3] = to_f16(s.w[i][1][2], s.w[i][1][3]);
-            }
-            const float sw = s.sw;
-            load_w(s, nb);
-            const bool part = (b + 1) * F8_BLOCK > K;
-            const bool dead0 = part && b * F8_BLOCK + g * 16 >= K, dead1 = part && b * F8_BLOCK + 64 + g * 16 >= K;
+                f4_t t = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int j = 0; j < RB; ++j) {
-                h8_t hx[4];
-                const float sc = sw * take_x<XIN>(s.x[j], s.sx[j], dead0, dead1, hx);
-                load_x(s, nb, j);
+                for (int q = 0; q < 4; ++q) t = __builtin_amdgcn_mfma_f32_16x16x32_f16(hw[i][q], hx[q], t, 0, 0, 0);
 #pragma unroll
-                for (int i = 0; i < NG; ++i) {
-                    f4_t t = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) t = __builtin_amdgcn_mfma_f32_16x16x32_f16(hw[i][q], hx[q], t, 0, 0, 0);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) acc[i][j][e] = fmaf(t[e], sc, acc[i][j][e]);
-                }
+                for (int e = 0; e < 4; ++e) acc[i][j][e] = fmaf(t[e], sc, acc[i][j][e]);
             }
         }
+    };
+    const std::true_type yes;
+    const std::false_type no;
+    // full rounds while every stage has a block to come (loads past the last block would cost as much as real ones)
+    int b0 = wave;
+    for (; b0 + (2 * D - 1) * NW < KB; b0 += D * NW) {
+#pragma unroll
+        for (int d = 0; d < D; ++d) step(st[d], b0 + d * NW, yes);
+    }
+#pragma unroll
+    for (int d = 0; d < 2 * D - 1; ++d) {
+        const int b = b0 + d * NW;
+        if (b >= KB) break;
+        if (d < D - 1 && b + D * NW < KB) step(st[d], b, yes);
+        else step(st[d % D], b, no);
     }
     __shared__ f4_t red[NW][NG][64];
     OT *y = reinterpret_cast<OT *>(a.y);
@@ -311,7 +317,7 @@ __global__ __launch_bounds__(64 * NW) void f8_stream_k(const F8Args a) {
 template <typename OT, int NG, int RB, int NW, int D, int XIN>
 static hipError_t launch_stream(const F8Args &a, hipStream_t s) {
     const int64_t wgs = (int64_t)((a.N + 16 * NG - 1) / (16 * NG)) * ((a.R + 16 * RB - 1) / (16 * RB));
-    hipLaunchKernelGGL((f8_stream_k<OT, NG, RB, NW, D, XIN>), grid_of(wgs), dim3(64 * NW), 0, s, a);  // R <= 32: below 2^28
+    hipLaunchKernelGGL((f8_stream_k<OT, NG, RB, NW, D, XIN>), grid_of(wgs), dim3(64 * NW), 0, s, a);
     return hipGetLastError();
 }
 
@@ -583,14 +589,15 @@ static hipError_t launch_shared(const F8Args &a, int shares, hipStream_t s) {
 }
 
 // ---- which kernel runs ---------------------------------------------------------------------------------------------
-// Times below: rows as fp32 or bf16 with fresh weights from HBM for every call, in microseconds.
+// Times below: fresh weights from HBM for every call, in microseconds, launches back to back.
 
 // Whether the product quantises fp32 / bf16 rows itself, in every workgroup anew, instead of by a launch of the quantiser
-// in front: for a few rows of a small matrix (1 x 2048 x 2048: 4.9 against 5.6 with both launches in a graph, 4 x 4096 x
-// 4096: 8.1 against 9.1; but 1 x 6144 x 4096: 12.0 against 10.4, 1 x 4096 x 14336: 20.0 against 14.6).
+// in front: for a few rows of a small matrix (both launches in a graph, fp32 rows: 1 x 2048 x 2048 5.4 against 5.9, 8 x 8192 x
+// 2048 7.9 against 8.3, 4 x 4096 x 4096 8.9 against 8.6, and a launch less for the host; but 1 x 4096 x 5632 10.6 against 9.1,
+// 1 x 2048 x 8192 12.4 against 9.8).
 bool gemm_f8_takes_wide(const F8Args &a) {
     const int64_t size = a.x_type == X_F32 ? 4 : 2;
-    return a.R <= 8 && a.K <= 4096 && (int64_t)a.N * a.K <= 4096 * 4096 && reinterpret_cast<uintptr_t>(a.x) % 16 == 0 &&
+    return a.R <= 8 && a.K <= 4096 && a.N <= 8192 && (int64_t)a.N * a.K <= 4096 * 4096 && reinterpret_cast<uintptr_t>(a.x) % 16 == 0 &&
            a.ldx * size % 16 == 0;
 }
 
@@ -602,25 +609,46 @@ static int pick_shares(const F8Args &a, int64_t tiles, int64_t wanted) {
     return (int)std::max<int64_t>(1, std::min({wanted / tiles, (int64_t)8, (int64_t)a.KB / 8, fit}));
 }
 
-// Up to 16 rows: the stream, sixteen waves once each has two blocks of k (1 x 28672 x 4096: 23.8 against 25.6 with eight;
-// 1 x 128256 x 2048: 61 against 42).
-template <typename OT, int XIN>
-static hipError_t launch_few(const F8Args &a, hipStream_t s) {
-    return a.KB >= 32 ? launch_stream<OT, 1, 1, 16, 1, XIN>(a, s) : launch_stream<OT, 1, 1, 8, 1, XIN>(a, s);
+// The stream with 16 RB rows a workgroup: 16, 32 or 64 columns, the fewest that need no more than one workgroup a compute
+// unit.  With more columns x is read less often, with fewer the chip fills sooner (16 / 32 / 64 columns: 9 x 4096 x 14336 13.8 /
+// 20 / -, 9 x 6144 x 4096 9.3 / 8.2 / -, 1 x 28672 x 4096 26.5 / 25.9 / 25.9, 32 x 4096 x 4096 8.2 / 9.7 / -, 32 x 6144 x 4096
+// 14.4 / 10.7 / -, 32 x 14336 x 4096 26.7 / 19.5 / 15.9).  Waves and stages: 9 x 4096 x 14336 13.8 with eight of two, 14.4 with
+// eight of one, 14.8 with sixteen of one; 64 x 4096 x 4096 12.9 with four waves, 13.3 with eight.
+template <typename OT, int RB, int XIN>
+static hipError_t launch_columns(const F8Args &a, hipStream_t s) {
+    const int64_t r_tiles = (a.R + 16 * RB - 1) / (16 * RB), groups = (a.N + 15) / 16;
+    constexpr int NW = RB == 4 ? 4 : 8;
+    if (groups * r_tiles <= 256) return launch_stream<OT, 1, RB, NW, RB == 1 ? 2 : 1, XIN>(a, s);
+    if constexpr (XIN == X_F8) {
+        if ((groups + 1) / 2 * r_tiles > 256) return launch_stream<OT, 4, RB, 4, 1, XIN>(a, s);
+    }
+    return launch_stream<OT, 2, RB, NW, 1, XIN>(a, s);
+}
+
+// Tiles of rows the stream makes of more than 32: of 48 rows if they are no more than tiles of 64 would be.
+static int64_t stream_row_tiles(const F8Args &a) { return (a.R + 63) / 64; }
+static bool tiles_of_48(const F8Args &a) { return (a.R + 47) / 48 == stream_row_tiles(a); }
+
+// Whether more than 32 rows go through the stream: for short rows, where the tiles' steps are few and their latency shows,
+// as long as workgroups of 64 columns fit the compute units or (48 rows, fp32: 64 rows) w is read once.  Stream against tiles, fp32 /
+// bf16 results: 40 x 2048 x 2048 6.5 / 6.4 against 11.0 / 9.7, 48 x 28672 x 4096 32.9 / 32.9 against 49.4 / 35.9, 64 x 28672 x 4096
+// 38.4 / 38.4 against 50.0 / 36.4, 128 x 4096 x 4096 15.8 / 15.4 against 18.5 / 16.4, 256 x 4096 x 2048 12.9 / 12.2 against 18.4 /
+// 15.9; but 40 x 2048 x 8192 16.8 / 16.5 against 15.8 / 14.1, 40 x 6144 x 6144 17.7 / 17.3 against 18.9 / 16.5, 192 x 8192 x 2048
+// 22.3 / 21.6 against 20.4 / 15.3.
+template <typename OT>
+static bool streams(const F8Args &a) {
+    constexpr bool exact = sizeof(OT) == 4;  // the tiles of fp32 results multiply at half the rate
+    if (a.KB > (exact ? 44 : 32)) return false;
+    return a.R <= (exact ? 64 : 48) || ((int64_t)a.N + 63) / 64 * stream_row_tiles(a) <= 256;
 }
 
 template <typename OT>
 static hipError_t launch_gemm_f8_t(const F8Args &a, hipStream_t s) {
-    if (a.x_type == X_F32) return launch_few<OT, X_F32>(a, s);
-    if (a.x_type == X_BF16) return launch_few<OT, X_BF16>(a, s);
-    if (a.R <= 16) return launch_few<OT, X_F8>(a, s);
-    if (a.R <= 32) {
-        // wider column tiles read x less often, and need more columns to give every compute unit one (24 x 4096 x 4096: 9.6 / 11.0 / 15.8
-        // with 16 / 32 / 64 columns, 32 x 6144 x 4096: 16.3 / 12.5 / 17.1, 32 x 28672 x 4096: 49.7 / 43.5 / 35.9)
-        if (a.N > 8192) return launch_stream<OT, 4, 2, 4, 1, X_F8>(a, s);
-        if (a.N > 4096) return launch_stream<OT, 2, 2, 4, 2, X_F8>(a, s);
-        return launch_stream<OT, 1, 2, 8, 1, X_F8>(a, s);
-    }
+    if (a.x_type == X_F32) return launch_columns<OT, 1, X_F32>(a, s);
+    if (a.x_type == X_BF16) return launch_columns<OT, 1, X_BF16>(a, s);
+    if (a.R <= 16) return launch_columns<OT, 1, X_F8>(a, s);
+    if (a.R <= 32) return launch_columns<OT, 2, X_F8>(a, s);
+    if (streams<OT>(a)) return tiles_of_48(a) ? launch_columns<OT, 3, X_F8>(a, s) : launch_columns<OT, 4, X_F8>(a, s);
     auto tiles = [&](int64_t tn, int64_t tr) { return (a.N + tn - 1) / tn * ((a.R + tr - 1) / tr); };
     // A tile's time is its steps times a latency that the workgroups sharing a compute unit hide, so a product with few
     // tiles takes smaller ones and shares K out (137 x 4096 x 11008: 64 with one share of 64 x 64 tiles, 29 with four).

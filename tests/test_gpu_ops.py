@@ -284,6 +284,25 @@ def test_product_launch_shapes(R, N, K, y_dtype):
     assert (got[:, N:] == 7.0).all()
 
 
+STREAMED = [(9, 4100, 2064), (16, 8200, 272), (5, 70, 4496), (1, 16, 2176), (13, 33, 16), (30, 500, 1168), (30, 4200, 400), (31, 8300, 272),
+            (47, 300, 1296), (90, 2100, 400), (40, 9000, 144), (60, 300, 2064), (120, 2200, 272), (60, 8300, 144), (200, 130, 4096)]
+TILED = [(700, 6200, 400), (140, 700, 6016), (260, 2500, 5776), (520, 4000, 5776)]
+
+
+@pytest.mark.parametrize("y_dtype", [F32, BF16])
+@pytest.mark.parametrize("R,N,K", STREAMED + TILED)
+def test_product_more_launch_shapes(R, N, K, y_dtype):
+    """One, two and four groups of columns by one to four of rows in the stream, with blocks of k that do not divide among
+    its waves; and the tiles, whole and in shares."""
+    test_product_launch_shapes(R, N, K, y_dtype)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("R,N,K", [(8, 5000, 2000), (3, 8192, 2048), (2, 4097, 144), (8, 4096, 4096)])
+def test_product_of_rows_equals_the_two_calls_in_wide_workgroups(R, N, K, dtype):
+    test_product_of_rows_equals_quantiser_and_product(R, N, K, dtype)
+
+
 # ---- norm and rotation -------------------------------------------------------------------------------------------
 def _tables(n_pos, hd):
     ang = np.arange(n_pos)[:, None] * 10000.0 ** (-2.0 * np.arange(hd // 2) / hd)[None, :]
