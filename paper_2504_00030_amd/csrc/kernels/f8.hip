@@ -85,6 +85,16 @@ __device__ __forceinline__ void store_y4(OT *y, const f4_t v, int n, int N, bool
         if (n + i < N) y[n + i] = (OT)v[i];
 }
 
+template <int N> using num = std::integral_constant<int, N>;
+// f(num<0>) .. f(num<N - 1>)
+template <int N, typename F>
+__device__ __forceinline__ void each(F f) {
+    if constexpr (N > 0) {
+        each<N - 1>(f);
+        f(num<N - 1>());
+    }
+}
+
 }  // namespace
 
 // ---- quantiser -------------------------------------------------------------------------------------------------
@@ -322,23 +332,37 @@ static hipError_t launch_stream(const F8Args &a, hipStream_t s) {
 }
 
 // ---- product: tiles in LDS -------------------------------------------------------------------------------------
-// This wave's copies into LDS have landed: vmcnt(0), the other counters as they are.  A barrier alone is no promise of it.
-__device__ __forceinline__ void copies_done() { __builtin_amdgcn_s_waitcnt(0x0f70); }
+// The workgroup meets once every wave's reads of LDS are done and its copies into LDS, but for the last N, have landed.  (A
+// barrier alone promises neither, and __syncthreads() would wait for the last N as well.)
+template <int N>
+__device__ __forceinline__ void meet_but() {
+    static_assert(N < 64, "six bits");
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");  // no instruction: keeps memory operations on their side
+    __builtin_amdgcn_s_waitcnt(0x0070 | (N & 15) | (N >> 4) << 14);  // vmcnt(N), lgkmcnt(0)
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
 
 // A workgroup computes TN columns by TR rows of y with PN x PR waves.  A stage of LDS holds one block of k of both
-// operands; two stages alternate, and while one multiplies, the next is on its way from memory straight into the other
-// (16 bytes a lane, no registers).  The two stages are two arrays, and the loop is unrolled over them: the compiler then
-// sees that fragment reads do not touch the stage in flight and does not wait for it.  A row of a stage is 128 bytes,
-// eight chunks; position p of row i holds chunk p ^ (i / 2 % 8), which spreads the sixteen rows a fragment read touches
-// over all banks.
+// operands; S stages go round, and while one multiplies, the others are on their way from memory straight into LDS (16 bytes
+// a lane, no registers).  A step cannot be shorter than a copy takes divided by the S - 1 blocks in flight: with two stages
+// and one workgroup a compute unit it took 0.8 us whatever the tile (64 x 4096 x 14336, tiles of 64 x 64: 94.5 us with two
+// stages, 50.7 with three, 39.5 with four), so the small tiles have three stages.  The large ones have two, which fill LDS,
+// and are long enough by themselves.  The stages are separate arrays, and the loop is unrolled over them: the compiler
+// then sees that fragment reads do not touch the stages in flight and does not wait for them.  A row of a stage is 128
+// bytes, eight chunks; position p of row i holds chunk p ^ (i / 2 % 8), which spreads the sixteen rows a fragment read
+// touches over all banks.
 // F16: the fragments are turned into fp16 (exact sums), otherwise multiplied as e4m3.
-template <typename OT, bool F16, int TN, int TR, int PN, int PR>
+template <typename OT, bool F16, int TN, int TR, int PN, int PR, int S>
 __global__ __launch_bounds__(64 * PN * PR, 2) void f8_tile_k(const F8Args a, const int n_tiles, const int r_tiles, const int shares) {
     constexpr int NT = 64 * PN * PR, WN = TN / PN / 16, WR = TR / PR / 16;
     constexpr int LW = TN * 8 / NT, LX = TR * 8 / NT;  // 16-byte chunks a thread moves per stage
     constexpr int LAG = 2;                             // matrix instructions between a tile's own and its additions
-    __shared__ __attribute__((aligned(16))) uint8_t stage0[(TN + TR) * F8_BLOCK];
-    __shared__ __attribute__((aligned(16))) uint8_t stage1[(TN + TR) * F8_BLOCK];
+    static_assert(S == 2 || S == 3, "");
+    constexpr int SCALES = (TN + TR) * F8_BLOCK, SIZE = SCALES + (S > 2 ? TR * 4 : 0);  // a stage's scales of x, its size
+    __shared__ __attribute__((aligned(16))) uint8_t stage0[SIZE];
+    __shared__ __attribute__((aligned(16))) uint8_t stage1[SIZE];
+    __shared__ __attribute__((aligned(16))) uint8_t stage2[SIZE];  // takes LDS only where it is used
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int sub = lane & 15, g = lane >> 4;
     const int wn = wave % PN, wr = wave / PN;
@@ -380,14 +404,35 @@ __global__ __launch_bounds__(64 * PN * PR, 2) void f8_tile_k(const F8Args a, con
 #pragma unroll
         for (int j = 0; j < WR; ++j) acc[i][j] = f4_t{0.f, 0.f, 0.f, 0.f};
     const float *wsp = a.ws + (int64_t)(min(n0 + wn * WN * 16, a.N - 1) / F8_BLOCK) * a.KB + b_share;
-    float xs[WR], ws;
-    auto scales = [&](int b) {
-        const char *p = reinterpret_cast<const char *>(a.xs + (int64_t)(b_share + b) * a.R + r0);
-        int own = wr * WR * 16 + sub;
-        asm volatile("" : "+v"(own));
+    // Scales of a block.  Two stages: loads into registers, a step ahead.  More: those of x go into the stage as well, one copy
+    // a wave (64 rows; waves beyond the rows repeat them), so that the copies in flight can be counted, and that of w is a
+    // scalar load.
+    float xs[WR], ws = 0.f;
+    auto load_scales = [&](int b, uint8_t *stage) {
+        if constexpr (S == 2) {
+            const char *p = reinterpret_cast<const char *>(a.xs + (int64_t)(b_share + b) * a.R + r0);
+            int own = wr * WR * 16 + sub;
+            asm volatile("" : "+v"(own));
 #pragma unroll
-        for (int j = 0; j < WR; ++j) xs[j] = *reinterpret_cast<const float *>(p + (uint32_t)min(own + j * 16, last_r) * 4);
-        ws = wsp[b];
+            for (int j = 0; j < WR; ++j) xs[j] = *reinterpret_cast<const float *>(p + (uint32_t)min(own + j * 16, last_r) * 4);
+            ws = wsp[b];
+        } else {
+            static_assert(TR % 64 == 0 && TR <= NT, "");
+            const __amdgpu_buffer_rsrc_t buf = __builtin_amdgcn_make_buffer_rsrc(
+                const_cast<float *>(a.xs + (int64_t)(b_share + b) * a.R + r0), 0, (min(TR - 1, last_r) + 1) * 4, 0x27000);
+            const int first = wave * 64 % TR;
+            int own = first + lane;
+            asm volatile("" : "+v"(own));
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(buf, (__attribute__((address_space(3))) void *)(stage + SCALES + first * 4), 4,
+                                                     min(own, last_r) * 4, 0, 0, 0);
+        }
+    };
+    auto take_scales = [&](int b, const uint8_t *stage) {
+        if constexpr (S > 2) {
+#pragma unroll
+            for (int j = 0; j < WR; ++j) xs[j] = *reinterpret_cast<const float *>(stage + SCALES + (wr * WR * 16 + j * 16 + sub) * 4);
+            ws = *(const __attribute__((address_space(4))) float *)(uintptr_t)(wsp + b);
+        }
     };
     const int f0 = sub * F8_BLOCK + ((g ^ (sub >> 1)) * 16), f1 = f0 ^ 64;
     auto frag = [&](const uint8_t *p, u4_t &c0, u4_t &c1) {
@@ -416,30 +461,30 @@ __global__ __launch_bounds__(64 * PN * PR, 2) void f8_tile_k(const F8Args a, con
     const int lw = wn * WN * 16 * F8_BLOCK, lx = (TN + wr * WR * 16) * F8_BLOCK;
     u4_t x0[WR], x1[WR], w0[2], w1[2];
     h8_t hx[F16 ? WR : 1][4], hw[2][4];  // fp16 fragments
-    // Step b multiplies the stage `cur` while block b + 1 is copied into `nxt`, CPR copies a row of tiles (all at once they
-    // would hold up the matrix instructions behind them).  Fragments are read a row of tiles ahead; in front of the last
-    // row, whose fragments are in registers by then, the workgroup meets: `nxt` is complete and nobody reads `cur` any
-    // more, and the first fragments of `nxt` are read behind the last row's instructions.
+    // Step b multiplies the stage `cur` while block b + S - 1 is copied into `far` (the stage of step b - 1), CPR copies a row of
+    // tiles (all at once they would hold up the matrix instructions behind them).  Fragments are read a row of tiles ahead;
+    // in front of the last row, whose fragments are in registers by then, the workgroup meets: `nxt` is complete and nobody
+    // reads `cur` any more, and the first fragments of `nxt` are read behind the last row's instructions.
+    // `more`: there is a block b + 1; `load`: there is a block b + S - 1.
     // Matrix and vector instructions of a wave alternate (left alone, the scheduler groups them, and each unit waits for
     // the other): a tile's additions follow matrix instructions issued after its own.
     constexpr int CPR = (LW + LX + WN / 2 - 1) / (WN / 2);
-    float sc[WR], nsc[WR];  // scales of this step and of the one to come
+    constexpr int FLIGHT = (S - 2) * (LW + LX + 1);  // copies younger than those of block b + 1 when step b meets
+    float sc[WR];           // scales of this step
     f4_t t[4];              // the last results; those of a step's last tiles are added in the next one
 #pragma unroll
     for (int u = 0; u < 4; ++u) t[u] = f4_t{0.f, 0.f, 0.f, 0.f};
-    auto step = [&](int b, uint8_t *cur, uint8_t *nxt, auto more) {
+    auto step = [&](int b, uint8_t *cur, uint8_t *nxt, uint8_t *far, auto more, auto load) __attribute__((always_inline)) {
         float old[LAG];
 #pragma unroll
         for (int q = 0; q < LAG; ++q) old[q] = sc[WR - LAG + q];
 #pragma unroll
-        for (int j = 0; j < WR; ++j) sc[j] = nsc[j];
+        for (int j = 0; j < WR; ++j) sc[j] = xs[j] * ws;
         auto meet = [&] {
-            copies_done();
-            __syncthreads();
+            meet_but<load ? FLIGHT : 0>();
             trim(b + 1, nxt);
             frag(nxt + lw, w0[0], w1[0]);
-#pragma unroll
-            for (int q = 0; q < WR; ++q) nsc[q] = xs[q] * ws;
+            take_scales(b + 1, nxt);
         };
         if constexpr (F16) {
 #pragma unroll
@@ -456,7 +501,9 @@ __global__ __launch_bounds__(64 * PN * PR, 2) void f8_tile_k(const F8Args a, con
 #pragma unroll
                         for (int j = 0; j < WR; ++j) frag(nxt + lx + j * 16 * F8_BLOCK, x0[j], x1[j]);
                     }
-                    if (jp == 0 && i == WN / 2 - 1) scales(b + 1);
+                }
+                if constexpr (load) {
+                    if (jp == 0 && i == WN / 2 - 1) load_scales(b + S - 1, far);
                 }
                 __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
@@ -465,9 +512,9 @@ __global__ __launch_bounds__(64 * PN * PR, 2) void f8_tile_k(const F8Args a, con
                     const f4_t z = {0.f, 0.f, 0.f, 0.f};
                     t[u & 3] = __builtin_amdgcn_mfma_f32_16x16x32_f16(hw[i & 1][q], hx[j][q], q == 0 ? z : t[u & 3], 0, 0, 0);
                     __builtin_amdgcn_sched_barrier(0);
-                    if constexpr (more) {
+                    if constexpr (load) {
                         const int k = i * CPR + jp * 8 + v;
-                        if (jp * 8 + v < CPR && i < WN / 2 && k < LW + LX) copy(b + 1, k, nxt);
+                        if (jp * 8 + v < CPR && i < WN / 2 && k < LW + LX) copy(b + S - 1, k, far);
                     }
                     const int d = u - 2;  // the pair before, one element of each tile at a time
                     if (d >= 0) add1(d / WR, d % WR, q, t[d & 3], sc[d % WR]);
@@ -483,18 +530,22 @@ __global__ __launch_bounds__(64 * PN * PR, 2) void f8_tile_k(const F8Args a, con
                 if (j == 0 && i + 1 < WN) frag(cur + lw + (i + 1) * 16 * F8_BLOCK, w0[(i + 1) & 1], w1[(i + 1) & 1]);
                 if constexpr (more) {
                     if (j == 0 && i + 1 == WN) meet();
-                    if (j == 0 && i == WN / 2 - 1) scales(b + 1);
+                }
+                if constexpr (load) {
+                    if (j == 0 && i == WN / 2 - 1) load_scales(b + S - 1, far);
                 }
                 __builtin_amdgcn_sched_barrier(0);
                 t[u & 3] = mfma_f8(w0[i & 1], w1[i & 1], x0[j], x1[j]);
                 __builtin_amdgcn_sched_barrier(0);
                 if constexpr (more) {
                     if (i + 1 == WN) frag(nxt + lx + j * 16 * F8_BLOCK, x0[j], x1[j]);
-                    if (j % (WR / 2) == 0) {
+                }
+                if constexpr (load) {
+                    if (j % (WR / 2) == 0 && i < WN / 2) {
 #pragma unroll
                         for (int q = 0; q < (CPR + 1) / 2; ++q) {
                             const int k = i * CPR + j / (WR / 2) * ((CPR + 1) / 2) + q;
-                            if (k < (i + 1) * CPR && k < LW + LX) copy(b + 1, k, nxt);
+                            if (k < (i + 1) * CPR && k < LW + LX) copy(b + S - 1, k, far);
                         }
                     }
                 }
@@ -505,31 +556,51 @@ __global__ __launch_bounds__(64 * PN * PR, 2) void f8_tile_k(const F8Args a, con
         }
     };
     static_assert(WN % 2 == 0 && WR % 2 == 0 && WN * WR % 4 == 0 && WR >= LAG, "the fragments of w alternate over whole steps");
+    auto stage = [&](auto n) -> uint8_t * {
+        constexpr int i = n % S;
+        if constexpr (i == 0) return stage0;
+        else if constexpr (i == 1) return stage1;
+        else return stage2;
+    };
+    // the first S - 1 blocks (a short product's last one over and over)
+    each<S - 1>([&](auto n) {
+        const int b = min((int)n, KB - 1);
 #pragma unroll
-    for (int i = 0; i < LW + LX; ++i) copy(0, i, stage0);
-    scales(0);
-    copies_done();
-    __syncthreads();
+        for (int i = 0; i < LW + LX; ++i) copy(b, i, stage(n));
+        load_scales(b, stage(n));
+    });
+    meet_but<FLIGHT>();
     trim(0, stage0);
 #pragma unroll
-    for (int j = 0; j < WR; ++j) { nsc[j] = xs[j] * ws; sc[j] = 0.f; }
+    for (int j = 0; j < WR; ++j) sc[j] = 0.f;
     frag(stage0 + lw, w0[0], w1[0]);
+    take_scales(0, stage0);
 #pragma unroll
     for (int j = 0; j < WR; ++j) frag(stage0 + lx + j * 16 * F8_BLOCK, x0[j], x1[j]);
     if constexpr (F16) widen(w0[0], w1[0], hw[0]);
     const std::true_type yes;
     const std::false_type no;
     int b = 0;
-    for (; b + 2 < KB; b += 2) {
-        step(b, stage0, stage1, yes);
-        step(b + 1, stage1, stage0, yes);
-    }
-    if (b + 1 < KB) {
-        step(b, stage0, stage1, yes);
-        step(b + 1, stage1, stage0, no);
-    } else {
-        step(b, stage0, stage1, no);
-    }
+    // rounds over the stages while every step has a block to load, then up to 2 S - 2 steps that may have none
+    for (; b + 2 * S - 2 < KB; b += S)
+        each<S>([&](auto n) { step(b + n, stage(n), stage(num<n + 1>()), stage(num<n + S - 1>()), yes, yes); });
+    auto rest = [&](auto self, auto n) __attribute__((always_inline)) {
+        if constexpr (n + 1 < 2 * S - 2) {
+            if (b + n + 1 < KB) {
+                uint8_t *const cur = stage(n), *const nxt = stage(num<n + 1>()), *const far = stage(num<n + S - 1>());
+                if constexpr (n < S - 1) {
+                    if (S == 2 || b + n + S - 1 < KB) step(b + n, cur, nxt, far, yes, yes);
+                    else step(b + n, cur, nxt, far, yes, no);
+                } else {
+                    step(b + n, cur, nxt, far, yes, no);
+                }
+                self(self, num<n + 1>());
+                return;
+            }
+        }
+        step(b + n, stage(n), nullptr, nullptr, no, no);
+    };
+    rest(rest, num<0>());
 #pragma unroll
     for (int q = 0; q < LAG; ++q) add(WN - 1, WR - LAG + q, t[(q - LAG) & 3], sc[WR - LAG + q]);
     OT *y = reinterpret_cast<OT *>(a.y) + (int64_t)share * a.R * a.ldy;  // several shares: slabs of partial sums
@@ -566,21 +637,21 @@ __global__ __launch_bounds__(256) void f8_sum_k(const float *__restrict__ part, 
     store_y4(y + (int64_t)r * ldy, v, n, N, aligned);
 }
 
-template <typename OT, bool F16, int TN, int TR, int PN, int PR>
+template <typename OT, bool F16, int TN, int TR, int PN, int PR, int S>
 static hipError_t launch_tile(const F8Args &a, hipStream_t s, int shares = 1) {
     const int64_t n_tiles = (a.N + TN - 1) / TN, r_tiles = (a.R + TR - 1) / TR, total = n_tiles * r_tiles * shares;
     if (total > 1 << 30) return hipErrorInvalidValue;  // beyond any memory: N and R are at most 2^30 each
-    hipLaunchKernelGGL((f8_tile_k<OT, F16, TN, TR, PN, PR>), grid_of((total + 7) / 8 * 8), dim3(64 * PN * PR), 0, s, a, (int)n_tiles,
+    hipLaunchKernelGGL((f8_tile_k<OT, F16, TN, TR, PN, PR, S>), grid_of((total + 7) / 8 * 8), dim3(64 * PN * PR), 0, s, a, (int)n_tiles,
                        (int)r_tiles, shares);
     return hipGetLastError();
 }
 
-template <typename OT, bool F16, int TN, int TR, int PN, int PR>
+template <typename OT, bool F16, int TN, int TR, int PN, int PR, int S>
 static hipError_t launch_shared(const F8Args &a, int shares, hipStream_t s) {
-    if (shares == 1) return launch_tile<OT, F16, TN, TR, PN, PR>(a, s);
+    if (shares == 1) return launch_tile<OT, F16, TN, TR, PN, PR, S>(a, s);
     F8Args p = a;  // partial sums: [shares][R][N]
     p.y = a.part; p.ldy = a.N;
-    const hipError_t e = launch_tile<float, F16, TN, TR, PN, PR>(p, s, shares);
+    const hipError_t e = launch_tile<float, F16, TN, TR, PN, PR, S>(p, s, shares);
     if (e != hipSuccess) return e;
     const int64_t items = (int64_t)a.R * ((a.N + 3) / 4);  // few tiles share: far below 2^32
     hipLaunchKernelGGL((f8_sum_k<OT>), dim3((unsigned)((items + 255) / 256)), dim3(256), 0, s, a.part, shares, a.R, a.N,
@@ -601,12 +672,15 @@ bool gemm_f8_takes_wide(const F8Args &a) {
            a.ldx * size % 16 == 0;
 }
 
-// Shares of K for a grid of `tiles` tiles that should be `wanted` workgroups: at most eight, eight blocks of k each, and the
-// partial sums have to fit the scratch.
-static int pick_shares(const F8Args &a, int64_t tiles, int64_t wanted) {
+// Shares of K for a grid of `tiles` tiles: one workgroup a compute unit, and two where that leaves each more than sixteen
+// blocks of k (137 x 4096 x 11008, 96 tiles: 44.6 / 28.7 / 24.7 / 28.7 with 1 / 2 / 5 / 8; 256 x 2048 x 8192, 64 tiles: 33.3 / 16.0 / 17.8
+// with 1 / 4 / 8; 192 x 8192 x 2048, 192 tiles: 12.3 / 15.4 with 1 / 2).  At most eight, eight blocks each, and the partial sums
+// have to fit the scratch.
+static int64_t pick_shares(const F8Args &a, int64_t tiles) {
     const int64_t slab = (int64_t)a.R * a.N * 4;
     const int64_t fit = a.part == nullptr ? 1 : a.part_bytes / slab;
-    return (int)std::max<int64_t>(1, std::min({wanted / tiles, (int64_t)8, (int64_t)a.KB / 8, fit}));
+    const int64_t two = std::min<int64_t>(8, 512 / tiles), n = a.KB > 16 * two ? two : 256 / tiles;
+    return std::max<int64_t>(1, std::min({n, (int64_t)8, (int64_t)a.KB / 8, fit}));
 }
 
 // The stream with 16 RB rows a workgroup: 16, 32 or 64 columns, the fewest that need no more than one workgroup a compute
@@ -629,39 +703,43 @@ static hipError_t launch_columns(const F8Args &a, hipStream_t s) {
 static int64_t stream_row_tiles(const F8Args &a) { return (a.R + 63) / 64; }
 static bool tiles_of_48(const F8Args &a) { return (a.R + 47) / 48 == stream_row_tiles(a); }
 
-// Whether more than 32 rows go through the stream: for short rows, where the tiles' steps are few and their latency shows,
-// as long as workgroups of 64 columns fit the compute units or (48 rows, fp32: 64 rows) w is read once.  Stream against tiles, fp32 /
-// bf16 results: 40 x 2048 x 2048 6.5 / 6.4 against 11.0 / 9.7, 48 x 28672 x 4096 32.9 / 32.9 against 49.4 / 35.9, 64 x 28672 x 4096
-// 38.4 / 38.4 against 50.0 / 36.4, 128 x 4096 x 4096 15.8 / 15.4 against 18.5 / 16.4, 256 x 4096 x 2048 12.9 / 12.2 against 18.4 /
-// 15.9; but 40 x 2048 x 8192 16.8 / 16.5 against 15.8 / 14.1, 40 x 6144 x 6144 17.7 / 17.3 against 18.9 / 16.5, 192 x 8192 x 2048
-// 22.3 / 21.6 against 20.4 / 15.3.
-template <typename OT>
-static bool streams(const F8Args &a) {
-    constexpr bool exact = sizeof(OT) == 4;  // the tiles of fp32 results multiply at half the rate
-    if (a.KB > (exact ? 44 : 32)) return false;
-    return a.R <= (exact ? 64 : 48) || ((int64_t)a.N + 63) / 64 * stream_row_tiles(a) <= 256;
+// Whether the stream takes the product: up to 16 rows always; more where the tiles would need longer, 0.37 a block of k a
+// share and 6 to start and to join the shares against 0.22 a block of k, as long as (more than 32 rows) workgroups of 32
+// columns fit the compute units.  Stream against tiles, fp32 / bf16 results: 24 x 4096 x 14336 22.1 against 19.4 / 17.5, 32 x 14336 x
+// 4096 15.9 against 19 / 17, 40 x 4096 x 4096 10.1 against 12.8 / 11.4, 40 x 2048 x 8192 16.2 against 14.1 / 12.8, 128 x 2048 x 2048 7.7 against
+// 11.2 / 9.6, 64 x 4096 x 14336 35.2 against 20.1 / 19.0 with eight shares and 74.2 / 60.3 with one, 48 x 28672 x 4096 32.6 against 31.1 / 29.1.
+static bool streams(const F8Args &a, int64_t shares) {
+    if (a.R <= 16) return true;
+    if (a.R > 32 && ((int64_t)a.N + 31) / 32 * stream_row_tiles(a) > 256) return false;
+    return 37 * (int64_t)a.KB / shares + 600 > 22 * (int64_t)a.KB;
 }
 
 template <typename OT>
 static hipError_t launch_gemm_f8_t(const F8Args &a, hipStream_t s) {
     if (a.x_type == X_F32) return launch_columns<OT, 1, X_F32>(a, s);
     if (a.x_type == X_BF16) return launch_columns<OT, 1, X_BF16>(a, s);
-    if (a.R <= 16) return launch_columns<OT, 1, X_F8>(a, s);
-    if (a.R <= 32) return launch_columns<OT, 2, X_F8>(a, s);
-    if (streams<OT>(a)) return tiles_of_48(a) ? launch_columns<OT, 3, X_F8>(a, s) : launch_columns<OT, 4, X_F8>(a, s);
     auto tiles = [&](int64_t tn, int64_t tr) { return (a.N + tn - 1) / tn * ((a.R + tr - 1) / tr); };
-    // A tile's time is its steps times a latency that the workgroups sharing a compute unit hide, so a product with few
-    // tiles takes smaller ones and shares K out (137 x 4096 x 11008: 64 with one share of 64 x 64 tiles, 29 with four).
-    constexpr bool F16 = sizeof(OT) == 4;
-    if constexpr (F16) {
-        const int64_t t = tiles(128, 128);  // 512 x 6144 x 4096: 45 with two shares, 48 with 64 x 64 tiles
-        if (t >= 128) return launch_shared<OT, true, 128, 128, 2, 2>(a, pick_shares(a, t, 384), s);
-    } else {
-        // 512 x 28672 x 4096: 77 / 92 / 111 / 126 with 256 x 256 / 128 x 128 / 128 x 64 / 64 x 64; 1024 x 6144 x 4096: 65 / 46 / 45 / 60
-        if (tiles(256, 256) >= 192) return launch_tile<OT, false, 256, 256, 2, 4>(a, s);
-        if (tiles(128, 64) >= 384) return launch_tile<OT, false, 128, 64, 4, 1>(a, s);
+    const int64_t shares = pick_shares(a, tiles(128, 64));
+    if (streams(a, shares)) {
+        if (a.R <= 16) return launch_columns<OT, 1, X_F8>(a, s);
+        if (a.R <= 32) return launch_columns<OT, 2, X_F8>(a, s);
+        return tiles_of_48(a) ? launch_columns<OT, 3, X_F8>(a, s) : launch_columns<OT, 4, X_F8>(a, s);
     }
-    return launch_shared<OT, F16, 64, 64, 2, 2>(a, pick_shares(a, tiles(64, 64), 768), s);
+    // Large tiles read each operand less often, but a round of them over the chip leaves more of it idle when it is not full:
+    // they are taken from two rounds on, or for one that fills.
+    auto fills = [](int64_t t, int64_t round, int64_t idle) { return t >= 2 * round || (round - t % round) % round <= idle; };
+    if constexpr (sizeof(OT) == 4) {
+        // tiles of 128 x 128 (two a compute unit) against 128 x 64: 4096 x 28672 x 4096 895 against 1047, 1300 x 14336 x 4096 164 against 184,
+        // 4096 x 2048 x 8192 (512 tiles) 129 against 151, 1024 x 6144 x 4096 (384) 66 against 63
+        if (fills(tiles(128, 128), 512, 64)) return launch_tile<OT, true, 128, 128, 2, 2, 2>(a, s);
+        return launch_shared<OT, true, 128, 64, 2, 2, 3>(a, (int)shares, s);
+    } else {
+        // tiles of 256 x 256 (one) against 128 x 64: 4096 x 28672 x 4096 464 against 715, 4096 x 6144 x 4096 (384 tiles) 123 against 156,
+        // 3000 x 6144 x 4096 (288) 114 against 105, 1500 x 6144 x 4096 (144) 61 against 65, 2048 x 4096 x 4096 (128) 58 against 56
+        const int64_t t = tiles(256, 256);
+        if (t > 128 && fills(t, 256, 128)) return launch_tile<OT, false, 256, 256, 2, 4, 2>(a, s);
+        return launch_shared<OT, false, 128, 64, 2, 2, 3>(a, (int)shares, s);
+    }
 }
 
 hipError_t launch_gemm_f8(const F8Args &a, hipStream_t s) {

@@ -286,7 +286,7 @@ def test_product_launch_shapes(R, N, K, y_dtype):
 
 STREAMED = [(9, 4100, 2064), (16, 8200, 272), (5, 70, 4496), (1, 16, 2176), (13, 33, 16), (30, 500, 1168), (30, 4200, 400), (31, 8300, 272),
             (47, 300, 1296), (90, 2100, 400), (40, 9000, 144), (60, 300, 2064), (120, 2200, 272), (60, 8300, 144), (200, 130, 4096)]
-TILED = [(700, 6200, 400), (140, 700, 6016), (260, 2500, 5776), (520, 4000, 5776)]
+TILED = [(700, 6200, 400), (140, 700, 6016), (260, 2500, 5776), (520, 4000, 5776), (24, 1000, 14336), (4100, 4100, 144), (4100, 4100, 16)]
 
 
 @pytest.mark.parametrize("y_dtype", [F32, BF16])
@@ -295,6 +295,26 @@ def test_product_more_launch_shapes(R, N, K, y_dtype):
     """One, two and four groups of columns by one to four of rows in the stream, with blocks of k that do not divide among
     its waves; and the tiles, whole and in shares."""
     test_product_launch_shapes(R, N, K, y_dtype)
+
+
+@pytest.mark.parametrize("y_dtype", [F32, BF16])
+@pytest.mark.parametrize("R,N", [(70, 8300), (1030, 12300)])
+@pytest.mark.parametrize("K", [16, 128, 240, 384, 512, 656, 784, 1024, 1040])
+def test_product_few_blocks_in_tiles(R, N, K, y_dtype):
+    """One to nine blocks of k in stages that go round, small tiles and large."""
+    test_product_launch_shapes(R, N, K, y_dtype)
+
+
+@pytest.mark.parametrize("R,N,K", [(24, 1000, 14336), (64, 300, 8192), (200, 700, 6016)])
+def test_product_without_scratch(R, N, K):
+    """Sizes that would share K out, without the scratch to do so."""
+    rng = np.random.default_rng(K)
+    w, ws = _weights(rng, N, K)
+    q, xs = ref.quantise(_activations(rng, R, K, F32).numpy())
+    y = torch.zeros((R, N), device="cuda")
+    pk.k_gemm_f8(_f8(w), torch.from_numpy(ws).cuda(), _f8(q), y, x_scale=torch.from_numpy(xs).cuda(), stream=_stream())
+    want, mag = ref.product(q, xs, w, ws)
+    assert (np.abs(y.double().cpu().numpy() - want) <= _product_tol(mag, want, ref.blocks(K), F32)).all()
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
