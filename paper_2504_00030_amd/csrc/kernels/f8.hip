@@ -99,7 +99,8 @@ __device__ __forceinline__ void each(F f) {
 
 // ---- quantiser -------------------------------------------------------------------------------------------------
 // Sixteen lanes per block of 128 columns, eight columns each: x is read once, and the block's largest is four shuffles
-// away.  VEC: the rows start on 16 bytes, so that the eight columns are one or two loads.
+// away.  VEC: the rows start on 16 bytes, so that the eight columns are one or two loads.  Bound by memory (4096 x 14336 bf16:
+// 35 us, 5.0 TB/s read and written) or, for few rows, by the launch (9 x 5120 fp32: 2.5 us).
 template <typename T, bool VEC>
 __global__ __launch_bounds__(256) void quant_f8_k(const T *__restrict__ x, int64_t ldx, int R, int K, int KB,
                                                   uint8_t *__restrict__ q, float *__restrict__ scale) {
@@ -157,8 +158,10 @@ hipError_t launch_quant_f8(const void *x, int dtype, int64_t ldx, int R, int K, 
 
 // ---- product: the waves of a workgroup share K ------------------------------------------------------------------
 // A workgroup computes 16 NG columns by 16 RB rows of y.  Its NW waves take the blocks of k in turn, each with fragments
-// of its own straight from memory (w passes each compute unit once and needs no LDS), and their sums meet in LDS in a
+// of its own straight from memory (no wave needs another's, so there is no LDS to fill), and their sums meet in LDS in a
 // fixed order.  The e4m3 values enter v_mfma_f32_16x16x32_f16 as fp16, which holds every one of them.
+// Bound by the stream of w from memory where w is large (1 x 28672 x 4096: 24.6 us, 4.8 TB/s; 9 x 5120 x 13824: 18 us, 3.9 TB/s;
+// 9 x 4096 x 14336: 13.8 us, 4.3 TB/s), by the latency of each wave's few loads where it is small (1 x 2048 x 2048: 3.8 us).
 // XIN: type of x: SPEC_F8's bytes with their scales, or fp32 / bf16 rows, which every wave quantises for itself (the
 // fragment of one block is 32 values in each of four lanes, so the block's largest is two shuffles away).
 enum { X_F8 = 0, X_F32 = 1, X_BF16 = 2 };
@@ -353,6 +356,11 @@ __device__ __forceinline__ void meet_but() {
 // bytes, eight chunks; position p of row i holds chunk p ^ (i / 2 % 8), which spreads the sixteen rows a fragment read
 // touches over all banks.
 // F16: the fragments are turned into fp16 (exact sums), otherwise multiplied as e4m3.
+// What bounds it: 4096 x 28672 x 4096 in tiles of 256 x 256 takes 464 - 480 us, 2.0 PFLOP/s, with the matrix units busy 53 % of the
+// cycles at a clock that the power limit holds at 1.8 GHz (zeros instead of data: 426 us); a library product of the same
+// operands without block scales takes 326 us.  With fp32 results 895 us, 1.1 PFLOP/s: half the rate, and the conversions.
+// Measured and not taken: four waves of 128 x 128 each (their accumulators do not fit the vector registers: 1020 us), copies
+// through registers (606), 32 x 32 x 64 instructions (spills: 578), all copies of a step at once (485), wave priorities (475).
 template <typename OT, bool F16, int TN, int TR, int PN, int PR, int S>
 __global__ __launch_bounds__(64 * PN * PR, 2) void f8_tile_k(const F8Args a, const int n_tiles, const int r_tiles, const int shares) {
     constexpr int NT = 64 * PN * PR, WN = TN / PN / 16, WR = TR / PR / 16;
@@ -663,8 +671,8 @@ static hipError_t launch_shared(const F8Args &a, int shares, hipStream_t s) {
 // Times below: fresh weights from HBM for every call, in microseconds, launches back to back.
 
 // Whether the product quantises fp32 / bf16 rows itself, in every workgroup anew, instead of by a launch of the quantiser
-// in front: for a few rows of a small matrix (both launches in a graph, fp32 rows: 1 x 2048 x 2048 5.4 against 5.9, 8 x 8192 x
-// 2048 7.9 against 8.3, 4 x 4096 x 4096 8.9 against 8.6, and a launch less for the host; but 1 x 4096 x 5632 10.6 against 9.1,
+// in front: for a few rows of a small matrix (both launches in a graph, fp32 rows: 1 x 2048 x 2048 4.8 against 5.9, 8 x 8192 x
+// 2048 7.9 against 8.3, 1 x 4096 x 4096 8.3 against 8.2, and a launch less for the host; but 1 x 4096 x 5632 10.6 against 9.1,
 // 1 x 2048 x 8192 12.4 against 9.8).
 bool gemm_f8_takes_wide(const F8Args &a) {
     const int64_t size = a.x_type == X_F32 ? 4 : 2;
@@ -687,13 +695,13 @@ static int64_t pick_shares(const F8Args &a, int64_t tiles) {
 // unit.  With more columns x is read less often, with fewer the chip fills sooner (16 / 32 / 64 columns: 9 x 4096 x 14336 13.8 /
 // 20 / -, 9 x 6144 x 4096 9.3 / 8.2 / -, 1 x 28672 x 4096 26.5 / 25.9 / 25.9, 32 x 4096 x 4096 8.2 / 9.7 / -, 32 x 6144 x 4096
 // 14.4 / 10.7 / -, 32 x 14336 x 4096 26.7 / 19.5 / 15.9).  Waves and stages: 9 x 4096 x 14336 13.8 with eight of two, 14.4 with
-// eight of one, 14.8 with sixteen of one; 64 x 4096 x 4096 12.9 with four waves, 13.3 with eight.
+// eight of one, 14.8 with sixteen of one (rows quantised here, 1 x 2048 x 2048: 5.4 with two stages, 4.8 with one); 64 x 4096 x 4096 12.9 with four waves, 13.3 with eight.
 template <typename OT, int RB, int XIN>
 static hipError_t launch_columns(const F8Args &a, hipStream_t s) {
     const int64_t r_tiles = (a.R + 16 * RB - 1) / (16 * RB), groups = (a.N + 15) / 16;
     constexpr int NW = RB == 4 ? 4 : 8;
-    if (groups * r_tiles <= 256) return launch_stream<OT, 1, RB, NW, RB == 1 ? 2 : 1, XIN>(a, s);
-    if constexpr (XIN == X_F8) {
+    if (groups * r_tiles <= 256) return launch_stream<OT, 1, RB, NW, RB == 1 && XIN == X_F8 ? 2 : 1, XIN>(a, s);
+    if constexpr (XIN == X_F8 && RB <= 2) {  // the others come with columns that fit
         if ((groups + 1) / 2 * r_tiles > 256) return launch_stream<OT, 4, RB, 4, 1, XIN>(a, s);
     }
     return launch_stream<OT, 2, RB, NW, 1, XIN>(a, s);
