@@ -670,14 +670,21 @@ static hipError_t launch_shared(const F8Args &a, int shares, hipStream_t s) {
 // ---- which kernel runs ---------------------------------------------------------------------------------------------
 // Times below: fresh weights from HBM for every call, in microseconds, launches back to back.
 
+// Tiles of rows the stream makes of more than 32: of 48 rows if they are no more than tiles of 64 would be.
+static int64_t stream_row_tiles(const F8Args &a) { return (a.R + 63) / 64; }
+static bool tiles_of_48(const F8Args &a) { return (a.R + 47) / 48 == stream_row_tiles(a); }
+
 // Whether the product quantises fp32 / bf16 rows itself, in every workgroup anew, instead of by a launch of the quantiser
-// in front: for a few rows of a small matrix (both launches in a graph, fp32 rows: 1 x 2048 x 2048 4.8 against 5.9, 8 x 8192 x
-// 2048 7.9 against 8.3, 1 x 4096 x 4096 8.3 against 8.2, and a launch less for the host; but 1 x 4096 x 5632 10.6 against 9.1,
-// 1 x 2048 x 8192 12.4 against 9.8).
+// in front: where that costs the GPU little, for it saves the host a launch (3 us).  Itself against both, in a graph, fp32
+// rows: 1 x 2048 x 2048 4.8 / 5.9, 1 x 4096 x 4096 8.3 / 8.2, 16 x 2048 x 2048 7.4 / 6.7, but 12 x 4096 x 4096 11.1 / 9.3, 1 x 2048 x 8192
+// 12.4 / 9.8; bf16: 16 x 4096 x 4096 9.2 / 9.5, 32 x 2048 x 2048 8.0 / 8.0, 200 x 512 x 1024 8.1 / 7.5, 4096 x 128 x 512 6.7 / 9.1, but 24 x 4096 x
+// 4096 13.4 / 11.0, 48 x 2048 x 2048 10.3 / 9.2.  Many columns make it too many times: 8 x 28672 x 512 9.9 / 8.1.
 bool gemm_f8_takes_wide(const F8Args &a) {
     const int64_t size = a.x_type == X_F32 ? 4 : 2;
-    return a.R <= 8 && a.K <= 4096 && a.N <= 8192 && (int64_t)a.N * a.K <= 4096 * 4096 && reinterpret_cast<uintptr_t>(a.x) % 16 == 0 &&
-           a.ldx * size % 16 == 0;
+    const int blocks = a.x_type == X_F32 ? (a.R <= 8 ? 32 : a.R <= 16 ? 16 : 0) : (a.R <= 16 ? 32 : a.R <= 32 ? 16 : 8);
+    return a.KB <= blocks && (int64_t)a.N * a.K <= 4096 * 4096 &&
+           (a.R <= 16 ? a.N <= 16384 : ((int64_t)a.N + 31) / 32 * stream_row_tiles(a) <= 256) &&
+           reinterpret_cast<uintptr_t>(a.x) % 16 == 0 && a.ldx * size % 16 == 0;
 }
 
 // Shares of K for a grid of `tiles` tiles: one workgroup a compute unit, and two where that leaves each more than sixteen
@@ -707,9 +714,16 @@ static hipError_t launch_columns(const F8Args &a, hipStream_t s) {
     return launch_stream<OT, 2, RB, NW, 1, XIN>(a, s);
 }
 
-// Tiles of rows the stream makes of more than 32: of 48 rows if they are no more than tiles of 64 would be.
-static int64_t stream_row_tiles(const F8Args &a) { return (a.R + 63) / 64; }
-static bool tiles_of_48(const F8Args &a) { return (a.R + 47) / 48 == stream_row_tiles(a); }
+template <typename OT, int XIN>
+static hipError_t launch_rows(const F8Args &a, hipStream_t s) {
+    if constexpr (XIN == X_F32) {
+        return launch_columns<OT, 1, XIN>(a, s);  // comes with no more rows
+    } else {
+        if (a.R <= 16) return launch_columns<OT, 1, XIN>(a, s);
+        if (a.R <= 32) return launch_columns<OT, 2, XIN>(a, s);
+        return tiles_of_48(a) ? launch_columns<OT, 3, XIN>(a, s) : launch_columns<OT, 4, XIN>(a, s);
+    }
+}
 
 // Whether the stream takes the product: up to 16 rows always; more where the tiles would need longer, 0.37 a block of k a
 // share and 6 to start and to join the shares against 0.22 a block of k, as long as (more than 32 rows) workgroups of 32
@@ -724,15 +738,11 @@ static bool streams(const F8Args &a, int64_t shares) {
 
 template <typename OT>
 static hipError_t launch_gemm_f8_t(const F8Args &a, hipStream_t s) {
-    if (a.x_type == X_F32) return launch_columns<OT, 1, X_F32>(a, s);
-    if (a.x_type == X_BF16) return launch_columns<OT, 1, X_BF16>(a, s);
+    if (a.x_type == X_F32) return launch_rows<OT, X_F32>(a, s);
+    if (a.x_type == X_BF16) return launch_rows<OT, X_BF16>(a, s);
     auto tiles = [&](int64_t tn, int64_t tr) { return (a.N + tn - 1) / tn * ((a.R + tr - 1) / tr); };
     const int64_t shares = pick_shares(a, tiles(128, 64));
-    if (streams(a, shares)) {
-        if (a.R <= 16) return launch_columns<OT, 1, X_F8>(a, s);
-        if (a.R <= 32) return launch_columns<OT, 2, X_F8>(a, s);
-        return tiles_of_48(a) ? launch_columns<OT, 3, X_F8>(a, s) : launch_columns<OT, 4, X_F8>(a, s);
-    }
+    if (streams(a, shares)) return launch_rows<OT, X_F8>(a, s);
     // Large tiles read each operand less often, but a round of them over the chip leaves more of it idle when it is not full:
     // they are taken from two rounds on, or for one that fills.
     auto fills = [](int64_t t, int64_t round, int64_t idle) { return t >= 2 * round || (round - t % round) % round <= idle; };

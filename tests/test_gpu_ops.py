@@ -318,7 +318,9 @@ def test_product_without_scratch(R, N, K):
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
-@pytest.mark.parametrize("R,N,K", [(8, 5000, 2000), (3, 8192, 2048), (2, 4097, 144), (8, 4096, 4096)])
+@pytest.mark.parametrize("R,N,K", [(8, 5000, 2000), (3, 8192, 2048), (2, 4097, 144), (8, 4096, 4096), (16, 2048, 2048), (14, 300, 4096),
+                                   (32, 2100, 1040), (25, 5000, 400), (48, 300, 1024), (60, 900, 912), (98, 131, 608), (300, 700, 272),
+                                   (1132, 99, 368), (120, 3000, 144)])
 def test_product_of_rows_equals_the_two_calls_in_wide_workgroups(R, N, K, dtype):
     test_product_of_rows_equals_quantiser_and_product(R, N, K, dtype)
 
