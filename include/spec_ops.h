@@ -40,6 +40,8 @@ int spec_k_quant_f8(const void *x, int32_t dtype, int64_t ldx, int32_t R, int32_
  * Sums are held in fp32.  With y_dtype SPEC_F32 the products enter them whole (error about 1e-7 of the result); with
  * SPEC_BF16 the matrix unit may sum eight neighbouring products at a time to 13 bits below the largest of them (about
  * 3e-5 of the result, against the 2e-3 of its rounding to bf16).
+ * The product of two scales is an fp32 number: where it leaves fp32's normal range, so does the precision (beyond 2^128
+ * the results are infinities or NaN).
  *  - x_dtype SPEC_F8: x e4m3 [R][K] (ldx == K), 16-byte aligned, with x_scale device fp32 [ceil(K / 128)][R], both as
  *    spec_k_quant_f8 leaves them.
  *  - x_dtype SPEC_F32 / SPEC_BF16: rows as for spec_k_quant_f8, quantised by the call by its rule; x_scale NULL.
