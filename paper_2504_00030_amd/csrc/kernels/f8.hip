@@ -756,6 +756,10 @@ static hipError_t launch_gemm_f8_t(const F8Args &a, hipStream_t s) {
         // 3000 x 6144 x 4096 (288) 114 against 105, 1500 x 6144 x 4096 (144) 61 against 65, 2048 x 4096 x 4096 (128) 58 against 56
         const int64_t t = tiles(256, 256);
         if (t > 128 && fills(t, 256, 128)) return launch_tile<OT, false, 256, 256, 2, 4, 2>(a, s);
+        // tiles of 128 x 128 (one) against 128 x 64: 500 x 6144 x 4096 (192 tiles) 26 against 29, 900 x 4096 x 11008 (256) 61 against 67,
+        // 1024 x 6144 x 4096 (384) 48 against 43; with shares of K neither wins by much (96 tiles: 27 / 31, 44 / 41)
+        const int64_t m = tiles(128, 128);
+        if (a.R > 64 && m > 128 && fills(m, 256, 64)) return launch_tile<OT, false, 128, 128, 4, 2, 3>(a, s);
         return launch_shared<OT, false, 128, 64, 2, 2, 3>(a, (int)shares, s);
     }
 }

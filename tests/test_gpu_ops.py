@@ -286,7 +286,8 @@ def test_product_launch_shapes(R, N, K, y_dtype):
 
 STREAMED = [(9, 4100, 2064), (16, 8200, 272), (5, 70, 4496), (1, 16, 2176), (13, 33, 16), (30, 500, 1168), (30, 4200, 400), (31, 8300, 272),
             (47, 300, 1296), (90, 2100, 400), (40, 9000, 144), (60, 300, 2064), (120, 2200, 272), (60, 8300, 144), (200, 130, 4096)]
-TILED = [(700, 6200, 400), (140, 700, 6016), (260, 2500, 5776), (520, 4000, 5776), (24, 1000, 14336), (4100, 4100, 144), (4100, 4100, 16)]
+TILED = [(700, 6200, 400), (140, 700, 6016), (260, 2500, 5776), (520, 4000, 5776), (24, 1000, 14336), (4100, 4100, 144), (4100, 4100, 16),
+         (500, 6100, 1040), (1000, 3970, 528), (99, 28600, 144)]
 
 
 @pytest.mark.parametrize("y_dtype", [F32, BF16])
