@@ -358,7 +358,9 @@ __device__ __forceinline__ void meet_but() {
 // F16: the fragments are turned into fp16 (exact sums), otherwise multiplied as e4m3.
 // What bounds it: 4096 x 28672 x 4096 in tiles of 256 x 256 takes 464 - 480 us, 2.0 PFLOP/s, with the matrix units busy 53 % of the
 // cycles at a clock that the power limit holds at 1.8 GHz (zeros instead of data: 426 us); a library product of the same
-// operands without block scales takes 326 us.  With fp32 results 895 us, 1.1 PFLOP/s: half the rate, and the conversions.
+// operands without block scales takes 326 us.  With fp32 results 895 us, 1.1 PFLOP/s: half the rate, and four
+// vector instructions (conversions, additions) for each matrix instruction, which share the issue with it: without three
+// quarters of the additions it would take 800 us, and the small tiles gained 3 % from offsets kept in registers.
 // Measured and not taken: four waves of 128 x 128 each (their accumulators do not fit the vector registers: 1020 us), copies
 // through registers (606), 32 x 32 x 64 instructions (spills: 578), all copies of a step at once (485), wave priorities (475).
 template <typename OT, bool F16, int TN, int TR, int PN, int PR, int S>
@@ -395,13 +397,24 @@ __global__ __launch_bounds__(64 * PN * PR, 2) void f8_tile_k(const F8Args a, con
     // the rows of this tile as buffers (a tile's rows span less than 2^31 bytes: the host bounds K)
     const __amdgpu_buffer_rsrc_t wbuf = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(wb), 0, min(TN - 1, last_n) * ld + K, 0x27000);
     const __amdgpu_buffer_rsrc_t xbuf = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(xb), 0, min(TR - 1, last_r) * ld + K, 0x27000);
+    uint32_t offset[LW + LX];  // of the rows of every copy; the large tiles have no registers for them and work them out anew
+    if constexpr (S > 2) {
+#pragma unroll
+        for (int i = 0; i < LW + LX; ++i)
+            offset[i] = __umul24(min(row + (i < LW ? i : i - LW) * (NT / 8), i < LW ? last_n : last_r), ld);
+    }
     auto copy = [&](int b, int i, uint8_t *stage) {  // 16 bytes a lane, 1 KiB of LDS a wave
         // a chunk past the end of the rows reads the block's first one; it is zeroed before the block is multiplied
         const uint32_t c = b * F8_BLOCK + chunk * 16 < K ? chunk * 16 : 0;
         const int ii = i < LW ? i : i - LW;
-        int own = row;
-        asm volatile("" : "+v"(own));  // no instruction: keeps the compiler from holding the offset of every copy in a register
-        const uint32_t o = __umul24(min(own + ii * (NT / 8), i < LW ? last_n : last_r), ld) + c;
+        uint32_t o;
+        if constexpr (S > 2) {
+            o = offset[i] + c;
+        } else {
+            int own = row;
+            asm volatile("" : "+v"(own));  // no instruction: keeps the compiler from holding the offset of every copy in a register
+            o = __umul24(min(own + ii * (NT / 8), i < LW ? last_n : last_r), ld) + c;
+        }
         uint8_t *to = stage + (i < LW ? 0 : TN * F8_BLOCK) + ii * NT * 16 + wave * 1024;
         __builtin_amdgcn_raw_ptr_buffer_load_lds(i < LW ? wbuf : xbuf, (__attribute__((address_space(3))) void *)to, 16, o,
                                                  b * F8_BLOCK, 0, 0);
