@@ -167,3 +167,13 @@ def test_norms_of_no_model_are_refused(model):
     with pytest.raises(pk.SpecError):
         eng.set_qk_norm(model, None, None)
     eng.close()
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("hd_target,hd_draft", [(256, 24), (512, 8), (136, 48)])
+def test_other_head_sizes(dtype, hd_target, hd_draft):
+    """Heads of 8 to 512 elements, whole lanes' worth and not, through the plain and the re-tiled projections."""
+    from synth.configs import ModelShape, PairConfig
+    target = ModelShape(2, 64, 2, 1, hd_target, 128, 512, 10000.0, 1e-5, dtype)
+    draft = ModelShape(2, 64, 4, 2, hd_draft, 128, 512, 10000.0, 1e-5, dtype)
+    _run(PairConfig("heads", target, draft, "independent", 40, 16, 8), n_generate=12, temperature=0.0, controller="fixed4")
