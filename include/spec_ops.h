@@ -37,18 +37,23 @@ int spec_k_quant_f8(const void *x, int32_t dtype, int64_t ldx, int32_t R, int32_
  * w: device e4m3 [N][K] row-major as a checkpoint holds it, 16-byte aligned; w_scale: device fp32 [ceil(N / 128)]
  * [ceil(K / 128)]; 1 <= N <= 2^30, 16 <= K <= 2^22, K % 16 == 0.  y: device, y_dtype SPEC_F32 or SPEC_BF16, row r at
  * element r * ldy (ldy >= N); columns N .. ldy - 1 are left alone.
- * Sums are held in fp32.  With y_dtype SPEC_F32 the products enter them whole (error about 1e-7 of the result); with
- * SPEC_BF16 the matrix unit may sum eight neighbouring products at a time to 13 bits below the largest of them (about
- * 3e-5 of the result, against the 2e-3 of its rounding to bf16).
+ * Sums are held in fp32.  With y_dtype SPEC_F32 the products enter them whole: a result is off by at most (131 + ceil(K / 128))
+ * 2^-23 of the sum of its terms' magnitudes, and for terms of either sign by about 1e-7 of its typical size (the root of
+ * the sum of the squared terms).  With SPEC_BF16 the matrix unit may sum eight neighbouring products at a time to 13 bits
+ * below the largest of them: at most 7 * 2^-13 of the sum of the magnitudes, typically 2e-5 to 3e-5 of a result's size (its
+ * rounding to bf16: 2e-3 of its value).  A caller who needs whole sums in bf16 takes SPEC_F32 results and rounds them.
+ * The same call gives the same bits every time.  How the sums are formed (their order and, for SPEC_BF16, which of them are
+ * whole) depends on R, N, K, the types, the alignment and stride of x and the size of the workspace, so a row's last bits
+ * may differ between calls that differ in these.
  * The product of two scales is an fp32 number: where it leaves fp32's normal range, so does the precision (beyond 2^128
  * the results are infinities or NaN).
  *  - x_dtype SPEC_F8: x e4m3 [R][K] (ldx == K), 16-byte aligned, with x_scale device fp32 [ceil(K / 128)][R], both as
  *    spec_k_quant_f8 leaves them.
  *  - x_dtype SPEC_F32 / SPEC_BF16: rows as for spec_k_quant_f8, quantised by the call by its rule; x_scale NULL.
  * workspace: device scratch, 16-byte aligned, of at least spec_k_gemm_f8_workspace() bytes (0: NULL will do).  More
- * lets products with few output columns share K out over workgroups: up to 32 MiB beyond that is put to use.  Contents
- * need no preparation and are overwritten; calls that may overlap (captured graphs replayed on two streams included)
- * need workspaces of their own.  SPEC_EINVAL when it is too small. */
+ * lets products with few output columns share K out over workgroups; from 32 MiB beyond that on, the result no longer
+ * depends on its size.  Contents need no preparation and are overwritten; calls that may overlap (captured graphs replayed
+ * on two streams included) need workspaces of their own.  SPEC_EINVAL when it is too small. */
 int spec_k_gemm_f8(const void *w, const float *w_scale, int32_t N, int32_t K, const void *x, int32_t x_dtype, int64_t ldx,
                    const float *x_scale, int32_t R, void *y, int32_t y_dtype, int64_t ldy, void *workspace,
                    int64_t workspace_bytes, void *stream);

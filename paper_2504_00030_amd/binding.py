@@ -600,7 +600,8 @@ def k_gemm_f8_workspace(K: int, R: int, x_dtype) -> int:
 def k_gemm_f8(w, w_scale, x, y, x_scale=None, workspace=None, stream: int = 0):
     """y [R][N] (fp32 or bf16, any row stride) = x . w^T with w e4m3 [N][K] and w_scale fp32 [ceil(N / 128)][ceil(K / 128)].
     x: e4m3 [R][K] with its x_scale as k_quant_f8 leaves them, or fp32 / bf16 rows, which the call quantises in
-    `workspace` (a GPU tensor of at least k_gemm_f8_workspace() bytes; more, up to 32 MiB, lets K be shared out)."""
+    `workspace` (a GPU tensor of at least k_gemm_f8_workspace() bytes; more, up to 32 MiB, lets K be shared out).  bf16
+    results may come from sums to 13 bits below the largest of eight products; fp32 results come from whole sums."""
     if not _KINDS:
         _setup()
     N, K = w.shape
