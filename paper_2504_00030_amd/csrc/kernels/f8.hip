@@ -605,23 +605,35 @@ __global__ __launch_bounds__(64 * PN * PR, 2) void f8_tile_k(const F8Args a, con
     // rounds over the stages while every step has a block to load, then up to 2 S - 2 steps that may have none
     for (; b + 2 * S - 2 < KB; b += S)
         each<S>([&](auto n) { step(b + n, stage(n), stage(num<n + 1>()), stage(num<n + S - 1>()), yes, yes); });
-    auto rest = [&](auto self, auto n) __attribute__((always_inline)) {
-        if constexpr (n + 1 < 2 * S - 2) {
-            if (b + n + 1 < KB) {
-                uint8_t *const cur = stage(n), *const nxt = stage(num<n + 1>()), *const far = stage(num<n + S - 1>());
-                if constexpr (n < S - 1) {
-                    if (S == 2 || b + n + S - 1 < KB) step(b + n, cur, nxt, far, yes, yes);
-                    else step(b + n, cur, nxt, far, yes, no);
-                } else {
-                    step(b + n, cur, nxt, far, yes, no);
-                }
-                self(self, num<n + 1>());
-                return;
-            }
+    if constexpr (S == 2) {
+        // One or two blocks are left.  Both ways share the last step, with its stage known only at run time: with a last step
+        // of its own for each, the accumulators met in different registers behind them, through scratch memory (4096 x 28672 x
+        // 4224, an odd number of blocks: 483 us, 559 that way; 128 x 128 tiles with fp32 results 951 and 980).
+        uint8_t *last = stage0;
+        if (b + 1 < KB) {
+            step(b++, stage0, stage1, stage1, yes, yes);
+            last = stage1;
         }
-        step(b + n, stage(n), nullptr, nullptr, no, no);
-    };
-    rest(rest, num<0>());
+        step(b, last, nullptr, nullptr, no, no);
+    } else {
+        auto rest = [&](auto self, auto n) __attribute__((always_inline)) {
+            if constexpr (n + 1 < 2 * S - 2) {
+                if (b + n + 1 < KB) {
+                    uint8_t *const cur = stage(n), *const nxt = stage(num<n + 1>()), *const far = stage(num<n + S - 1>());
+                    if constexpr (n < S - 1) {
+                        if (b + n + S - 1 < KB) step(b + n, cur, nxt, far, yes, yes);
+                        else step(b + n, cur, nxt, far, yes, no);
+                    } else {
+                        step(b + n, cur, nxt, far, yes, no);
+                    }
+                    self(self, num<n + 1>());
+                    return;
+                }
+            }
+            step(b + n, stage(n), nullptr, nullptr, no, no);
+        };
+        rest(rest, num<0>());
+    }
 #pragma unroll
     for (int q = 0; q < LAG; ++q) add(WN - 1, WR - LAG + q, t[(q - LAG) & 3], sc[WR - LAG + q]);
     OT *y = reinterpret_cast<OT *>(a.y) + (int64_t)share * a.R * a.ldy;  // several shares: slabs of partial sums
