@@ -56,9 +56,12 @@ int spec_debug_set_block_table(spec_ctx *ctx, const int32_t *table);
 
 /* Time kernel classes with HIP event pairs on the context's stream.  model: 0 draft, 1 target.
  * kind: 1 QKV projection, 2 output and down projection together, 3 gate/up projection with SwiGLU, 4 LM head,
- * 5 output projection, 6 down projection, 7 attention with the merge of its chunk partials; 0 times every class of
- * both models (model is then ignored); -1 switches timing off.  Projections are timed by the dispatch itself (kernel
- * start to kernel end), class 7 by events recorded on the stream around its two launches.  Only launches made outside
+ * 5 output projection, 6 down projection, 7 attention with the merge of its chunk partials, 8 norm and rotation of the
+ * heads with the writes of queries and cache (models with normed heads; the others do this within class 1, which for a
+ * model of the first sort is the projection alone: three launches where it does not run on the matrix cores); 0 times
+ * every class of both models (model is then ignored); -1 switches timing off.  Projections are timed by the dispatch
+ * itself (kernel start to kernel end) where they run on the matrix cores, everything else by events recorded on the
+ * stream around the class's launches.  Only launches made outside
  * captured graphs (use_graphs = 0) are timed.  spec_profile_read_class() waits for the stream and returns the number
  * of timed launches of one (model, kind) and the sum of their durations in milliseconds since the last
  * spec_profile_read(), which returns the same over everything timed and clears the record. */

@@ -1,7 +1,8 @@
 /*
  * Operators on caller buffers that a layer of a checkpoint with 8-bit floating point weights (e4m3, one scale per
  * 128 x 128 block) and normed query / key heads needs: the row quantiser, the product, and the heads' norm and
- * rotation.  The engine of spec.h runs the last one in its own layers after spec_set_qk_norm().
+ * rotation.  The layers of the engine of spec.h do the last one's arithmetic after spec_set_qk_norm(), in a kernel of
+ * their own that reads the projection's result and writes the queries and the cache; the first two they do not use.
  *
  * Same conventions as spec.h: 0 or a negative SPEC_E* code, the text of a failure from spec_last_error(NULL); "device"
  * pointers belong to the current device; work is enqueued on `stream` (a hipStream_t, NULL: the null stream), nothing

@@ -121,7 +121,8 @@ struct spec_ctx {
     std::vector<hipGraph_t> graphs;
     // optional timing of one kernel class with event pairs (direct launches only)
     // timed kernel class (-1: none, 0: every class of both models) and model; classes: 1 QKV, 2 output and down
-    // projection together, 3 gate/up, 4 LM head, 5 output projection, 6 down projection, 7 attention with its merge
+    // projection together, 3 gate/up, 4 LM head, 5 output projection, 6 down projection, 7 attention with its merge,
+    // 8 norm and rotation of heads
     int prof_epi = -1, prof_model = 0;
     std::vector<int> prof_tag;            // per event pair: 16 * model + class
     bool capturing = false;
@@ -585,6 +586,7 @@ int forward(spec_ctx *c, ModelRT &m, const RowPlan &plan, const LogitsPlan &lp, 
             n.q_norm = m.q_norm[l]; n.k_norm = m.k_norm[l]; n.eps = s.rms_eps;
             n.rope_cos = m.rope_cos; n.rope_sin = m.rope_sin; n.row_pos = m.row_pos; n.row_seq = m.row_seq;
             n.q = m.q; n.qb = m.qb; n.qb_lo = qb_lo; n.kv = kv_of(c, m, l); n.kv_dtype = s.dtype; n.active = active;
+            ProfScope ps_(c, m, 8, false);
             HIPCHK(c, launch_qkv_norm(n, st));
         }
         {
@@ -1548,7 +1550,7 @@ int spec_debug_write_kv(spec_ctx *c, int32_t model, int32_t layer, int32_t seq, 
 int spec_profile_kernel(spec_ctx *c, int32_t model, int32_t kind) {
     if (!c) return SPEC_EINVAL;
     if (model != 0 && model != 1) return fail(c, SPEC_EINVAL, "profile: model must be 0 (draft) or 1 (target)");
-    if (kind < -1 || kind > 7) return fail(c, SPEC_EINVAL, "profile: unknown kernel class");
+    if (kind < -1 || kind > 8) return fail(c, SPEC_EINVAL, "profile: unknown kernel class");
     HIPCHK(c, hipStreamSynchronize(c->stream));
     c->prof_epi = kind;
     c->prof_model = model;

@@ -177,3 +177,28 @@ def test_other_head_sizes(dtype, hd_target, hd_draft):
     target = ModelShape(2, 64, 2, 1, hd_target, 128, 512, 10000.0, 1e-5, dtype)
     draft = ModelShape(2, 64, 4, 2, hd_draft, 128, 512, 10000.0, 1e-5, dtype)
     _run(PairConfig("heads", target, draft, "independent", 40, 16, 8), n_generate=12, temperature=0.0, controller="fixed4")
+
+
+@pytest.mark.parametrize("pair", ["tiny", "small-bf16"])
+def test_the_norm_kernel_is_timed(pair):
+    """Class 8 of the kernel timing: one launch a layer and pass in models with normed heads, none in the others."""
+    cfg = synth.pair(pair)
+    Wt, Wd = _models(cfg, which=("target",))
+    eng = _engine(cfg, Wt, Wd, 17, 8, 1, temperature=0.0)
+    eng.prefill(synth.make_prompts(1, 17, cfg.target.vocab, 7))
+    for kind in (0, 8):
+        eng.profile_kernel(1, kind)
+        eng.draft(3)
+        eng.verify(3)
+        eng.accept()
+        launches, ms = eng.profile_read_class(1, 8)
+        assert launches == cfg.target.n_layers and ms > 0
+        assert eng.profile_read_class(0, 8)[0] == 0
+        if kind == 0:
+            assert eng.profile_read_class(1, 1)[0] == cfg.target.n_layers * (3 if pair == "tiny" else 1)
+            assert eng.profile_read_class(0, 1)[0] == 3 * cfg.draft.n_layers
+        total, ms_total = eng.profile_read()
+        assert total >= launches and ms_total >= ms
+    with pytest.raises(pk.SpecError):
+        eng.profile_kernel(1, 9)
+    eng.close()
