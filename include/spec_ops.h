@@ -65,7 +65,8 @@ int64_t spec_k_gemm_f8_workspace(int32_t K, int32_t R, int32_t x_dtype);
 
 /* RMS norm of each query and key head, then the rotation of spec.h (element j pairs with j + hd / 2), in one pass:
  *     h <- h / sqrt(mean(h^2) + eps) * norm,   (h[j], h[j + hd/2]) <- (h[j] c - h[j + hd/2] s, h[j + hd/2] c + h[j] s)
- * with c = rope_cos[pos[r]][j], s = rope_sin[pos[r]][j], in fp32 (the squares too: elements beyond 2^59 overflow them).
+ * with c = rope_cos[pos[r]][j], s = rope_sin[pos[r]][j], in fp32.  So are the squares: elements beyond 2^59 overflow them,
+ * and where eps is 0 (it may be) heads with nothing above 2^-60 lose them; a head of zeros is then NaN.
  * q, k: device, dtype SPEC_F32 or SPEC_BF16, head i of row r at element r * ldq + i * hd (k likewise with ldk): the query
  * and key columns of a fused QKV row, or arrays of their own; ldq >= nq * hd, ldk >= nkv * hd.  q_norm, k_norm: device
  * fp32 [hd].  rope_cos, rope_sin: device fp32 [n_pos][hd / 2].  pos: device int32 [R]; a row whose position lies outside

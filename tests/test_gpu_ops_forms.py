@@ -56,6 +56,23 @@ def test_norm_of_key_heads_alone(t_in, t_out):
     ops._norm_case(np.random.default_rng(6), 9, 0, 4, 64, t_in, t_out)
 
 
+def test_norm_without_eps():
+    """eps = 0: any size of a head whose squares fp32 holds comes out normed."""
+    R, hd = 7, 96
+    rng = np.random.default_rng(4)
+    h = rng.standard_normal((R, 1, hd)) * 2.0 ** np.array([-45, -20, -3, 0, 8, 30, 55])[:, None, None]
+    cos, sin = ops._tables(R, hd)
+    g = np.ones(hd, dtype=np.float32)
+    cu = lambda a: torch.from_numpy(a).cuda()
+    q = cu(h.astype(np.float32))
+    out = [torch.zeros_like(q), torch.zeros_like(q)]
+    pk.k_qk_norm_rope(q, q, cu(g), cu(g), cu(cos), cu(sin), torch.arange(R, dtype=torch.int32, device="cuda"), *out, eps=0.0,
+                      stream=ops._stream())
+    want, mag = ref.norm_rope(q.double().cpu().numpy(), g.astype(np.float64), 0.0, cos.astype(np.float64), sin.astype(np.float64))
+    for o in out:
+        assert (np.abs(o.double().cpu().numpy() - want) <= (hd / 2 + 8) * 2.0 ** -23 * mag + 2.0 ** -24 * np.abs(want)).all()
+
+
 @pytest.mark.parametrize("t_in,t_out", [(F32, F32), (F32, BF16), (BF16, F32), (BF16, BF16)])
 @pytest.mark.parametrize("hd", [64, 128, 256])
 @pytest.mark.parametrize("shift,extra", [(1, 3), (2, 0), (4, 4), (8, 12)])
