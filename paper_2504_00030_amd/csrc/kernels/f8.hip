@@ -356,11 +356,12 @@ __device__ __forceinline__ void meet_but() {
 // bytes, eight chunks; position p of row i holds chunk p ^ (i / 2 % 8), which spreads the sixteen rows a fragment read
 // touches over all banks.
 // F16: the fragments are turned into fp16 (exact sums), otherwise multiplied as e4m3.
-// What bounds it: 4096 x 28672 x 4096 in tiles of 256 x 256 takes 464 - 480 us, 2.0 PFLOP/s, with the matrix units busy 53 % of the
-// cycles at a clock that the power limit holds at 1.8 GHz (zeros instead of data: 426 us); a library product of the same
-// operands without block scales takes 326 us.  With fp32 results 895 us, 1.1 PFLOP/s: half the rate, and four
+// What bounds it: 4096 x 28672 x 4096 in tiles of 256 x 256 takes 470 us, 2.0 PFLOP/s, with the matrix units busy 52 % of the
+// cycles: 5.7 vector instructions for each matrix instruction (four of them additions, the others mostly addresses of the
+// copies), and a clock that the power limit holds at 1.8 GHz (zeros instead of data took a tenth less); a library product of
+// the same operands without block scales takes 331 us.  With fp32 results 918 us, 1.05 PFLOP/s: half the rate, and four
 // vector instructions (conversions, additions) for each matrix instruction, which share the issue with it: without three
-// quarters of the additions it would take 800 us, and the small tiles gained 3 % from offsets kept in registers.
+// quarters of the additions it would take a tenth less, and the small tiles gained 3 % from offsets kept in registers.
 // Measured and not taken: four waves of 128 x 128 each (their accumulators do not fit the vector registers: 1020 us), copies
 // through registers (606), 32 x 32 x 64 instructions (spills: 578), all copies of a step at once (485), wave priorities (475).
 template <typename OT, bool F16, int TN, int TR, int PN, int PR, int S>

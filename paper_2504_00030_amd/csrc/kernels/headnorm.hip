@@ -4,8 +4,8 @@
 //
 // A head is held by a group of lanes (a power of two), four or eight pairs (j, j + hd/2) a lane, so both partners of every
 // pair and the whole sum of squares stay in registers and a head is read and written once.  What bounds the kernel is
-// memory (16384 rows x 40 heads of 128, bf16 to bf16 66 us, fp32 to fp32 117 us: 5.1 and 5.7 TB/s) or, for small calls, the
-// launch (one row: 2.9 us).
+// memory (16384 rows x 40 heads of 128, bf16 to bf16 65 us, fp32 to fp32 117 us: 5.2 and 5.7 TB/s; a copy of such arrays
+// reaches 6.0) or, for small calls, the launch (one row: 2.9 us).
 #include "common.hpp"
 #include "kv.hpp"
 #include "params.hpp"
@@ -171,8 +171,8 @@ hipError_t launch_head_norm(const HeadNormArgs &a, hipStream_t s) {
 
 // The engine's form: the plain result of a layer's QKV projection -> queries (fp32 and two bf16 terms) and the paged
 // cache, what the QKV epilogue writes for models without head norms.  A group of lanes per head, value heads included.
-// A prompt's 1024 rows of 48 heads of 128: 19.7 us, 3.2 TB/s (29.7 with every element stored by itself; the projection in
-// front takes 159); nine rows of a verification pass: 4.9 us.
+// A prompt of 1024 tokens, 48 heads of 128: 18.5 us, 3.4 TB/s (29.7 with every element stored by itself; the projection in
+// front takes 159); nine rows of a verification pass: 5.0 us.
 template <int LPH>
 __global__ __launch_bounds__(256) void qkv_norm_k(const QkvNormArgs a) {
     if (a.active != nullptr && *a.active == 0) return;
