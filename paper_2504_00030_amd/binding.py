@@ -29,6 +29,7 @@ EXPORTS = [
     "spec_debug_drafted", "spec_debug_read", "spec_debug_fill_kv", "spec_debug_write_kv", "spec_debug_set_block_table", "spec_device_bytes", "spec_profile_kernel", "spec_profile_read", "spec_profile_read_class", "spec_debug_verify_rows", "spec_destroy",
     "spec_strerror", "spec_last_error", "spec_k_gemv", "spec_k_gemv_tiled", "spec_k_gemm_tiled", "spec_k_retile_q8", "spec_k_gemv_tiled_q8", "spec_k_gemm_tiled_q8", "spec_k_retile", "spec_k_copy", "spec_k_philox", "spec_k_accept", "spec_k_accept_static",
     "spec_k_quant_f8", "spec_k_gemm_f8", "spec_k_gemm_f8_workspace", "spec_k_qk_norm_rope",
+    "spec_k_rope_tables", "spec_k_rope_cache", "spec_k_attn_shared", "spec_k_attn_shared_workspace", "spec_k_verify", "spec_k_verify_workspace",
     "gammatune_init", "gammatune_update",
 ]
 
@@ -57,6 +58,11 @@ class SpecConfig(C.Structure):
 
 class SpecGenStats(C.Structure):
     _fields_ = [(n, C.c_int64) for n in ("steps", "generated", "accepted", "drafted", "gamma_sum", "seq_steps")]
+
+
+class SpecRope(C.Structure):
+    _fields_ = [("theta", C.c_double), ("scaling", C.c_int32), ("factor", C.c_double), ("low", C.c_double), ("high", C.c_double),
+                ("context", C.c_double), ("magnitude", C.c_double)]
 
 
 class GtParams(C.Structure):
@@ -143,6 +149,16 @@ def load() -> C.CDLL:
     lib.spec_k_gemm_f8_workspace.restype = i64
     lib.spec_k_qk_norm_rope.argtypes = [vp, i64, i32, vp, i64, i32, i32, i32, i32, vp, vp, C.c_float, vp, vp, i32, vp, vp, i64,
                                         vp, i64, i32, vp]
+    lib.spec_k_rope_tables.argtypes = [C.POINTER(SpecRope), i32, i32, vp, vp, vp]
+    lib.spec_k_rope_cache.argtypes = [vp, i64, i32, vp, i64, vp, i64, i32, i32, i32, i32, vp, vp, i32, i32, i32, vp, vp, vp, i64, vp, vp,
+                                      i32, i32, i32, vp]
+    lib.spec_k_attn_shared.argtypes = [vp, i64, i32, i32, i32, i32, i32, vp, i32, vp, vp, i32, i32, vp, i32, vp, i32, vp, C.c_float, vp,
+                                       i64, vp, i64, vp]
+    lib.spec_k_attn_shared_workspace.argtypes = [i32] * 8
+    lib.spec_k_attn_shared_workspace.restype = i64
+    lib.spec_k_verify.argtypes = [vp, i64, vp, i64, i32, i32, vp, i32, i32, vp, vp, vp, vp, vp, vp, i64, vp]
+    lib.spec_k_verify_workspace.argtypes = [i32, i32]
+    lib.spec_k_verify_workspace.restype = i64
     lib.gammatune_init.argtypes = [C.POINTER(GtState), C.POINTER(GtParams), C.c_int32]
     lib.gammatune_update.argtypes = [C.POINTER(GtState), C.c_int32, C.c_int32]
     lib.gammatune_update.restype = C.c_int32
@@ -688,3 +704,213 @@ def k_qk_norm_rope(q, k, q_norm, k_norm, cos, sin, pos, q_out, k_out, eps: float
                                     q_out.data_ptr(), ldqo, k_out.data_ptr(), ldko, _kind(q_out, "q_out"), stream)
     if rc != 0:
         _refused(rc, "spec_k_qk_norm_rope")
+
+
+# ---- operators of a verification pass over a batch that shares a prefix (include/spec_batch.h) -------------------------
+ROPE_SCALINGS = {"plain": 0, "linear": 1, "base": 2, "bands": 3, "ramp": 4}
+
+
+def _vector(t, name: str, n: int, dtype):
+    if t.dtype is not dtype or t.numel() != n or not t.is_contiguous():
+        _need(t, name, f"a contiguous {dtype} tensor of {n} elements")
+
+
+def _work(workspace, dev: int):
+    if workspace is None:
+        return None, 0
+    if workspace.get_device() != dev or not workspace.is_contiguous():
+        _need(workspace, "workspace", "contiguous, on the device of the operands")
+    return workspace.data_ptr(), workspace.nbytes
+
+
+def _heads(t, name: str, R: int, hd: int) -> int:
+    """Row stride of a [R][heads][hd] tensor whose rows hold their heads one after the other."""
+    shape, stride = t.shape, t.stride()
+    if len(shape) != 3 or shape[0] != R or shape[2] != hd or stride[2] != 1 or (stride[1] != hd and shape[1] > 1):
+        _need(t, name, f"[{R}][heads][{hd}] with the heads of a row one after the other")
+    return stride[0] if R > 1 else shape[1] * hd  # (the stride of a single row says nothing)
+
+
+def _pool(k_pages, v_pages):
+    shape = k_pages.shape
+    if len(shape) != 4 or v_pages.shape != shape or k_pages.dtype is not v_pages.dtype or not (k_pages.is_contiguous() and v_pages.is_contiguous()):
+        raise ValueError("k_pages and v_pages must be contiguous tensors [pages][heads][page_tokens][hd] of one shape and type")
+    return shape
+
+
+def k_rope_tables(cos, sin, theta: float = 10000.0, scaling: str = "plain", factor: float = 1.0, low: float = 1.0, high: float = 32.0,
+                  context: float = 8192.0, magnitude: float = 0.0, stream: int = 0):
+    """Fill cos, sin (fp32 [n_pos][rot / 2]) for a base theta.  scaling "plain", or for contexts `factor` times as long "linear",
+    "base", "bands" or "ramp" (spec_batch.h states them; the last two keep pairs that turn more than `high` times over `context`
+    positions and interpolate those below `low`; magnitude 0 is the ramp's own)."""
+    if not _KINDS:
+        _setup()
+    if scaling not in ROPE_SCALINGS:
+        raise ValueError(f"scaling must be one of {sorted(ROPE_SCALINGS)}, not {scaling!r}")
+    n_pos, half = cos.shape
+    if (n_pos | 2 * half) >> 31:
+        _too_long(n_pos, half)
+    _vector(cos, "cos", n_pos * half, _F32T)
+    _vector(sin, "sin", n_pos * half, _F32T)
+    dev = cos.get_device()
+    if sin.get_device() != dev:
+        _elsewhere(cos, sin)
+    _on(dev, cos)
+    rope = SpecRope(theta, ROPE_SCALINGS[scaling], factor, low, high, context, magnitude)
+    rc = load().spec_k_rope_tables(C.byref(rope), 2 * half, n_pos, cos.data_ptr(), sin.data_ptr(), stream)
+    if rc != 0:
+        _refused(rc, "spec_k_rope_tables")
+
+
+def k_rope_cache(q, k, v, cos, sin, pos, slot, q_out, k_pages, v_pages, interleaved: bool = False, stream: int = 0):
+    """Rotate the heads of q [R][nq][hd] and k [R][nkv][hd] (fp32 or bf16, views into fused rows included) by their positions and
+    write queries to q_out, keys and the values v [R][nkv][hd] to slots of the pages [n_pages][nkv][page_tokens][hd].  The first
+    2 * cos.shape[1] elements of a head turn, in halves or interleaved pairs.  pos, slot: int32 [R]; rows with a position outside the
+    tables are left out, rows with a slot outside the pool write their queries alone.  q and q_out None: cache alone; k, v, slot
+    and pages None: queries alone."""
+    if not _KINDS:
+        _setup()
+    if (q is None) != (q_out is None) or any((t is None) != (k is None) for t in (v, slot, k_pages, v_pages)) or (q is None and k is None):
+        raise ValueError("q and q_out go together, and so do k, v, slot, k_pages and v_pages; one of the two sets is needed")
+    main = q if q is not None else k
+    if len(main.shape) != 3:
+        _need(main, "q" if q is not None else "k", "[R][heads][hd]")
+    R, _, hd = main.shape
+    n_pos, half = cos.shape
+    nq = nkv = ldq = ldqo = ldk = ldv = n_pages = page = 0
+    qp = qop = kp = vp = sp = kpp = vpp = None
+    dev = main.get_device()
+    on = [cos.get_device(), sin.get_device(), pos.get_device()]
+    if q is not None:
+        nq, ldq, ldqo = q.shape[1], _heads(q, "q", R, hd), _heads(q_out, "q_out", R, hd)
+        if q_out.shape != q.shape:
+            _need(q_out, "q_out", f"of the shape of q, {tuple(q.shape)}")
+        qp, qop, out = q.data_ptr(), q_out.data_ptr(), q_out
+        on.append(q_out.get_device())
+    if k is not None:
+        nkv, ldk, ldv = k.shape[1], _heads(k, "k", R, hd), _heads(v, "v", R, hd)
+        shape = _pool(k_pages, v_pages)
+        n_pages, page = shape[0], shape[2]
+        if v.shape != k.shape or v.dtype is not k.dtype or shape[1] != nkv or shape[3] != hd:
+            raise ValueError("k, v and the pages must agree in heads and head size, k and v in type")
+        if q is not None and (q.dtype is not k.dtype or q_out.dtype is not k_pages.dtype):
+            raise ValueError("q and k must have one type, and q_out and the pages theirs")
+        _vector(slot, "slot", R, _I32T)
+        kp, vp, sp, kpp, vpp, out = k.data_ptr(), v.data_ptr(), slot.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(), k_pages
+        on += [k.get_device(), v.get_device(), slot.get_device(), k_pages.get_device(), v_pages.get_device()]
+    if (R | nq | nkv | hd | n_pos | half * 2 | n_pages | page) >> 31:
+        _too_long(R, nq, nkv, hd, n_pos, half, n_pages, page)
+    _vector(cos, "cos", n_pos * half, _F32T)
+    _vector(sin, "sin", n_pos * half, _F32T)
+    _vector(pos, "pos", R, _I32T)
+    if on.count(dev) != len(on):
+        _elsewhere(*[t for t in (q, k, v, cos, sin, pos, slot, q_out, k_pages, v_pages) if t is not None])
+    _on(dev, main)
+    rc = load().spec_k_rope_cache(qp, ldq, nq, kp, ldk, vp, ldv, nkv, _kind(main, "q"), hd, R, cos.data_ptr(), sin.data_ptr(), n_pos,
+                                  2 * half, 1 if interleaved else 0, pos.data_ptr(), sp, qop, ldqo, kpp, vpp, n_pages, page,
+                                  _kind(out, "q_out"), stream)
+    if rc != 0:
+        _refused(rc, "spec_k_rope_cache")
+
+
+def k_attn_shared_workspace(R: int, n_seq: int, nq: int, nkv: int, hd: int, dtype, prefix_len: int, own_capacity: int) -> int:
+    """Bytes of workspace k_attn_shared needs; own_capacity is table.shape[1] * page_tokens."""
+    if not _KINDS:
+        _setup()
+    if dtype not in _KINDS:
+        raise ValueError(f"unsupported element type {dtype}")
+    sizes = (R, n_seq, nq, nkv, hd, prefix_len, own_capacity)
+    if any(not -2**31 <= n < 2**31 for n in sizes):
+        _too_long(*sizes)
+    n = load().spec_k_attn_shared_workspace(R, n_seq, nq, nkv, hd, _KINDS[dtype], prefix_len, own_capacity)
+    if n < 0:
+        _refused(int(n), "spec_k_attn_shared_workspace")
+    return int(n)
+
+
+def k_attn_shared(q, k_pages, v_pages, row_start, table, own_len, out, workspace, prefix_table=None, prefix_len: int = 0,
+                  scale: Optional[float] = None, stream: int = 0):
+    """Attention of the rows q [R][nq][hd] (bf16 or fp32, as pages and out) over a shared prefix and their sequences' own positions,
+    from pages [n_pages][nkv][page_tokens][hd].  Sequence b has rows row_start[b] .. row_start[b + 1] - 1, the last of its own_len[b]
+    own positions, on the pages table[b] (int32 [n_seq][pages]); all see the prefix_len positions on the pages prefix_table.  scale
+    defaults to hd ** -0.5.  workspace: a GPU tensor of k_attn_shared_workspace() bytes at least, or None where that is 0."""
+    if not _KINDS:
+        _setup()
+    if len(q.shape) != 3:
+        _need(q, "q", "[R][heads][hd]")
+    R, nq, hd = q.shape
+    ldq, ldo = _heads(q, "q", R, hd), _heads(out, "out", R, hd)
+    n_pages, nkv, page, pd = _pool(k_pages, v_pages)
+    if out.shape != q.shape or not (q.dtype is out.dtype is k_pages.dtype) or pd != hd:
+        raise ValueError("q, out and the pages must have one type and head size, q and out one shape")
+    n_seq = own_len.numel()
+    if table.dtype is not _I32T or len(table.shape) != 2 or table.shape[0] != n_seq or not table.is_contiguous():
+        _need(table, "table", f"a contiguous int32 tensor of {n_seq} x pages")
+    if (R | nq | nkv | hd | n_pages | page | n_seq | table.shape[1]) >> 31 or prefix_len >> 31 > 0:
+        _too_long(R, nq, nkv, hd, n_pages, page, n_seq, table.shape[1], prefix_len)
+    _vector(own_len, "own_len", n_seq, _I32T)
+    _vector(row_start, "row_start", n_seq + 1, _I32T)
+    dev = q.get_device()
+    pt = None
+    if prefix_len > 0:
+        if prefix_table is None or prefix_table.dtype is not _I32T or prefix_table.numel() < (prefix_len + page - 1) // page or \
+                not prefix_table.is_contiguous() or prefix_table.get_device() != dev:
+            raise ValueError("prefix_table must be a contiguous int32 tensor with a page for every page_tokens positions of the prefix, on the device of q")
+        pt = prefix_table.data_ptr()
+    if not (k_pages.get_device() == v_pages.get_device() == row_start.get_device() == table.get_device() == own_len.get_device() ==
+            out.get_device() == dev):
+        _elsewhere(q, k_pages, v_pages, row_start, table, own_len, out)
+    _on(dev, q)
+    work, work_bytes = _work(workspace, dev)
+    rc = load().spec_k_attn_shared(q.data_ptr(), ldq, nq, nkv, hd, _kind(q, "q"), R, row_start.data_ptr(), n_seq, k_pages.data_ptr(),
+                                   v_pages.data_ptr(), n_pages, page, pt, prefix_len, table.data_ptr(), table.shape[1], own_len.data_ptr(),
+                                   hd ** -0.5 if scale is None else scale, out.data_ptr(), ldo, work, work_bytes, stream)
+    if rc != 0:
+        _refused(rc, "spec_k_attn_shared")
+
+
+def k_verify_workspace(n_seq: int, vocab: int) -> int:
+    """Bytes of workspace k_verify needs."""
+    if any(not -2**31 <= n < 2**31 for n in (n_seq, vocab)):
+        _too_long(n_seq, vocab)
+    n = load().spec_k_verify_workspace(n_seq, vocab)
+    if n < 0:
+        _refused(int(n), "spec_k_verify_workspace")
+    return int(n)
+
+
+def k_verify(p, q, draft_start, drafted, u_accept, u_next, n_accepted, next_token, workspace, stream: int = 0):
+    """Verify drafts against the probabilities p [n_drafts + n_seq][vocab] of the target and q [n_drafts][vocab] of the draft
+    model (fp32 or bf16, any row stride; q None: drafts without probabilities).  Sequence b has drafts draft_start[b] ..
+    draft_start[b + 1] - 1 and the rows of p from draft_start[b] + b on, one more than drafts.  u_accept fp32 [n_drafts], u_next fp32
+    [n_seq]: the random numbers; n_accepted, next_token: int32 [n_seq], the result."""
+    if not _KINDS:
+        _setup()
+    ldp = _rows(p, "p")
+    vocab, n_seq, n_drafts = p.shape[1], u_next.numel(), drafted.numel()
+    if (vocab | p.shape[0]) >> 31:
+        _too_long(vocab, p.shape[0])
+    if p.shape[0] != n_seq + n_drafts:
+        _need(p, "p", f"of {n_seq + n_drafts} rows, one for every draft and one for every sequence")
+    _vector(draft_start, "draft_start", n_seq + 1, _I32T)
+    _vector(drafted, "drafted", n_drafts, _I32T)
+    _vector(u_accept, "u_accept", n_drafts, _F32T)
+    _vector(u_next, "u_next", n_seq, _F32T)
+    _vector(n_accepted, "n_accepted", n_seq, _I32T)
+    _vector(next_token, "next_token", n_seq, _I32T)
+    dev = p.get_device()
+    qp, ldq = None, vocab
+    if q is not None:
+        ldq = _rows(q, "q") if n_drafts else vocab
+        if q.shape != (n_drafts, vocab) or q.dtype is not p.dtype or q.get_device() != dev:
+            _need(q, "q", f"{n_drafts} x {vocab} of the type and on the device of p")
+        qp = q.data_ptr()
+    if not (draft_start.get_device() == drafted.get_device() == u_accept.get_device() == u_next.get_device() == n_accepted.get_device() ==
+            next_token.get_device() == dev):
+        _elsewhere(p, draft_start, drafted, u_accept, u_next, n_accepted, next_token)
+    _on(dev, p)
+    work, work_bytes = _work(workspace, dev)
+    rc = load().spec_k_verify(p.data_ptr(), ldp, qp, ldq, _kind(p, "p"), vocab, draft_start.data_ptr(), n_seq, n_drafts, drafted.data_ptr(),
+                              u_accept.data_ptr(), u_next.data_ptr(), n_accepted.data_ptr(), next_token.data_ptr(), work, work_bytes, stream)
+    if rc != 0:
+        _refused(rc, "spec_k_verify")

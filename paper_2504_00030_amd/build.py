@@ -35,9 +35,12 @@ HIP_SOURCES = [
     "kernels/misc.hip",
     "kernels/f8.hip",
     "kernels/headnorm.hip",
+    "kernels/rope.hip",
+    "kernels/shared_attention.hip",
+    "kernels/verify.hip",
 ]
 C_SOURCES = ["gammatune.c"]
-MFMA_SOURCES = ["kernels/gemv_mfma.hip", "kernels/gemm_mfma.hip", "kernels/attention.hip", "kernels/f8.hip"]  # scanned by isa_guard after compiling
+MFMA_SOURCES = ["kernels/gemv_mfma.hip", "kernels/gemm_mfma.hip", "kernels/attention.hip", "kernels/f8.hip", "kernels/shared_attention.hip"]  # scanned by isa_guard after compiling
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 HIP_FLAGS = [

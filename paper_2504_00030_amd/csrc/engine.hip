@@ -7,6 +7,7 @@
 #include "spec.h"
 #include "spec_debug.h"
 #include "spec_ops.h"
+#include "spec_batch.h"
 #include "gammatune.h"
 
 #include <hip/hip_runtime.h>
@@ -1835,6 +1836,163 @@ int spec_k_qk_norm_rope(const void *q, int64_t ldq, int32_t nq, const void *k, i
     a.q_norm = q_norm; a.k_norm = k_norm; a.eps = eps; a.rope_cos = rope_cos; a.rope_sin = rope_sin; a.n_pos = n_pos; a.pos = pos;
     a.q_out = q_out; a.k_out = k_out; a.ldqo = ldqo; a.ldko = ldko; a.out_dtype = out_dtype;
     return launched(launch_head_norm(a, reinterpret_cast<hipStream_t>(stream)), "qk_norm_rope: launch failed");
+}
+
+// ---- operators of a verification pass over a batch that shares a prefix (spec_batch.h) -------------------------------
+
+static int shift_of(int32_t page_tokens) {  // -1: not a power of two from 8 to 2^20
+    for (int s = 3; s <= 20; ++s)
+        if (page_tokens == 1 << s) return s;
+    return -1;
+}
+
+int spec_k_rope_tables(const spec_rope *rope, int32_t rot, int32_t n_pos, float *rope_cos, float *rope_sin, void *stream) {
+    if (!rope || !rope_cos || !rope_sin) return refuse(SPEC_EINVAL, "rope_tables: null pointer");
+    if (off(rope_cos, 4) || off(rope_sin, 4)) return refuse(SPEC_EINVAL, "rope_tables: misaligned pointer");
+    if (rot < 2 || rot > 512 || rot % 2 || n_pos < 1 || n_pos > 1 << 28)
+        return refuse(SPEC_EINVAL, "rope_tables: rot must be even, 2 to 512, n_pos 1 to 2^28");
+    const int kind = rope->scaling;
+    const double th = rope->theta, fa = rope->factor, lo = rope->low, hi = rope->high, ctx = rope->context;
+    const bool bands = kind == SPEC_ROPE_BANDS, ramp = kind == SPEC_ROPE_RAMP;
+    if (kind < SPEC_ROPE_PLAIN || kind > SPEC_ROPE_RAMP) return refuse(SPEC_EINVAL, "rope_tables: unknown scaling");
+    if (!(th > (ramp ? 1.0 : 0.0) && std::isfinite(th)) || (kind != SPEC_ROPE_PLAIN && !(fa > 0.0 && std::isfinite(fa))))
+        return refuse(SPEC_EINVAL, "rope_tables: theta and factor must be positive and finite (theta beyond 1 for a ramp)");
+    if ((bands || ramp) && !(lo >= 0.0 && hi > lo && std::isfinite(hi) && ctx > 0.0 && std::isfinite(ctx) && (bands || lo > 0.0)))
+        return refuse(SPEC_EINVAL, "rope_tables: low must lie below high, neither negative (nor 0 for a ramp), and context be positive");
+    if (ramp && !(rope->magnitude >= 0.0 && std::isfinite(rope->magnitude))) return refuse(SPEC_EINVAL, "rope_tables: magnitude must be finite and not negative");
+    RopeTableArgs a{};
+    a.rope_cos = rope_cos; a.rope_sin = rope_sin; a.n_pos = n_pos; a.half = rot / 2;
+    a.magnitude = !ramp ? 1.0 : rope->magnitude > 0.0 ? rope->magnitude : 0.1 * std::log(fa) + 1.0;
+    const double two_pi = 6.283185307179586476925287;
+    const double base = kind == SPEC_ROPE_BASE ? th * std::pow(fa, (double)rot / std::max(rot - 2, 1)) : th;
+    double first = 0.0, last = 0.0;
+    if (ramp) {
+        auto pair = [&](double turns) { return rot * std::log(ctx / (two_pi * turns)) / (2.0 * std::log(th)); };
+        first = std::max(std::floor(pair(hi)), 0.0);
+        last = std::min(std::ceil(pair(lo)), rot - 1.0);
+    }
+    for (int j = 0; j < rot / 2; ++j) {
+        const double t = std::pow(base, -2.0 * j / rot);
+        double f = t;
+        if (kind == SPEC_ROPE_LINEAR) {
+            f = t / fa;
+        } else if (bands) {
+            const double s = std::min(std::max((ctx * t / two_pi - lo) / (hi - lo), 0.0), 1.0);
+            f = t * (s + (1.0 - s) / fa);
+        } else if (ramp) {
+            const double g = std::min(std::max((j - first) / std::max(last - first, 0.001), 0.0), 1.0);
+            f = t * (1.0 - g + g / fa);
+        }
+        if (!std::isfinite(f * n_pos)) return refuse(SPEC_EINVAL, "rope_tables: angles beyond the range of 64 bits");
+        a.f[j] = f;
+    }
+    return launched(launch_rope_tables(a, reinterpret_cast<hipStream_t>(stream)), "rope_tables: launch failed");
+}
+
+int spec_k_rope_cache(const void *q, int64_t ldq, int32_t nq, const void *k, int64_t ldk, const void *v, int64_t ldv, int32_t nkv,
+                      int32_t dtype, int32_t hd, int32_t R, const float *rope_cos, const float *rope_sin, int32_t n_pos, int32_t rot,
+                      int32_t interleaved, const int32_t *pos, const int32_t *slot, void *q_out, int64_t ldqo, void *k_pages,
+                      void *v_pages, int32_t n_pages, int32_t page_tokens, int32_t out_dtype, void *stream) {
+    if (!wide(dtype) || !wide(out_dtype)) return refuse(SPEC_EINVAL, "rope_cache: heads and pages must be fp32 or bf16");
+    if (hd < 2 || hd > 512 || rot < 2 || rot > hd || rot % 2) return refuse(SPEC_EINVAL, "rope_cache: hd must be 2 to 512, rot even, 2 to hd");
+    if (nq < 0 || nkv < 0 || (int64_t)nq + nkv < 1 || R < 0 || (int64_t)nq + 2 * (int64_t)nkv > 1 << 20 ||
+        (int64_t)R * ((int64_t)nq + 2 * (int64_t)nkv) > 0x7fffffff || n_pos < 1)
+        return refuse(SPEC_EINVAL, "rope_cache: no heads, more than 2^20 of them, R < 0, R * heads beyond 2^31 or n_pos < 1");
+    if ((nq && (ldq < (int64_t)nq * hd || ldqo < (int64_t)nq * hd)) || (nkv && (ldk < (int64_t)nkv * hd || ldv < (int64_t)nkv * hd)))
+        return refuse(SPEC_EINVAL, "rope_cache: row stride below the heads' width");
+    const int shift = nkv ? shift_of(page_tokens) : 0;
+    if (nkv && (shift < 0 || n_pages < 1 || ((int64_t)n_pages << shift) > 0x7fffffff))
+        return refuse(SPEC_EINVAL, "rope_cache: page_tokens must be a power of two from 8 to 2^20, and the pool hold 1 to 2^31 - 1 slots");
+    if (R == 0) return SPEC_OK;
+    if (!rope_cos || !rope_sin || !pos || (nq && (!q || !q_out)) || (nkv && (!k || !v || !slot || !k_pages || !v_pages)))
+        return refuse(SPEC_EINVAL, "rope_cache: null pointer");
+    if (off(rope_cos, 4) || off(rope_sin, 4) || off(pos, 4) || (nq && (off(q, width(dtype)) || off(q_out, width(out_dtype)))) ||
+        (nkv && (off(k, width(dtype)) || off(v, width(dtype)) || off(slot, 4) || off(k_pages, 16) || off(v_pages, 16))))
+        return refuse(SPEC_EINVAL, "rope_cache: misaligned pointer");
+    RopeCacheArgs a{};
+    a.q = q; a.k = k; a.v = v; a.ldq = ldq; a.ldk = ldk; a.ldv = ldv; a.nq = nq; a.nkv = nkv; a.dtype = dtype; a.hd = hd; a.R = R;
+    a.rope_cos = rope_cos; a.rope_sin = rope_sin; a.n_pos = n_pos; a.rot = rot; a.interleaved = interleaved != 0; a.pos = pos; a.slot = slot;
+    a.q_out = q_out; a.ldqo = ldqo; a.k_pages = k_pages; a.v_pages = v_pages; a.page_shift = shift; a.out_dtype = out_dtype;
+    a.slots = nkv ? (int32_t)((int64_t)n_pages << shift) : 0;
+    return launched(launch_rope_cache(a, reinterpret_cast<hipStream_t>(stream)), "rope_cache: launch failed");
+}
+
+// The sizes of an attention call in `a`; false where they are refused.
+static bool shared_sizes(SharedAttnArgs &a, int32_t R, int32_t n_seq, int32_t nq, int32_t nkv, int32_t hd, int32_t dtype,
+                         int32_t prefix_len, int64_t own_capacity) {
+    if (!wide(dtype) || R < 0 || n_seq < 1 || n_seq > 65536 || nq < 1 || nkv < 1 || nq % nkv || hd < 8 || hd > 256 || hd % 8 ||
+        prefix_len < 0 || prefix_len >= 1 << 30 || own_capacity < 0 || own_capacity >= 1 << 30 || (int64_t)R * nq > 0x7fffffff)
+        return false;
+    a.dtype = dtype; a.R = R; a.n_seq = n_seq; a.nq = nq; a.nkv = nkv; a.g = nq / nkv; a.hd = hd; a.prefix_len = prefix_len;
+    plan_shared_attention(a, own_capacity);
+    return true;
+}
+static int64_t shared_bytes(const SharedAttnArgs &a) { return (int64_t)a.R * a.nq * shared_attention_parts(a) * (a.hd + 2) * 4; }
+
+int64_t spec_k_attn_shared_workspace(int32_t R, int32_t n_seq, int32_t nq, int32_t nkv, int32_t hd, int32_t dtype, int32_t prefix_len,
+                                     int32_t own_capacity) {
+    SharedAttnArgs a{};
+    if (!shared_sizes(a, R, n_seq, nq, nkv, hd, dtype, prefix_len, own_capacity)) return refuse(SPEC_EINVAL, "attn_shared_workspace: sizes that attn_shared refuses");
+    return shared_bytes(a);
+}
+
+int spec_k_attn_shared(const void *q, int64_t ldq, int32_t nq, int32_t nkv, int32_t hd, int32_t dtype, int32_t R,
+                       const int32_t *row_start, int32_t n_seq, const void *k_pages, const void *v_pages, int32_t n_pages,
+                       int32_t page_tokens, const int32_t *prefix_table, int32_t prefix_len, const int32_t *table,
+                       int32_t table_pages, const int32_t *own_len, float scale, void *out, int64_t ldo, void *workspace,
+                       int64_t workspace_bytes, void *stream) {
+    const int shift = shift_of(page_tokens);
+    if (shift < 0 || n_pages < 1 || ((int64_t)n_pages << shift) > 0x7fffffff)
+        return refuse(SPEC_EINVAL, "attn_shared: page_tokens must be a power of two from 8 to 2^20, and the pool hold 1 to 2^31 - 1 slots");
+    SharedAttnArgs a{};
+    if (table_pages < 0 || !shared_sizes(a, R, n_seq, nq, nkv, hd, dtype, prefix_len, (int64_t)table_pages << shift))
+        return refuse(SPEC_EINVAL, "attn_shared: fp32 or bf16; hd a multiple of 8 up to 256, nq one of nkv, 1 to 65536 sequences, R * nq below 2^31, prefix and tables below 2^30 positions");
+    a.scale2 = (float)((double)scale * 1.4426950408889634);
+    if (!(scale > 0.f) || !(a.scale2 > 0.f) || !std::isfinite(a.scale2)) return refuse(SPEC_EINVAL, "attn_shared: scale must be positive and finite");
+    if (ldq < (int64_t)nq * hd || ldo < (int64_t)nq * hd || workspace_bytes < 0) return refuse(SPEC_EINVAL, "attn_shared: row stride below the heads' width");
+    if (R == 0) return SPEC_OK;
+    if (!q || !out || !row_start || !own_len || !k_pages || !v_pages || (prefix_len && !prefix_table) || (table_pages && !table))
+        return refuse(SPEC_EINVAL, "attn_shared: null pointer");
+    if (off(q, width(dtype)) || off(out, width(dtype)) || off(row_start, 4) || off(own_len, 4) || off(prefix_table, 4) || off(table, 4) ||
+        off(k_pages, 16) || off(v_pages, 16) || off(workspace, 16))
+        return refuse(SPEC_EINVAL, "attn_shared: misaligned pointer");
+    if ((workspace ? workspace_bytes : 0) < shared_bytes(a)) return refuse(SPEC_EINVAL, "attn_shared: workspace too small");
+    a.q = q; a.ldq = ldq; a.out = out; a.ldo = ldo; a.k_pages = k_pages; a.v_pages = v_pages; a.n_pages = n_pages; a.page_shift = shift;
+    a.row_start = row_start; a.own_len = own_len; a.prefix_table = prefix_table; a.table = table; a.table_pages = table_pages;
+    a.q_whole = !off(q, 16) && ldq % (16 / (int64_t)width(dtype)) == 0;
+    a.part_o = reinterpret_cast<float *>(workspace);
+    a.part_ml = a.part_o + (int64_t)R * nq * shared_attention_parts(a) * hd;
+    return launched(launch_shared_attention(a, reinterpret_cast<hipStream_t>(stream)), "attn_shared: launch failed");
+}
+
+int64_t spec_k_verify_workspace(int32_t n_seq, int32_t vocab) {
+    if (n_seq < 0 || n_seq > 65535 || vocab < 1 || vocab > 1 << 24)
+        return refuse(SPEC_EINVAL, "verify_workspace: n_seq outside 0 .. 65535 or vocab outside 1 .. 2^24");
+    const int64_t tiles = (vocab + VERIFY_TILE - 1) / VERIFY_TILE;
+    return (int64_t)n_seq * (16 * tiles + 4);
+}
+
+int spec_k_verify(const void *p, int64_t ldp, const void *q, int64_t ldq, int32_t dtype, int32_t vocab, const int32_t *draft_start,
+                  int32_t n_seq, int32_t n_drafts, const int32_t *drafted, const float *u_accept, const float *u_next,
+                  int32_t *n_accepted, int32_t *next_token, void *workspace, int64_t workspace_bytes, void *stream) {
+    if (!wide(dtype)) return refuse(SPEC_EINVAL, "verify: probabilities must be fp32 or bf16");
+    if (n_seq < 0 || n_seq > 65535 || vocab < 1 || vocab > 1 << 24 || n_drafts < 0 || (int64_t)n_drafts + n_seq > 0x7fffffff)
+        return refuse(SPEC_EINVAL, "verify: n_seq outside 0 .. 65535, vocab outside 1 .. 2^24 or n_drafts < 0");
+    if (ldp < vocab || (q && ldq < vocab)) return refuse(SPEC_EINVAL, "verify: row stride below vocab");
+    if (n_seq == 0) return SPEC_OK;
+    if (!p || !draft_start || !u_next || !n_accepted || !next_token || (n_drafts && (!drafted || !u_accept)))
+        return refuse(SPEC_EINVAL, "verify: null pointer");
+    if (off(p, width(dtype)) || off(q, width(dtype)) || off(draft_start, 4) || off(drafted, 4) || off(u_accept, 4) || off(u_next, 4) ||
+        off(n_accepted, 4) || off(next_token, 4) || off(workspace, 16))
+        return refuse(SPEC_EINVAL, "verify: misaligned pointer");
+    if ((workspace ? workspace_bytes : 0) < spec_k_verify_workspace(n_seq, vocab)) return refuse(SPEC_EINVAL, "verify: workspace too small");
+    VerifyArgs a{};
+    a.p = p; a.ldp = ldp; a.q = q; a.ldq = ldq; a.dtype = dtype; a.vocab = vocab; a.tiles = (vocab + VERIFY_TILE - 1) / VERIFY_TILE;
+    a.n_seq = n_seq; a.n_drafts = n_drafts; a.draft_start = draft_start; a.drafted = drafted; a.u_accept = u_accept; a.u_next = u_next;
+    a.n_accepted = n_accepted; a.next_token = next_token;
+    a.sums = reinterpret_cast<double *>(workspace);
+    a.taken = reinterpret_cast<int32_t *>(a.sums + (int64_t)n_seq * a.tiles * 2);
+    return launched(launch_verify(a, reinterpret_cast<hipStream_t>(stream)), "verify: launch failed");
 }
 
 }  // extern "C"

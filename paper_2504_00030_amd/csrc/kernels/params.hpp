@@ -243,6 +243,60 @@ struct QkvNormArgs {
     const int32_t *active;
 };
 
+// Rotary tables (rope.hip).
+struct RopeTableArgs {
+    float *rope_cos, *rope_sin;  // [n_pos][half]
+    int32_t n_pos, half;
+    double magnitude;
+    double f[256];               // radians a position, per pair
+};
+
+// Rotation of heads with the writes of the paged cache (rope.hip); strides in elements.
+struct RopeCacheArgs {
+    const void *q, *k, *v;
+    int64_t ldq, ldk, ldv;
+    int32_t nq, nkv, dtype, hd, R;
+    const float *rope_cos, *rope_sin;  // [n_pos][rot/2]
+    int32_t n_pos, rot, interleaved;
+    const int32_t *pos, *slot;         // [R]
+    void *q_out;
+    int64_t ldqo;
+    void *k_pages, *v_pages;           // [slots / page][nkv][page][hd]
+    int32_t slots, page_shift, out_dtype;
+};
+
+// Attention over a shared prefix and own positions (shared_attention.hip).
+struct SharedAttnArgs {
+    const void *q, *k_pages, *v_pages;
+    void *out;
+    int64_t ldq, ldo;
+    int32_t dtype, nq, nkv, g, hd, R, n_seq, n_pages, page_shift;  // g = nq / nkv
+    const int32_t *row_start, *prefix_table, *table, *own_len;
+    int32_t prefix_len, table_pages;
+    bool q_whole;     // query rows can be read in 16-byte vectors
+    float scale2;     // scale * log2(e)
+    // what plan_shared_attention() lays down
+    int32_t qt, prefix_parts, prefix_chunk, own_parts;
+    uint32_t prefix_groups, own_tiles;
+    int64_t prefix_groups64, own_groups64;
+    float *part_o;    // [R][nq][parts][hd]
+    float *part_ml;   // [R][nq][parts][2]: maximum (times scale2), sum
+};
+
+constexpr int VERIFY_TILE = 4096;  // elements of a row that one workgroup sums
+
+// Verification against given uniforms (verify.hip).
+struct VerifyArgs {
+    const void *p, *q;
+    int64_t ldp, ldq;
+    int32_t dtype, vocab, tiles, n_seq, n_drafts;  // tiles = ceil(vocab / VERIFY_TILE)
+    const int32_t *draft_start, *drafted;
+    const float *u_accept, *u_next;
+    int32_t *n_accepted, *next_token;
+    double *sums;    // [n_seq][tiles][2]: mass of the residual, of the target's row
+    int32_t *taken;  // [n_seq]
+};
+
 // ---- launchers (defined next to the kernels) -----------------------------------------------------
 hipError_t launch_begin_draft(const State &st, const int32_t *gamma_plan, hipStream_t s);
 hipError_t launch_embed(const EmbedArgs &a, hipStream_t s);
@@ -289,5 +343,11 @@ bool gemm_f8_takes_wide(const F8Args &a);  // whether the product quantises fp32
 hipError_t launch_gemm_f8(const F8Args &a, hipStream_t s);
 hipError_t launch_head_norm(const HeadNormArgs &a, hipStream_t s);
 hipError_t launch_qkv_norm(const QkvNormArgs &a, hipStream_t s);
+hipError_t launch_rope_tables(const RopeTableArgs &a, hipStream_t s);
+hipError_t launch_rope_cache(const RopeCacheArgs &a, hipStream_t s);
+void plan_shared_attention(SharedAttnArgs &a, int64_t own_capacity);  // from dtype, sizes, prefix_len
+int64_t shared_attention_parts(const SharedAttnArgs &a);              // parts of a row that the workspace holds
+hipError_t launch_shared_attention(const SharedAttnArgs &a, hipStream_t s);
+hipError_t launch_verify(const VerifyArgs &a, hipStream_t s);
 
 }  // namespace sd
