@@ -17,6 +17,7 @@
 
 #include <algorithm>
 #include <math.h>
+#include <type_traits>
 
 namespace sd {
 
@@ -31,6 +32,7 @@ typedef uint32_t u4_t __attribute__((ext_vector_type(4)));
 constexpr int TILE = 32;      // positions a wave takes at a time
 constexpr int MIN_PART = 128; // least positions of a part: a tile for each of a workgroup's four waves
 constexpr int MAX_PARTS = 64;
+constexpr int STAGE = 64;     // positions of a stage in shared memory
 
 template <int N> struct words { uint32_t w[N]; };
 template <int BYTES, typename E> struct vec_of;
@@ -52,12 +54,23 @@ __device__ __forceinline__ void load_words(const void *p, uint32_t (&w)[N]) {
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 __device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
 
+// over the four lanes of a column
+__device__ __forceinline__ float group_max(float x) {
+    x = fmaxf(x, __shfl_xor(x, 16, WAVE));
+    return fmaxf(x, __shfl_xor(x, 32, WAVE));
+}
+__device__ __forceinline__ float group_sum(float x) {
+    x += __shfl_xor(x, 16, WAVE);
+    return x + __shfl_xor(x, 32, WAVE);
+}
+
 // What one lane keeps of QT x 16 columns in bf16.  HDP: head size rounded up to 32, 64, 128 or 256; channels from hd on are
 // zeros.  W: neighbouring channels of V a lane holds, NB blocks of 16 W.
 template <int HDP_, int QT_, bool EXACT>
 struct CoreBf16 {
     typedef __bf16 T;
     static constexpr int HDP = HDP_, QT = QT_, W = HDP >= 128 ? 8 : HDP / 16, NB = HDP / (16 * W), KC = HDP / 32;
+    static constexpr bool LATE = HDP == 256;  // walk() loads V when K's registers are free: both do not fit
     b8_t q[QT][KC];
     u4_t k[2][KC];            // positions lane % 16 of the tile's two sixteens, channels 32 c + 8 g ..
     uint32_t v[8][NB][W / 2]; // positions 4 g + i of the first (i < 4) and second sixteen, channels W (lane % 16) ..
@@ -91,11 +104,27 @@ struct CoreBf16 {
 #pragma unroll
             for (int n = 0; n < NB; ++n) {
                 const int ch = 16 * W * n + W * c16;
-                if (EXACT || ch < hd) load_words<W / 2>(rows + (int64_t)i * hd + ch, v[4 * s + i][n]);
+                if (EXACT || ch < hd) load_words<W / 2>(rows + i * (EXACT ? HDP : hd) + ch, v[4 * s + i][n]);
                 else {
 #pragma unroll
                     for (int w = 0; w < W / 2; ++w) v[4 * s + i][n][w] = 0;
                 }
+            }
+    }
+    // The same from a stage in shared memory: rows of HDP elements, chunk u (16 bytes) of row r at place u ^ (r % UNITS).
+    static constexpr int UNITS = HDP / 8;
+    __device__ __forceinline__ void read_k(int s, const uint8_t *stage, int row, int g) {
+#pragma unroll
+        for (int c = 0; c < KC; ++c)
+            k[s][c] = *reinterpret_cast<const u4_t *>(stage + row * HDP * 2 + (((4 * c + g) ^ (row & (UNITS - 1))) << 4));
+    }
+    __device__ __forceinline__ void read_v(int s, const uint8_t *stage, int row, int c16) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int n = 0; n < NB; ++n) {
+                const int at = 32 * W * n + 2 * W * c16;  // byte of the row
+                load_words<W / 2>(stage + (row + i) * HDP * 2 + (((at >> 4) ^ ((row + i) & (UNITS - 1))) << 4) + (at & 15), v[4 * s + i][n]);
             }
     }
     __device__ __forceinline__ void scores(int t, f4_t (&s)[2]) const {
@@ -112,13 +141,18 @@ struct CoreBf16 {
 #pragma unroll
             for (int w = 0; w < W / 2; ++w) v[i][n][w] = keep ? v[i][n][w] : 0u;
     }
-    // whether row i of this lane's values holds an infinity or a NaN
-    __device__ __forceinline__ bool odd(int i) const {
+    // infinities and NaN of row i of this lane's values become zeros (where `on`); whether there were any
+    __device__ __forceinline__ bool clean(int i, bool on) {
         bool bad = false;
 #pragma unroll
         for (int n = 0; n < NB; ++n)
 #pragma unroll
-            for (int w = 0; w < W / 2; ++w) bad |= (v[i][n][w] & 0x7f80u) == 0x7f80u || (v[i][n][w] & 0x7f800000u) == 0x7f800000u;
+            for (int w = 0; w < W / 2; ++w) {
+                uint32_t &x = v[i][n][w];
+                const bool lo = on && (x & 0x7f80u) == 0x7f80u, hi = on && (x & 0x7f800000u) == 0x7f800000u;
+                x &= (lo ? 0xffff0000u : 0xffffffffu) & (hi ? 0x0000ffffu : 0xffffffffu);
+                bad |= lo || hi;
+            }
         return bad;
     }
     struct Weights { b8_t p; };
@@ -128,7 +162,13 @@ struct CoreBf16 {
         for (int i = 0; i < 4; ++i) { x.p[i] = (__bf16)s[0][i]; x.p[4 + i] = (__bf16)s[1][i]; }
         return x;
     }
-    __device__ __forceinline__ static Weights none() { return Weights{b8_t{}}; }
+    // sums of the weights as they were rounded: a product with ones, which leaves a column's whole sum with all its lanes
+    __device__ __forceinline__ static void add_up(const Weights &w, f4_t &l) {
+        const __bf16 one = (__bf16)1.f;
+        const b8_t ones = {one, one, one, one, one, one, one, one};
+        l = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, w.p, l, 0, 0, 0);
+    }
+    __device__ __forceinline__ static float total(const f4_t &l) { return l[0]; }
     // channel pair w of block n, positions turned into rows: the first product operand of channels 2 w and 2 w + 1
     __device__ __forceinline__ void turned(int n, int w, b8_t &even, b8_t &odd_) const {
         u4_t lo, hi;
@@ -162,6 +202,7 @@ template <int HDP_, bool EXACT>
 struct CoreF32 {
     typedef float T;
     static constexpr int HDP = HDP_, QT = 1, W = HDP >= 64 ? 4 : HDP / 16, NB = HDP / (16 * W), KC = HDP / 16;
+    static constexpr bool LATE = HDP == 256;
     f4_t q[1][KC];   // channels 16 c + 4 g ..
     f4_t k[2][KC];
     uint32_t v[8][NB][W];
@@ -194,7 +235,7 @@ struct CoreF32 {
 #pragma unroll
             for (int n = 0; n < NB; ++n) {
                 const int ch = 16 * W * n + W * c16;
-                if (EXACT || ch < hd) load_words<W>(rows + (int64_t)i * hd + ch, v[4 * s + i][n]);
+                if (EXACT || ch < hd) load_words<W>(rows + i * (EXACT ? HDP : hd) + ch, v[4 * s + i][n]);
                 else {
 #pragma unroll
                     for (int w = 0; w < W; ++w) v[4 * s + i][n][w] = 0;
@@ -217,17 +258,22 @@ struct CoreF32 {
 #pragma unroll
             for (int w = 0; w < W; ++w) v[i][n][w] = keep ? v[i][n][w] : 0u;
     }
-    __device__ __forceinline__ bool odd(int i) const {
+    __device__ __forceinline__ bool clean(int i, bool on) {
         bool bad = false;
 #pragma unroll
         for (int n = 0; n < NB; ++n)
 #pragma unroll
-            for (int w = 0; w < W; ++w) bad |= (v[i][n][w] & 0x7f800000u) == 0x7f800000u;
+            for (int w = 0; w < W; ++w) {
+                const bool odd = on && (v[i][n][w] & 0x7f800000u) == 0x7f800000u;
+                v[i][n][w] = odd ? 0u : v[i][n][w];
+                bad |= odd;
+            }
         return bad;
     }
     struct Weights { f4_t p[2]; };
     __device__ __forceinline__ static Weights weights(const f4_t (&s)[2]) { return Weights{{s[0], s[1]}}; }
-    __device__ __forceinline__ static Weights none() { return Weights{{f4_t{0.f, 0.f, 0.f, 0.f}, f4_t{0.f, 0.f, 0.f, 0.f}}}; }
+    __device__ __forceinline__ static void add_up(const Weights &w, f4_t &l) { l += w.p[0] + w.p[1]; }
+    __device__ __forceinline__ static float total(const f4_t &l) { return group_sum((l[0] + l[1]) + (l[2] + l[3])); }
     __device__ __forceinline__ void values(const Weights (&p)[1], f4_t (&o)[1][NB * W]) const {
 #pragma unroll
         for (int i = 0; i < 8; ++i)
@@ -244,7 +290,7 @@ struct OwnParts { int len, chunk, used; };
 __device__ __forceinline__ OwnParts own_parts_of(const SharedAttnArgs &a, int b) {
     OwnParts p;
     p.len = max(0, min(a.own_len[b], a.table_pages << a.page_shift));
-    p.chunk = max(MIN_PART, ((p.len + a.own_parts - 1) / a.own_parts + TILE - 1) & ~(TILE - 1));
+    p.chunk = max(MIN_PART, ((p.len + a.own_parts - 1) / a.own_parts + STAGE - 1) & ~(STAGE - 1));  // stages begin with their pages
     p.used = max(1, (p.len + p.chunk - 1) / p.chunk);
     return p;
 }
@@ -263,6 +309,7 @@ struct Piece {
     int len;                // positions of the prefix or the sequence
     bool own, direct;
     int part, begin, chunk;
+    __device__ __forceinline__ int sees(int row) const { return own ? max(0, len - n + row + 1) : len; }  // positions
 };
 
 // Which piece workgroup `id` has: prefix pieces first, tiles of `cols` columns.  false: none.  Same answer in every wave.
@@ -342,76 +389,110 @@ __device__ __forceinline__ Places places_of(const SharedAttnArgs &a, const Piece
 }
 // element of position t of head h on `page` (page 0 stands in for one outside the pool)
 __device__ __forceinline__ int64_t element(const SharedAttnArgs &a, int page, int h, int t) {
-    const int pg = (uint32_t)page < (uint32_t)a.n_pages ? page : 0;
-    return ((((int64_t)pg * a.nkv + h) << a.page_shift) + (t & ((1 << a.page_shift) - 1))) * a.hd;
+    const uint32_t pg = (uint32_t)page < (uint32_t)a.n_pages ? page : 0;
+    // (slots are below 2^31, and so are slots of all heads below 2^51)
+    return (int64_t)(((uint64_t)(pg * (uint64_t)(uint32_t)a.nkv + (uint32_t)h) << a.page_shift) + (uint32_t)(t & ((1 << a.page_shift) - 1))) * a.hd;
 }
 
-__device__ __forceinline__ float group_max(float x) {
-    x = fmaxf(x, __shfl_xor(x, 16, WAVE));
-    return fmaxf(x, __shfl_xor(x, 32, WAVE));
-}
-__device__ __forceinline__ float group_sum(float x) {
-    x += __shfl_xor(x, 16, WAVE);
-    return x + __shfl_xor(x, 32, WAVE);
-}
-
-// One tile's softmax step of one column tile: scores -> weights, running maximum, sum and results brought up to date.
-template <int NO>
-__device__ __forceinline__ void soften(f4_t (&s)[2], float scale2, float &m, float &l, f4_t (&o)[NO]) {
-    float top = s[0][0];
-#pragma unroll
-    for (int i = 1; i < 8; ++i) top = fmaxf(top, s[i / 4][i % 4]);
-    top = fmaxf(m, group_max(top) * scale2);
-    if (__ballot(top > m)) {
-        const float by = exp2_(m - (top == -INFINITY ? 0.f : top));
-        l *= by;
-#pragma unroll
-        for (int i = 0; i < NO; ++i) o[i] *= by;
-        m = top;
-    }
-    const float base = m == -INFINITY ? 0.f : m;
-    float sum = 0.f;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const float e = exp2_(fmaf(s[i / 4][i % 4], scale2, -base));
-        s[i / 4][i % 4] = e;
-        sum += e;
-    }
-    l += sum;
-}
-
-}  // namespace
-
-// Few columns: the four waves of a workgroup take the same QT x 16 columns and every fourth tile of the positions, and
-// join their sums through shared memory at the end.
+// Reference, sum and results of a wave's columns.  Weights are powers of two over a reference, which follows the maximum
+// at a distance: it moves when a score (in powers of two) lies more than 8 above it, so weights stay below 2^8, which costs
+// no precision, and nearly every tile does without the exchange between lanes and the rescaling.  The test is one of integers:
+// where the bound is positive, floats compare with it as their bits do (a NaN counts as above it).  A reference below -7 would
+// make the bound negative; -7 serves as well down to maxima of -100, the weights being floating point, and below that every
+// tile is compared in full.
 template <class C>
-__global__ __launch_bounds__(256) void attn_split_k(const SharedAttnArgs a) {
-    typedef typename C::T T;
-    constexpr int QT = C::QT, NO = C::NB * C::W, LD = C::HDP + 4;
-    __shared__ float so[4][16][LD];
-    __shared__ float sm[4][QT * 16], sl[4][QT * 16];
-    Piece p;
-    if (!piece_of<QT * 16>(a, workgroup(), p)) return;
-    const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), g = lane >> 4, c16 = lane & 15;
-    const int cols = p.n * a.g, m0 = p.tile * QT * 16;
-    const bool whole = a.q_whole;
-    C core;
-    int lim[QT];  // positions a column sees
-    float m[QT], l[QT];
-    f4_t o[QT][NO];
-    auto sees = [&](int row) { return p.own ? max(0, p.len - p.n + row + 1) : p.len; };
+struct Running {
+    static constexpr int QT = C::QT, NO = C::NB * C::W;
+    float m[QT], base[QT];  // the reference, and -infinity and 0 before there is one
+    int bound[QT];          // scores (not yet scaled) of larger bits move it
+    f4_t l[QT], o[QT][NO];
+    __device__ __forceinline__ void clear() {
 #pragma unroll
-    for (int t = 0; t < QT; ++t) {
-        const int col = min(m0 + 16 * t + c16, cols - 1), row = col / a.g;
-        lim[t] = sees(row);
-        core.load_q(t, reinterpret_cast<const T *>(a.q) + (int64_t)(p.row0 + row) * a.ldq + (int64_t)(p.h * a.g + col % a.g) * a.hd, whole, a.hd, g);
-        m[t] = -INFINITY;
-        l[t] = 0.f;
+        for (int t = 0; t < QT; ++t) {
+            m[t] = -INFINITY;
+            base[t] = 0.f;
+            bound[t] = (int)0x80000000;
+            l[t] = f4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int i = 0; i < NO; ++i) o[t][i] = f4_t{0.f, 0.f, 0.f, 0.f};
+            for (int i = 0; i < NO; ++i) o[t][i] = l[t];
+        }
     }
-    const int least = sees(m0 / a.g), most = sees(min(m0 + QT * 16, cols) - 1) , end = min(p.begin + p.chunk, sees((min(m0 + QT * 16, cols) - 1) / a.g));
-    (void)most;
+    __device__ __forceinline__ void follow(const f4_t (&s)[QT][2], float scale2) {
+        float top[QT];
+        bool above = false;
+#pragma unroll
+        for (int t = 0; t < QT; ++t) {
+            top[t] = s[t][0][0];
+#pragma unroll
+            for (int i = 1; i < 8; ++i) top[t] = fmaxf(top[t], s[t][i / 4][i % 4]);
+            top[t] *= scale2;
+            above |= top[t] > m[t] + 8.f;
+        }
+        if (__ballot(above)) {
+#pragma unroll
+            for (int t = 0; t < QT; ++t) {
+                const float to = fmaxf(m[t], group_max(top[t]));
+                const float ref = to == -INFINITY ? 0.f : to, by = exp2_(m[t] - ref);
+                m[t] = to;
+                base[t] = ref;
+                l[t] *= by;
+#pragma unroll
+                for (int i = 0; i < NO; ++i) o[t][i] *= by;
+            }
+        }
+    }
+    __device__ __forceinline__ void weigh(f4_t (&s)[QT][2], float scale2, typename C::Weights (&w)[QT]) const {
+#pragma unroll
+        for (int t = 0; t < QT; ++t) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) s[t][i / 4][i % 4] = exp2_(fmaf(s[t][i / 4][i % 4], scale2, -base[t]));
+            w[t] = C::weights(s[t]);
+        }
+    }
+    __device__ __forceinline__ void add(const C &core, const typename C::Weights (&w)[QT]) {
+#pragma unroll
+        for (int t = 0; t < QT; ++t) C::add_up(w[t], l[t]);
+        core.values(w, o);
+    }
+};
+
+// Values that are infinite or NaN at positions that some columns of a tile see and others do not: 0 times them would reach the
+// others, so the products have zeros in their place, and at the end every column adds those it sees (times any weight they
+// are what they are).  Positions from .. end - 1, of every `of` tiles those of number `nth`.
+template <class C, int QT = C::QT>
+__device__ __forceinline__ void add_odd(const SharedAttnArgs &a, const Piece &p, int from, int end, int nth, int of, const int (&lim)[QT],
+                                        Running<C> &run) {
+    typedef typename C::T T;
+    const int lane = threadIdx.x & 63, g = lane >> 4;
+    for (int x = max(from, p.begin); x < end; ++x) {
+        if ((x - p.begin) / TILE % of != nth) continue;
+        const int page = p.table[min(x >> a.page_shift, p.pages - 1)];
+        if ((uint32_t)page >= (uint32_t)a.n_pages) continue;
+        const T *row = reinterpret_cast<const T *>(a.v_pages) + element(a, page, p.h, x);
+#pragma unroll
+        for (int n = 0; n < C::NB; ++n)
+#pragma unroll
+            for (int k = 0; k < C::W; ++k)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int ch = 16 * C::W * n + C::W * (4 * g + r) + k;
+                    float v = ch < a.hd ? (float)row[ch] : 0.f;
+                    if ((__float_as_uint(v) & 0x7f800000u) != 0x7f800000u) v = 0.f;
+#pragma unroll
+                    for (int t = 0; t < QT; ++t) run.o[t][n * C::W + k][r] += x < lim[t] ? v : 0.f;
+                }
+    }
+}
+
+// Tiles t0, t0 + step, .. up to `end`, straight from the pages; columns see at least `least` positions.  odd: whether values
+// were left for add_odd().  The loads of a tile are on their way while the one before is worked on: K's from its scores on, V's
+// from its values' product on.
+template <class C>
+__device__ __forceinline__ void walk(const SharedAttnArgs &a, const Piece &p, C &core, const int (&lim)[C::QT], Running<C> &run, int t0, const int step,
+                                     const int end, const int least, int &odd) {
+    typedef typename C::T T;
+    constexpr int QT = C::QT;
+    const int lane = threadIdx.x & 63, g = lane >> 4, c16 = lane & 15;
     const T *kp = reinterpret_cast<const T *>(a.k_pages), *vp = reinterpret_cast<const T *>(a.v_pages);
     auto load_k = [&](const Places &x, int t0) {
 #pragma unroll
@@ -421,79 +502,87 @@ __global__ __launch_bounds__(256) void attn_split_k(const SharedAttnArgs a) {
 #pragma unroll
         for (int s = 0; s < 2; ++s) core.load_v(s, vp + element(a, x.v[s], p.h, t0 + 16 * s + 4 * g), a.hd, c16);
     };
-    int t0 = p.begin + TILE * wave;
-    if (t0 < end) {
-        Places now = places_of(a, p, t0, c16, g), next = places_of(a, p, t0 + 4 * TILE, c16, g);
-        load_k(now, t0);
-        load_v(now, t0);
-        for (; t0 < end; t0 += 4 * TILE) {
-            f4_t s[QT][2];
+    if (t0 >= end) return;
+    Places now = places_of(a, p, t0, c16, g), next = places_of(a, p, t0 + step, c16, g);
+    load_k(now, t0);
+    if constexpr (!C::LATE) load_v(now, t0);
+    for (; t0 < end; t0 += step) {
+        f4_t s[QT][2];
 #pragma unroll
-            for (int t = 0; t < QT; ++t) core.scores(t, s[t]);
-            const int t1 = t0 + 4 * TILE;
-            const bool more = t1 < end;
-            if (more) load_k(next, t1);
-            const bool there[2] = {(uint32_t)now.v[0] < (uint32_t)a.n_pages, (uint32_t)now.v[1] < (uint32_t)a.n_pages};
-            bool apart = false;  // whether a column has to be kept from values that another one sees
-            if (t0 + TILE > least || __ballot(!(there[0] && there[1]))) {
-                bool bad = false;
+        for (int t = 0; t < QT; ++t) core.scores(t, s[t]);
+        const int t1 = t0 + step;
+        const bool more = t1 < end;
+        if constexpr (C::LATE) load_v(now, t0);
+        else if (more) load_k(next, t1);
+        const bool there[2] = {(uint32_t)now.v[0] < (uint32_t)a.n_pages, (uint32_t)now.v[1] < (uint32_t)a.n_pages};
+        if (t0 + TILE > least || __ballot(!(there[0] && there[1]))) {
+            bool bad = false;
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const int at = t0 + 16 * (i / 4) + 4 * g + i % 4;
-                    const bool seen = there[i / 4] && at < end;
+            for (int i = 0; i < 8; ++i) {
+                const int at = t0 + 16 * (i / 4) + 4 * g + i % 4;
+                const bool seen = there[i / 4] && at < end;
 #pragma unroll
-                    for (int t = 0; t < QT; ++t)
-                        if (!seen || at >= lim[t]) s[t][i / 4][i % 4] = -INFINITY;
-                    core.forget(i, seen);
-                    bad |= at >= least && core.odd(i);
-                }
-                apart = __ballot(bad) != 0;
+                for (int t = 0; t < QT; ++t)
+                    if (!seen || at >= lim[t]) s[t][i / 4][i % 4] = -INFINITY;
+                core.forget(i, seen);
+                if (core.clean(i, at >= least)) bad = true;
             }
-            typename C::Weights w[QT];
-#pragma unroll
-            for (int t = 0; t < QT; ++t) {
-                soften<NO>(s[t], a.scale2, m[t], l[t], o[t]);
-                w[t] = C::weights(s[t]);
-            }
-            if (!apart) {
-                core.values(w, o);
-            } else {
-                // an infinity or a NaN that some columns see and others do not: 0 times it would reach those, so each
-                // column is multiplied by itself, with the values it sees
-                for (int c = 0; c < 16; ++c) {
-#pragma unroll
-                    for (int t = 0; t < QT; ++t) {
-                        const int see = __builtin_amdgcn_readlane(lim[t], c);
-                        C alone = core;
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) alone.forget(i, t0 + 16 * (i / 4) + 4 * g + i % 4 < see);
-                        typename C::Weights one[QT];
-                        f4_t sum[QT][NO];
-#pragma unroll
-                        for (int u = 0; u < QT; ++u) {
-                            one[u] = u == t && c16 == c ? w[u] : C::none();
-#pragma unroll
-                            for (int i = 0; i < NO; ++i) sum[u][i] = f4_t{0.f, 0.f, 0.f, 0.f};
-                        }
-                        alone.values(one, sum);
-#pragma unroll
-                        for (int i = 0; i < NO; ++i)
-                            if (c16 == c) o[t][i] += sum[t][i];
-                    }
-                }
-            }
-            if (more) {
-                load_v(next, t1);
-                now = next;
-                next = places_of(a, p, t1 + 4 * TILE, c16, g);
-            }
+            if (__ballot(bad)) odd = 1;
+        }
+        run.follow(s, a.scale2);
+        typename C::Weights w[QT];
+        run.weigh(s, a.scale2, w);
+        run.add(core, w);
+        if (more) {
+            if constexpr (C::LATE) load_k(next, t1);
+            else load_v(next, t1);
+            now = next;
+            next = places_of(a, p, t1 + step, c16, g);
         }
     }
+}
+
+// Queries of a wave's columns from m0 on, and the positions each sees; columns past the last one repeat it.
+template <class C>
+__device__ __forceinline__ void take_columns(const SharedAttnArgs &a, const Piece &p, int m0, C &core, int (&lim)[C::QT]) {
+    const int lane = threadIdx.x & 63, cols = p.n * a.g;
+#pragma unroll
+    for (int t = 0; t < C::QT; ++t) {
+        const int col = min(m0 + 16 * t + (lane & 15), cols - 1), row = col / a.g;
+        lim[t] = p.sees(row);
+        core.load_q(t, reinterpret_cast<const typename C::T *>(a.q) + (int64_t)(p.row0 + row) * a.ldq + (int64_t)(p.h * a.g + col % a.g) * a.hd,
+                    a.q_whole, a.hd, lane >> 4);
+    }
+}
+
+}  // namespace
+
+// Few columns: the four waves of a workgroup take the same QT x 16 columns and every fourth tile of the positions, and
+// join their sums through shared memory at the end.
+template <class C>
+__global__ __launch_bounds__(256, sizeof(typename C::T) == 2 || C::HDP < 128 ? 2 : 1) void attn_split_k(const SharedAttnArgs a) {
+    typedef typename C::T T;
+    constexpr int QT = C::QT, LD = C::HDP + 4;
+    __shared__ float so[4][16][LD];
+    __shared__ float sm[4][QT * 16], sl[4][QT * 16];
+    Piece p;
+    if (!piece_of<QT * 16>(a, workgroup(), p)) return;
+    const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), g = lane >> 4, c16 = lane & 15;
+    const int cols = p.n * a.g, m0 = p.tile * QT * 16;
+    C core;
+    Running<C> run;
+    int lim[QT], odd = 0;
+    take_columns(a, p, m0, core, lim);
+    run.clear();
+    // positions that the first column sees, and those that the last one does within this part
+    const int least = p.sees(m0 / a.g), end = min(p.begin + p.chunk, p.sees((min(m0 + QT * 16, cols) - 1) / a.g));
+    walk(a, p, core, lim, run, p.begin + TILE * wave, 4 * TILE, end, least, odd);
+    if (uniform(odd)) add_odd(a, p, least, end, wave, 4, lim, run);
     // the waves' sums meet: 16 columns at a time
 #pragma unroll
     for (int t = 0; t < QT; ++t) {
-        l[t] = group_sum(l[t]);
-        if (g == 0) { sm[wave][16 * t + c16] = m[t]; sl[wave][16 * t + c16] = l[t]; }
+        const float sum = C::total(run.l[t]);
+        if (g == 0) { sm[wave][16 * t + c16] = run.m[t]; sl[wave][16 * t + c16] = sum; }
     }
     const int parts = a.prefix_parts + a.own_parts, my = threadIdx.x >> 4, sub = threadIdx.x & 15;
 #pragma unroll
@@ -504,7 +593,7 @@ __global__ __launch_bounds__(256) void attn_split_k(const SharedAttnArgs a) {
 #pragma unroll
             for (int r = 0; r < 4; ++r)
 #pragma unroll
-                for (int w = 0; w < C::W; ++w) so[wave][c16][16 * C::W * n + C::W * (4 * g + r) + w] = o[t][n * C::W + w][r];
+                for (int w = 0; w < C::W; ++w) so[wave][c16][16 * C::W * n + C::W * (4 * g + r) + w] = run.o[t][n * C::W + w][r];
         __syncthreads();
         const int col = m0 + 16 * t + my;
         if (col >= cols) continue;
@@ -518,7 +607,7 @@ __global__ __launch_bounds__(256) void attn_split_k(const SharedAttnArgs a) {
         }
         const int row = p.row0 + col / a.g, head = p.h * a.g + col % a.g;
         if (p.direct) {
-            const float inv = sum == 0.f ? 0.f : 1.f / sum;
+            const float inv = 1.f / sum;
             T *dst = reinterpret_cast<T *>(a.out) + (int64_t)row * a.ldo + (int64_t)head * a.hd;
             for (int ch = sub; ch < a.hd; ch += 16) {
                 float x = 0.f;
@@ -537,6 +626,187 @@ __global__ __launch_bounds__(256) void attn_split_k(const SharedAttnArgs a) {
             }
             if (sub == 0) *reinterpret_cast<f2_t *>(a.part_ml + 2 * at) = f2_t{top, sum};
         }
+    }
+}
+
+// f(num<0>) .. f(num<N - 1>)
+template <int N> using num = std::integral_constant<int, N>;
+template <int N, typename F>
+__device__ __forceinline__ void each(F f) {
+    if constexpr (N > 0) {
+        each<N - 1>(f);
+        f(num<N - 1>());
+    }
+}
+
+// The copies of this wave have arrived, and with the barrier those of all waves.
+__device__ __forceinline__ void meet() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");  // no instruction: keeps memory operations on their side
+    __builtin_amdgcn_s_waitcnt(0x0070);                     // vmcnt(0), lgkmcnt(0)
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
+// Many columns: every wave has QT x 16 of its own, and those of a workgroup share the positions, which pass through shared
+// memory in stages of 64, three in turn.  The loop is for whole stages that all columns see; the positions behind them, and
+// pieces with pages outside the pool, follow stage by stage.
+template <int HDP, int QT, int WAVES, bool EXACT>
+__global__ __launch_bounds__(64 * WAVES, WAVES / 4) void attn_share_k(const SharedAttnArgs a) {
+    typedef CoreBf16<HDP, QT, EXACT> C;
+    typedef __bf16 T;
+    constexpr int UNITS = C::UNITS, BYTES = STAGE * HDP * 2, SHARE = WAVES * 1024, COPIES = BYTES / SHARE, COLS = 16 * QT * WAVES;
+    static_assert(COPIES >= 1 && BYTES % SHARE == 0, "every thread copies");
+    __shared__ __attribute__((aligned(16))) uint8_t k0[BYTES], k1[BYTES], k2[BYTES], v0[BYTES], v1[BYTES], v2[BYTES];
+    Piece p;
+    if (!piece_of<COLS>(a, workgroup(), p)) return;
+    const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), g = lane >> 4, c16 = lane & 15;
+    const int cols = p.n * a.g, first = p.tile * COLS, m0 = first + wave * 16 * QT;
+    C core;
+    Running<C> run;
+    int lim[QT], odd = 0;
+    take_columns(a, p, m0, core, lim);
+    run.clear();
+    // positions: of the part that some column sees, and stages that all columns see
+    const int end = min(p.begin + p.chunk, p.sees((min(first + COLS, cols) - 1) / a.g));
+    const int all = (max(0, end - p.begin) + STAGE - 1) / STAGE;
+    int stages = max(0, min(end, p.sees(first / a.g)) - p.begin) / STAGE;
+    if (stages > 0) {  // every wave looks at the same pages and comes to the same answer
+        bool gone = false;
+        const int last = (p.begin + stages * STAGE - 1) >> a.page_shift;
+        for (int i = (p.begin >> a.page_shift) + lane; i <= last; i += 64) gone |= (uint32_t)p.table[min(i, p.pages - 1)] >= (uint32_t)a.n_pages;
+        if (__ballot(gone)) stages = 0;
+    }
+    if constexpr (!EXACT) {  // chunks beyond hd are never copied: the products need numbers there
+        uint8_t *every[6] = {k0, k1, k2, v0, v1, v2};
+#pragma unroll
+        for (int i = 0; i < 6; ++i)
+            for (int b = threadIdx.x * 16; b < BYTES; b += SHARE) *reinterpret_cast<u4_t *>(every[i] + b) = u4_t{0, 0, 0, 0};
+        __syncthreads();
+    }
+    const T *kp = reinterpret_cast<const T *>(a.k_pages), *vp = reinterpret_cast<const T *>(a.v_pages);
+    auto page_at = [&](int st) { return p.table[min((p.begin + st * STAGE + lane) >> a.page_shift, p.pages - 1)]; };
+    auto copy = [&](int st, int page, uint8_t *ks, uint8_t *vs) {
+        const int t0 = p.begin + st * STAGE;
+        const int64_t whole = a.page_shift >= 6 ? element(a, uniform(page), p.h, t0) : 0;
+        // what this thread copies: rows i * SHARE / 16 / UNITS + mine, one chunk each (worked out anew each time: the loop has no
+        // registers left to keep it)
+        int own = lane;
+        asm volatile("" : "+v"(own));
+        const int mine = (wave * 64 + own) / UNITS, place = own % UNITS;
+#pragma unroll
+        for (int i = 0; i < COPIES; ++i) {
+            const int row = i * (SHARE / 16 / UNITS) + mine, chunk = place ^ (row & (UNITS - 1));
+            int64_t at;
+            if (a.page_shift >= 6) at = whole + row * (EXACT ? HDP : a.hd) + chunk * 8;
+            else at = element(a, __shfl(page, row, WAVE), p.h, t0 + row) + chunk * 8;
+            if (EXACT || chunk * 8 < a.hd) {
+                __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(kp + at),
+                                                 (__attribute__((address_space(3))) void *)(ks + i * SHARE + wave * 1024), 16, 0, 0);
+                __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(vp + at),
+                                                 (__attribute__((address_space(3))) void *)(vs + i * SHARE + wave * 1024), 16, 0, 0);
+            }
+        }
+    };
+    f4_t s[2][QT][2];
+    auto scores = [&](const uint8_t *ks, int half, f4_t (&to)[QT][2]) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) core.read_k(h, ks, 32 * half + 16 * h + c16, g);
+#pragma unroll
+        for (int t = 0; t < QT; ++t) core.scores(t, to[t]);
+    };
+    if (stages > 0) {
+        auto kst = [&](auto n) -> uint8_t * { return n % 3 == 0 ? k0 : n % 3 == 1 ? k1 : k2; };
+        auto vst = [&](auto n) -> uint8_t * { return n % 3 == 0 ? v0 : n % 3 == 1 ? v1 : v2; };
+        // one half of a stage, whose scores are there; `next` computes those of the half behind it meanwhile
+        auto half_step = [&](const uint8_t *vs, int half, f4_t (&x)[QT][2], auto next) {
+            run.follow(x, a.scale2);
+            next();
+            typename C::Weights w[QT];
+            run.weigh(x, a.scale2, w);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) core.read_v(h, vs, 32 * half + 16 * h + 4 * g, c16);
+            run.add(core, w);
+        };
+        int page = page_at(1);  // of the stage after the next copy's
+        copy(0, page_at(0), k0, v0);
+        if (stages > 1) copy(1, page, k1, v1);
+        page = page_at(2);
+        meet();
+        scores(k0, 0, s[0]);
+        for (int st0 = 0; st0 < stages; st0 += 3) {
+            each<3>([&](auto n) {
+                const int st = st0 + n;
+                if (st >= stages) return;
+                half_step(vst(n), 0, s[0], [&]() { scores(kst(n), 1, s[1]); });
+                // the next stage has arrived; the one before this has been read by all
+                meet();
+                if (st + 2 < stages) {
+                    copy(st + 2, page, kst(num<n + 2>()), vst(num<n + 2>()));
+                    page = page_at(st + 3);
+                }
+                // (behind the last stage: scores of an old one, which nobody reads)
+                half_step(vst(n), 1, s[1], [&]() { scores(kst(num<n + 1>()), 0, s[0]); });
+            });
+        }
+    }
+    const int least = p.sees(min(m0, cols - 1) / a.g);  // positions that all of this wave's columns see
+    for (int st = stages; st < all; ++st) {
+        const int page = page_at(st);
+        const uint64_t there = __ballot((uint32_t)page < (uint32_t)a.n_pages);
+        __syncthreads();
+        copy(st, page, k0, v0);
+        meet();
+#pragma unroll 1
+        for (int half = 0; half < 2; ++half) {
+            const int t0 = p.begin + st * STAGE + 32 * half;
+            scores(k0, half, s[0]);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) core.read_v(h, v0, 32 * half + 16 * h + 4 * g, c16);
+            bool bad = false;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int pos = 16 * (i / 4) + 4 * g + i % 4;
+                const bool seen = (there >> (32 * half + pos) & 1) && t0 + pos < end;
+#pragma unroll
+                for (int t = 0; t < QT; ++t)
+                    if (!seen || t0 + pos >= lim[t]) s[0][t][i / 4][i % 4] = -INFINITY;
+                core.forget(i, seen);
+                if (core.clean(i, t0 + pos >= least)) bad = true;
+            }
+            if (__ballot(bad)) odd = 1;
+            run.follow(s[0], a.scale2);
+            typename C::Weights w[QT];
+            run.weigh(s[0], a.scale2, w);
+            run.add(core, w);
+        }
+    }
+    if (uniform(odd)) add_odd(a, p, max(least, p.begin + stages * STAGE), end, 0, 1, lim, run);
+    const int parts = a.prefix_parts + a.own_parts;
+#pragma unroll
+    for (int t = 0; t < QT; ++t) {
+        const int col = m0 + 16 * t + c16;
+        if (col >= cols) continue;
+        const int row = p.row0 + col / a.g, head = p.h * a.g + col % a.g;
+        const float sum = C::total(run.l[t]), inv = 1.f / sum;
+        const int64_t at = ((int64_t)row * a.nq + head) * parts + p.part;
+        float *po = a.part_o + at * a.hd;
+        T *out = reinterpret_cast<T *>(a.out) + (int64_t)row * a.ldo + (int64_t)head * a.hd;
+        if (!p.direct && g == 0) *reinterpret_cast<f2_t *>(a.part_ml + 2 * at) = f2_t{run.m[t], sum};
+#pragma unroll
+        for (int n = 0; n < C::NB; ++n)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int ch = 16 * C::W * n + C::W * (4 * g + r);
+                if (!EXACT && ch >= a.hd) continue;
+                if (p.direct) {
+#pragma unroll
+                    for (int w = 0; w < C::W; ++w) out[ch + w] = (T)(sum == 0.f ? 0.f : run.o[t][n * C::W + w][r] * inv);
+                } else {
+#pragma unroll
+                    for (int w = 0; w < C::W; ++w) po[ch + w] = run.o[t][n * C::W + w][r];
+                }
+            }
     }
 }
 
@@ -583,27 +853,43 @@ __global__ __launch_bounds__(256) void attn_join_k(const SharedAttnArgs a) {
 
 // Parts and tiles of a call; a function of the sizes alone, so that the workspace is known beforehand.
 void plan_shared_attention(SharedAttnArgs &a, int64_t own_capacity) {
-    const int64_t columns = (int64_t)a.R * a.g;
-    a.qt = a.dtype == DT_BF16 && columns > (int64_t)16 * a.n_seq ? 2 : 1;
-    const int64_t cols = 16 * a.qt;
-    const int64_t tiles = (columns + cols - 1) / cols;
-    auto parts = [&](int64_t positions, int64_t groups) {
-        groups = std::max<int64_t>(groups, 1);
-        const int64_t want = (1024 + groups - 1) / groups, most = (positions + MIN_PART - 1) / MIN_PART;
-        return std::max<int64_t>(1, std::min<int64_t>({want, most, MAX_PARTS}));
+    const int64_t columns = (int64_t)a.R * a.g, each_seq = columns / a.n_seq;  // of a cache head; of one sequence, on average
+    // Columns a workgroup takes: 16 or 32 where its waves split the positions, 64, 128 or 256 where they share them.
+    auto kind = [&](int64_t n) {
+        if (a.dtype != DT_BF16) return 16;
+        if (n >= 64 && a.hd <= 128) return n > 128 ? 256 : n > 64 ? 128 : 64;
+        return n > 16 && a.hd <= 128 ? 32 : 16;
     };
-    a.prefix_parts = 0;
-    a.prefix_chunk = 0;
+    auto parts = [&](int64_t positions, int64_t groups, int cols) -> int64_t {
+        groups = std::max<int64_t>(groups, 1);
+        const int64_t most = std::min<int64_t>((positions + MIN_PART - 1) / MIN_PART, MAX_PARTS);
+        if (cols < 64) return std::max<int64_t>(1, std::min((1024 + groups - 1) / groups, most));
+        // one workgroup a compute unit: rounds of 256, each as long as a part and a start (two stages' time)
+        int64_t best = 1;
+        double least = 1e300;
+        const double stages = (double)((positions + STAGE - 1) / STAGE);
+        for (int64_t n = 1; n <= most; ++n) {
+            const double cost = (double)((groups * n + 255) / 256) * (std::ceil(stages / n) + 2.0) + 0.5 * n;
+            if (cost < least) { least = cost; best = n; }
+        }
+        return best;
+    };
+    a.prefix_parts = a.own_parts = a.prefix_chunk = 0;
+    a.prefix_groups64 = a.own_groups64 = 0;
+    a.prefix_cols = kind(columns);
+    a.own_cols = kind(each_seq);
     if (a.prefix_len > 0) {
-        const int64_t n = parts(a.prefix_len, tiles * a.nkv);
-        a.prefix_chunk = (int)(((a.prefix_len + n - 1) / n + TILE - 1) / TILE * TILE);
+        const int64_t tiles = (columns + a.prefix_cols - 1) / a.prefix_cols, n = parts(a.prefix_len, tiles * a.nkv, a.prefix_cols);
+        a.prefix_chunk = (int)(((a.prefix_len + n - 1) / n + STAGE - 1) / STAGE * STAGE);
         a.prefix_parts = (a.prefix_len + a.prefix_chunk - 1) / a.prefix_chunk;
+        a.prefix_groups64 = tiles * a.nkv * a.prefix_parts;
     }
-    a.own_tiles = (uint32_t)(a.n_seq + columns / cols);
-    a.own_parts = own_capacity > 0 ? (int)parts(own_capacity, std::max<int64_t>(tiles, a.n_seq) * a.nkv) : 0;
-    // (prefix_groups, own_groups beyond 2^31 are refused by the launcher)
-    a.prefix_groups64 = a.prefix_len > 0 ? tiles * a.nkv * a.prefix_parts : 0;
-    a.own_groups64 = (int64_t)a.own_tiles * a.nkv * a.own_parts;
+    a.own_tiles = (uint32_t)(a.n_seq + columns / a.own_cols);
+    if (own_capacity > 0) {
+        const int64_t tiles = std::max<int64_t>((columns + a.own_cols - 1) / a.own_cols, a.n_seq);
+        a.own_parts = (int)parts(own_capacity, tiles * a.nkv, a.own_cols);
+        a.own_groups64 = (int64_t)a.own_tiles * a.nkv * a.own_parts;
+    }
     a.prefix_groups = (uint32_t)a.prefix_groups64;
 }
 
@@ -612,30 +898,44 @@ int64_t shared_attention_parts(const SharedAttnArgs &a) {
     return a.prefix_parts == 0 && a.own_parts <= 1 ? 0 : n;
 }
 
-template <class C>
-static hipError_t launch_split(const SharedAttnArgs &a, hipStream_t s) {
-    hipLaunchKernelGGL((attn_split_k<C>), grid_of(a.prefix_groups64 + a.own_groups64), dim3(256), 0, s, a);
+// `groups` workgroups of one width
+template <int HDP, bool EXACT>
+static hipError_t launch_cols(const SharedAttnArgs &a, int cols, int64_t groups, hipStream_t s) {
+    const dim3 grid = grid_of(groups), block(256);
+    if constexpr (HDP <= 128) {
+        switch (a.dtype == DT_F32 ? 0 : cols) {
+            case 256: hipLaunchKernelGGL((attn_share_k<HDP, HDP == 32 ? 4 : 2, HDP == 32 ? 4 : 8, EXACT>), grid, dim3(HDP == 32 ? 256 : 512), 0, s, a); return hipGetLastError();
+            case 128: hipLaunchKernelGGL((attn_share_k<HDP, 2, 4, EXACT>), grid, block, 0, s, a); return hipGetLastError();
+            case 64: hipLaunchKernelGGL((attn_share_k<HDP, 1, 4, EXACT>), grid, block, 0, s, a); return hipGetLastError();
+            case 32: hipLaunchKernelGGL((attn_split_k<CoreBf16<HDP, 2, EXACT>>), grid, block, 0, s, a); return hipGetLastError();
+            default: break;
+        }
+    }
+    if (a.dtype == DT_F32) hipLaunchKernelGGL((attn_split_k<CoreF32<HDP, EXACT>>), grid, block, 0, s, a);
+    else hipLaunchKernelGGL((attn_split_k<CoreBf16<HDP, 1, EXACT>>), grid, block, 0, s, a);
     return hipGetLastError();
 }
 
-template <int HDP, bool EXACT>
-static hipError_t launch_core(const SharedAttnArgs &a, hipStream_t s) {
-    if (a.dtype == DT_F32) return launch_split<CoreF32<HDP, EXACT>>(a, s);
-    if (a.qt == 1) return launch_split<CoreBf16<HDP, 1, EXACT>>(a, s);
-    return launch_split<CoreBf16<HDP, 2, EXACT>>(a, s);
+static hipError_t launch_head(const SharedAttnArgs &a, int cols, int64_t groups, hipStream_t s) {
+    if (groups == 0) return hipSuccess;
+    if (a.hd <= 32) return a.hd == 32 ? launch_cols<32, true>(a, cols, groups, s) : launch_cols<32, false>(a, cols, groups, s);
+    if (a.hd <= 64) return a.hd == 64 ? launch_cols<64, true>(a, cols, groups, s) : launch_cols<64, false>(a, cols, groups, s);
+    if (a.hd <= 128) return a.hd == 128 ? launch_cols<128, true>(a, cols, groups, s) : launch_cols<128, false>(a, cols, groups, s);
+    return a.hd == 256 ? launch_cols<256, true>(a, cols, groups, s) : launch_cols<256, false>(a, cols, groups, s);
 }
 
-template <int HDP>
-static hipError_t launch_exact(const SharedAttnArgs &a, hipStream_t s) {
-    return a.hd == HDP ? launch_core<HDP, true>(a, s) : launch_core<HDP, false>(a, s);
-}
-
-hipError_t launch_shared_attention(const SharedAttnArgs &a, hipStream_t s) {
+hipError_t launch_shared_attention(const SharedAttnArgs &args, hipStream_t s) {
+    SharedAttnArgs a = args;
     if (a.prefix_groups64 + a.own_groups64 > 0x7fffffff) return hipErrorInvalidValue;
-    if (a.prefix_groups64 + a.own_groups64 > 0) {
-        const hipError_t e = a.hd <= 32 ? launch_exact<32>(a, s) : a.hd <= 64 ? launch_exact<64>(a, s) : a.hd <= 128 ? launch_exact<128>(a, s) : launch_exact<256>(a, s);
-        if (e != hipSuccess) return e;
+    hipError_t e;
+    if (a.prefix_cols == a.own_cols) {  // both in one launch
+        e = launch_head(a, a.own_cols, a.prefix_groups64 + a.own_groups64, s);
+    } else {
+        e = launch_head(a, a.prefix_cols, a.prefix_groups64, s);
+        a.prefix_groups = 0;
+        if (e == hipSuccess) e = launch_head(a, a.own_cols, a.own_groups64, s);
     }
+    if (e != hipSuccess) return e;
     if (a.prefix_parts == 0 && a.own_parts == 1) return hipSuccess;  // every row is written by its only part
     const dim3 grid = grid_of(((int64_t)a.R * a.nq + 3) / 4);
     if (a.dtype == DT_F32) hipLaunchKernelGGL((attn_join_k<float>), grid, dim3(256), 0, s, a);
