@@ -71,6 +71,8 @@ struct CoreBf16 {
     typedef __bf16 T;
     static constexpr int HDP = HDP_, QT = QT_, W = HDP >= 128 ? 8 : HDP / 16, NB = HDP / (16 * W), KC = HDP / 32;
     static constexpr bool LATE = HDP == 256;  // walk() loads V when K's registers are free: both do not fit
+    // channel of row r of a lane's i-th block of results
+    __device__ __forceinline__ static int channel(int i, int r, int g) { return 16 * W * (i / W) + W * (4 * g + r) + i % W; }
     b8_t q[QT][KC];
     u4_t k[2][KC];            // positions lane % 16 of the tile's two sixteens, channels 32 c + 8 g ..
     uint32_t v[8][NB][W / 2]; // positions 4 g + i of the first (i < 4) and second sixteen, channels W (lane % 16) ..
@@ -109,22 +111,6 @@ struct CoreBf16 {
 #pragma unroll
                     for (int w = 0; w < W / 2; ++w) v[4 * s + i][n][w] = 0;
                 }
-            }
-    }
-    // The same from a stage in shared memory: rows of HDP elements, chunk u (16 bytes) of row r at place u ^ (r % UNITS).
-    static constexpr int UNITS = HDP / 8;
-    __device__ __forceinline__ void read_k(int s, const uint8_t *stage, int row, int g) {
-#pragma unroll
-        for (int c = 0; c < KC; ++c)
-            k[s][c] = *reinterpret_cast<const u4_t *>(stage + row * HDP * 2 + (((4 * c + g) ^ (row & (UNITS - 1))) << 4));
-    }
-    __device__ __forceinline__ void read_v(int s, const uint8_t *stage, int row, int c16) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-            for (int n = 0; n < NB; ++n) {
-                const int at = 32 * W * n + 2 * W * c16;  // byte of the row
-                load_words<W / 2>(stage + (row + i) * HDP * 2 + (((at >> 4) ^ ((row + i) & (UNITS - 1))) << 4) + (at & 15), v[4 * s + i][n]);
             }
     }
     __device__ __forceinline__ void scores(int t, f4_t (&s)[2]) const {
@@ -197,12 +183,76 @@ struct CoreBf16 {
     }
 };
 
+// The same with positions that lie in shared memory, rows of HDP elements.  Values are read turned (a lane's address names four
+// channels of a row, and it gets one channel of four rows), so channels stay in their order.  Chunk u (16 bytes) of row r is at
+// place u ^ turn(r), which spreads over all banks both the eight rows of one chunk that an eighth of a key load reads and the
+// four rows of two chunks that a quarter of a value load does.
+template <int HDP_, int QT_, bool EXACT>
+struct CoreLds : CoreBf16<HDP_, QT_, EXACT> {
+    typedef CoreBf16<HDP_, QT_, EXACT> Base;
+    static constexpr int HDP = HDP_, QT = QT_, KC = Base::KC, W = 1, NB = HDP / 16, UNITS = HDP / 8;
+    uint32_t v[NB][4];  // channel 16 n + lane % 16, positions 4 g .. + 3 of the first and the second sixteen
+    __device__ __forceinline__ static int channel(int i, int r, int g) { return 16 * i + 4 * g + r; }
+    __device__ __forceinline__ static int turn(int row) {
+        return UNITS == 4 ? (row & 2) | (row >> 2 & 1) : ((row & 3) << 1 | (row >> 2 & 1) | (row & 8)) & (UNITS - 1);
+    }
+    __device__ __forceinline__ void read_k(int s, const uint8_t *stage, int row, int g) {
+#pragma unroll
+        for (int c = 0; c < KC; ++c) this->k[s][c] = *reinterpret_cast<const u4_t *>(stage + row * HDP * 2 + (((4 * c + g) ^ turn(row)) << 4));
+    }
+    __device__ __forceinline__ void read_v(const uint8_t *stage, int row0, int g, int c16) {
+        typedef short s4_t __attribute__((ext_vector_type(4)));
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            const int row = row0 + 16 * s + 4 * g + (c16 >> 2);
+#pragma unroll
+            for (int n = 0; n < NB; ++n) {
+                const uint8_t *from = stage + row * HDP * 2 + (((2 * n + (c16 >> 1 & 1)) ^ turn(row)) << 4) + 8 * (c16 & 1);
+                const uint2 x = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s4_t *)from));
+                v[n][2 * s] = x.x;
+                v[n][2 * s + 1] = x.y;
+            }
+        }
+    }
+    // positions i of this lane's (bit i of `keep` off) become zeros
+    __device__ __forceinline__ void forget(uint32_t keep) {
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            const uint32_t both = (keep >> 2 * w & 1 ? 0x0000ffffu : 0u) | (keep >> (2 * w + 1) & 1 ? 0xffff0000u : 0u);
+#pragma unroll
+            for (int n = 0; n < NB; ++n) v[n][w] &= both;
+        }
+    }
+    // infinities and NaN at positions whose bit is on become zeros; whether there were any
+    __device__ __forceinline__ bool clean(uint32_t on) {
+        bool bad = false;
+#pragma unroll
+        for (int w = 0; w < 4; ++w)
+#pragma unroll
+            for (int n = 0; n < NB; ++n) {
+                uint32_t &x = v[n][w];
+                const bool lo = (on >> 2 * w & 1) && (x & 0x7f80u) == 0x7f80u, hi = (on >> (2 * w + 1) & 1) && (x & 0x7f800000u) == 0x7f800000u;
+                x &= (lo ? 0xffff0000u : 0xffffffffu) & (hi ? 0x0000ffffu : 0xffffffffu);
+                bad |= lo || hi;
+            }
+        return bad;
+    }
+    __device__ __forceinline__ void values(const typename Base::Weights (&p)[QT], f4_t (&o)[QT][NB]) const {
+#pragma unroll
+        for (int n = 0; n < NB; ++n)
+#pragma unroll
+            for (int t = 0; t < QT; ++t)
+                o[t][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(b8_t, u4_t{v[n][0], v[n][1], v[n][2], v[n][3]}), p[t].p, o[t][n], 0, 0, 0);
+    }
+};
+
 // The same in fp32: 16 x 16 x 4 instructions, their four channels (positions) those of the four groups of lanes.
 template <int HDP_, bool EXACT>
 struct CoreF32 {
     typedef float T;
     static constexpr int HDP = HDP_, QT = 1, W = HDP >= 64 ? 4 : HDP / 16, NB = HDP / (16 * W), KC = HDP / 16;
     static constexpr bool LATE = HDP == 256;
+    __device__ __forceinline__ static int channel(int i, int r, int g) { return 16 * W * (i / W) + W * (4 * g + r) + i % W; }
     f4_t q[1][KC];   // channels 16 c + 4 g ..
     f4_t k[2][KC];
     uint32_t v[8][NB][W];
@@ -395,23 +445,19 @@ __device__ __forceinline__ int64_t element(const SharedAttnArgs &a, int page, in
 }
 
 // Reference, sum and results of a wave's columns.  Weights are powers of two over a reference, which follows the maximum
-// at a distance: it moves when a score (in powers of two) lies more than 8 above it, so weights stay below 2^8, which costs
-// no precision, and nearly every tile does without the exchange between lanes and the rescaling.  The test is one of integers:
-// where the bound is positive, floats compare with it as their bits do (a NaN counts as above it).  A reference below -7 would
-// make the bound negative; -7 serves as well down to maxima of -100, the weights being floating point, and below that every
-// tile is compared in full.
+// at a distance: it moves when a score (in powers of two) lies more than 8 above it.  Weights stay below 2^8, which costs no
+// precision, and most tiles need neither the exchange between lanes nor the rescaling.
 template <class C>
 struct Running {
     static constexpr int QT = C::QT, NO = C::NB * C::W;
-    float m[QT], base[QT];  // the reference, and -infinity and 0 before there is one
-    int bound[QT];          // scores (not yet scaled) of larger bits move it
+    float m[QT], base[QT];  // the reference: -infinity and 0 before there is one
+    float bound[QT];        // scores, not yet scaled, that move it
     f4_t l[QT], o[QT][NO];
     __device__ __forceinline__ void clear() {
 #pragma unroll
         for (int t = 0; t < QT; ++t) {
-            m[t] = -INFINITY;
+            m[t] = bound[t] = -INFINITY;
             base[t] = 0.f;
-            bound[t] = (int)0x80000000;
             l[t] = f4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int i = 0; i < NO; ++i) o[t][i] = l[t];
@@ -425,16 +471,16 @@ struct Running {
             top[t] = s[t][0][0];
 #pragma unroll
             for (int i = 1; i < 8; ++i) top[t] = fmaxf(top[t], s[t][i / 4][i % 4]);
-            top[t] *= scale2;
-            above |= top[t] > m[t] + 8.f;
+            above |= top[t] > bound[t];
         }
         if (__ballot(above)) {
 #pragma unroll
             for (int t = 0; t < QT; ++t) {
-                const float to = fmaxf(m[t], group_max(top[t]));
+                const float to = fmaxf(m[t], group_max(top[t]) * scale2);
                 const float ref = to == -INFINITY ? 0.f : to, by = exp2_(m[t] - ref);
                 m[t] = to;
                 base[t] = ref;
+                bound[t] = (to + 8.f) * __builtin_amdgcn_rcpf(scale2);
                 l[t] *= by;
 #pragma unroll
                 for (int i = 0; i < NO; ++i) o[t][i] *= by;
@@ -470,17 +516,15 @@ __device__ __forceinline__ void add_odd(const SharedAttnArgs &a, const Piece &p,
         if ((uint32_t)page >= (uint32_t)a.n_pages) continue;
         const T *row = reinterpret_cast<const T *>(a.v_pages) + element(a, page, p.h, x);
 #pragma unroll
-        for (int n = 0; n < C::NB; ++n)
+        for (int i = 0; i < C::NB * C::W; ++i)
 #pragma unroll
-            for (int k = 0; k < C::W; ++k)
+            for (int r = 0; r < 4; ++r) {
+                const int ch = C::channel(i, r, g);
+                float v = ch < a.hd ? (float)row[ch] : 0.f;
+                if ((__float_as_uint(v) & 0x7f800000u) != 0x7f800000u) v = 0.f;
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int ch = 16 * C::W * n + C::W * (4 * g + r) + k;
-                    float v = ch < a.hd ? (float)row[ch] : 0.f;
-                    if ((__float_as_uint(v) & 0x7f800000u) != 0x7f800000u) v = 0.f;
-#pragma unroll
-                    for (int t = 0; t < QT; ++t) run.o[t][n * C::W + k][r] += x < lim[t] ? v : 0.f;
-                }
+                for (int t = 0; t < QT; ++t) run.o[t][i][r] += x < lim[t] ? v : 0.f;
+            }
     }
 }
 
@@ -647,12 +691,17 @@ __device__ __forceinline__ void meet() {
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
 
+// 16 bytes a lane from memory to a wave's KiB of shared memory, without passing through registers
+__device__ __forceinline__ void copy16(const void *from, uint8_t *to) {
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)from, (__attribute__((address_space(3))) void *)to, 16, 0, 0);
+}
+
 // Many columns: every wave has QT x 16 of its own, and those of a workgroup share the positions, which pass through shared
 // memory in stages of 64, three in turn.  The loop is for whole stages that all columns see; the positions behind them, and
 // pieces with pages outside the pool, follow stage by stage.
 template <int HDP, int QT, int WAVES, bool EXACT>
 __global__ __launch_bounds__(64 * WAVES, WAVES / 4) void attn_share_k(const SharedAttnArgs a) {
-    typedef CoreBf16<HDP, QT, EXACT> C;
+    typedef CoreLds<HDP, QT, EXACT> C;
     typedef __bf16 T;
     constexpr int UNITS = C::UNITS, BYTES = STAGE * HDP * 2, SHARE = WAVES * 1024, COPIES = BYTES / SHARE, COLS = 16 * QT * WAVES;
     static_assert(COPIES >= 1 && BYTES % SHARE == 0, "every thread copies");
@@ -685,25 +734,31 @@ __global__ __launch_bounds__(64 * WAVES, WAVES / 4) void attn_share_k(const Shar
     }
     const T *kp = reinterpret_cast<const T *>(a.k_pages), *vp = reinterpret_cast<const T *>(a.v_pages);
     auto page_at = [&](int st) { return p.table[min((p.begin + st * STAGE + lane) >> a.page_shift, p.pages - 1)]; };
+    // what this thread copies of a stage: one chunk each of rows i * STEP + mine
+    constexpr int STEP = SHARE / 16 / UNITS;
+    static_assert(STEP % 16 == 0, "the chunk is the same in each of them");
+    const int mine = (wave * 64 + lane) / UNITS, chunk = lane % UNITS ^ C::turn(mine), step = STEP * (EXACT ? HDP : a.hd);
+    const uint32_t at = mine * (EXACT ? HDP : a.hd) + chunk * 8;
     auto copy = [&](int st, int page, uint8_t *ks, uint8_t *vs) {
         const int t0 = p.begin + st * STAGE;
-        const int64_t whole = a.page_shift >= 6 ? element(a, uniform(page), p.h, t0) : 0;
-        // what this thread copies: rows i * SHARE / 16 / UNITS + mine, one chunk each (worked out anew each time: the loop has no
-        // registers left to keep it)
-        int own = lane;
-        asm volatile("" : "+v"(own));
-        const int mine = (wave * 64 + own) / UNITS, place = own % UNITS;
+        const bool there = EXACT || chunk * 8 < a.hd;
+        if (a.page_shift >= 6) {  // one page
+            const int64_t whole = element(a, uniform(page), p.h, t0);
+            if (there) {
 #pragma unroll
-        for (int i = 0; i < COPIES; ++i) {
-            const int row = i * (SHARE / 16 / UNITS) + mine, chunk = place ^ (row & (UNITS - 1));
-            int64_t at;
-            if (a.page_shift >= 6) at = whole + row * (EXACT ? HDP : a.hd) + chunk * 8;
-            else at = element(a, __shfl(page, row, WAVE), p.h, t0 + row) + chunk * 8;
-            if (EXACT || chunk * 8 < a.hd) {
-                __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(kp + at),
-                                                 (__attribute__((address_space(3))) void *)(ks + i * SHARE + wave * 1024), 16, 0, 0);
-                __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(vp + at),
-                                                 (__attribute__((address_space(3))) void *)(vs + i * SHARE + wave * 1024), 16, 0, 0);
+                for (int i = 0; i < COPIES; ++i) {
+                    copy16(kp + whole + i * step + at, ks + i * SHARE + wave * 1024);
+                    copy16(vp + whole + i * step + at, vs + i * SHARE + wave * 1024);
+                }
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < COPIES; ++i) {  // (every lane takes part in the exchange)
+                const int64_t from = element(a, __shfl(page, i * STEP + mine, WAVE), p.h, t0 + i * STEP + mine) + chunk * 8;
+                if (there) {
+                    copy16(kp + from, ks + i * SHARE + wave * 1024);
+                    copy16(vp + from, vs + i * SHARE + wave * 1024);
+                }
             }
         }
     };
@@ -723,9 +778,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES / 4) void attn_share_k(const Shar
             next();
             typename C::Weights w[QT];
             run.weigh(x, a.scale2, w);
-            __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-            for (int h = 0; h < 2; ++h) core.read_v(h, vs, 32 * half + 16 * h + 4 * g, c16);
+            core.read_v(vs, 32 * half, g, c16);
             run.add(core, w);
         };
         int page = page_at(1);  // of the stage after the next copy's
@@ -761,9 +814,8 @@ __global__ __launch_bounds__(64 * WAVES, WAVES / 4) void attn_share_k(const Shar
         for (int half = 0; half < 2; ++half) {
             const int t0 = p.begin + st * STAGE + 32 * half;
             scores(k0, half, s[0]);
-#pragma unroll
-            for (int h = 0; h < 2; ++h) core.read_v(h, v0, 32 * half + 16 * h + 4 * g, c16);
-            bool bad = false;
+            core.read_v(v0, 32 * half, g, c16);
+            uint32_t keep = 0, apart = 0;
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const int pos = 16 * (i / 4) + 4 * g + i % 4;
@@ -771,10 +823,11 @@ __global__ __launch_bounds__(64 * WAVES, WAVES / 4) void attn_share_k(const Shar
 #pragma unroll
                 for (int t = 0; t < QT; ++t)
                     if (!seen || t0 + pos >= lim[t]) s[0][t][i / 4][i % 4] = -INFINITY;
-                core.forget(i, seen);
-                if (core.clean(i, t0 + pos >= least)) bad = true;
+                keep |= (uint32_t)seen << i;
+                apart |= (uint32_t)(t0 + pos >= least) << i;
             }
-            if (__ballot(bad)) odd = 1;
+            core.forget(keep);
+            if (__ballot(core.clean(apart))) odd = 1;
             run.follow(s[0], a.scale2);
             typename C::Weights w[QT];
             run.weigh(s[0], a.scale2, w);
@@ -794,19 +847,16 @@ __global__ __launch_bounds__(64 * WAVES, WAVES / 4) void attn_share_k(const Shar
         T *out = reinterpret_cast<T *>(a.out) + (int64_t)row * a.ldo + (int64_t)head * a.hd;
         if (!p.direct && g == 0) *reinterpret_cast<f2_t *>(a.part_ml + 2 * at) = f2_t{run.m[t], sum};
 #pragma unroll
-        for (int n = 0; n < C::NB; ++n)
+        for (int n = 0; n < C::NB; ++n) {
+            const int ch = 16 * n + 4 * g;
+            if (!EXACT && ch >= a.hd) continue;
+            if (p.direct) {
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int ch = 16 * C::W * n + C::W * (4 * g + r);
-                if (!EXACT && ch >= a.hd) continue;
-                if (p.direct) {
-#pragma unroll
-                    for (int w = 0; w < C::W; ++w) out[ch + w] = (T)(sum == 0.f ? 0.f : run.o[t][n * C::W + w][r] * inv);
-                } else {
-#pragma unroll
-                    for (int w = 0; w < C::W; ++w) po[ch + w] = run.o[t][n * C::W + w][r];
-                }
+                for (int r = 0; r < 4; ++r) out[ch + r] = (T)(sum == 0.f ? 0.f : run.o[t][n][r] * inv);
+            } else {
+                *reinterpret_cast<f4_t *>(po + ch) = run.o[t][n];
             }
+        }
     }
 }
 
