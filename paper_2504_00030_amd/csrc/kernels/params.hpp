@@ -277,6 +277,7 @@ struct SharedAttnArgs {
     float scale2;     // scale * log2(e)
     // what plan_shared_attention() lays down
     int32_t prefix_cols, own_cols, prefix_parts, prefix_chunk, own_parts;  // columns of a workgroup, parts along the positions
+    bool through;     // a workgroup goes through the prefix and the own positions of its columns
     uint32_t prefix_groups, own_tiles;
     int64_t prefix_groups64, own_groups64;
     float *part_o;    // [R][nq][parts][hd]

@@ -586,17 +586,23 @@ __device__ __forceinline__ void walk(const SharedAttnArgs &a, const Piece &p, C 
     }
 }
 
-// Queries of a wave's columns from m0 on, and the positions each sees; columns past the last one repeat it.
+// Queries of a wave's columns from m0 on; columns past the last one repeat it.
 template <class C>
-__device__ __forceinline__ void take_columns(const SharedAttnArgs &a, const Piece &p, int m0, C &core, int (&lim)[C::QT]) {
+__device__ __forceinline__ void take_columns(const SharedAttnArgs &a, const Piece &p, int m0, C &core) {
     const int lane = threadIdx.x & 63, cols = p.n * a.g;
 #pragma unroll
     for (int t = 0; t < C::QT; ++t) {
         const int col = min(m0 + 16 * t + (lane & 15), cols - 1), row = col / a.g;
-        lim[t] = p.sees(row);
         core.load_q(t, reinterpret_cast<const typename C::T *>(a.q) + (int64_t)(p.row0 + row) * a.ldq + (int64_t)(p.h * a.g + col % a.g) * a.hd,
                     a.q_whole, a.hd, lane >> 4);
     }
+}
+// Positions each of them sees.
+template <int QT>
+__device__ __forceinline__ void limits(const SharedAttnArgs &a, const Piece &p, int m0, int (&lim)[QT]) {
+    const int lane = threadIdx.x & 63, cols = p.n * a.g;
+#pragma unroll
+    for (int t = 0; t < QT; ++t) lim[t] = p.sees(min(m0 + 16 * t + (lane & 15), cols - 1) / a.g);
 }
 
 }  // namespace
@@ -616,7 +622,8 @@ __global__ __launch_bounds__(256, sizeof(typename C::T) == 2 || C::HDP < 128 ? 2
     C core;
     Running<C> run;
     int lim[QT], odd = 0;
-    take_columns(a, p, m0, core, lim);
+    take_columns(a, p, m0, core);
+    limits(a, p, m0, lim);
     run.clear();
     // positions that the first column sees, and those that the last one does within this part
     const int least = p.sees(m0 / a.g), end = min(p.begin + p.chunk, p.sees((min(m0 + QT * 16, cols) - 1) / a.g));
@@ -713,24 +720,13 @@ __global__ __launch_bounds__(64 * WAVES, WAVES / 4) void attn_share_k(const Shar
     C core;
     Running<C> run;
     int lim[QT], odd = 0;
-    take_columns(a, p, m0, core, lim);
+    take_columns(a, p, m0, core);
     run.clear();
-    // positions: of the part that some column sees, and stages that all columns see
-    const int end = min(p.begin + p.chunk, p.sees((min(first + COLS, cols) - 1) / a.g));
-    const int all = (max(0, end - p.begin) + STAGE - 1) / STAGE;
-    int stages = max(0, min(end, p.sees(first / a.g)) - p.begin) / STAGE;
-    if (stages > 0) {  // every wave looks at the same pages and comes to the same answer
-        bool gone = false;
-        const int last = (p.begin + stages * STAGE - 1) >> a.page_shift;
-        for (int i = (p.begin >> a.page_shift) + lane; i <= last; i += 64) gone |= (uint32_t)p.table[min(i, p.pages - 1)] >= (uint32_t)a.n_pages;
-        if (__ballot(gone)) stages = 0;
-    }
     if constexpr (!EXACT) {  // chunks beyond hd are never copied: the products need numbers there
         uint8_t *every[6] = {k0, k1, k2, v0, v1, v2};
 #pragma unroll
         for (int i = 0; i < 6; ++i)
             for (int b = threadIdx.x * 16; b < BYTES; b += SHARE) *reinterpret_cast<u4_t *>(every[i] + b) = u4_t{0, 0, 0, 0};
-        __syncthreads();
     }
     const T *kp = reinterpret_cast<const T *>(a.k_pages), *vp = reinterpret_cast<const T *>(a.v_pages);
     auto page_at = [&](int st) { return p.table[min((p.begin + st * STAGE + lane) >> a.page_shift, p.pages - 1)]; };
@@ -762,6 +758,27 @@ __global__ __launch_bounds__(64 * WAVES, WAVES / 4) void attn_share_k(const Shar
             }
         }
     };
+#pragma unroll 1
+    for (int segment = a.through ? 0 : 1; segment < 2; ++segment) {
+    const Piece whole_piece = p;
+    if (segment == 0) {  // the prefix in front of the sequence's own positions
+        p.table = a.prefix_table;
+        p.pages = ((a.prefix_len - 1) >> a.page_shift) + 1;
+        p.len = p.chunk = a.prefix_len;
+        p.begin = 0;
+        p.own = false;
+    }
+    limits(a, p, m0, lim);
+    // positions: of the part that some column sees, and stages that all columns see
+    const int end = min(p.begin + p.chunk, p.sees((min(first + COLS, cols) - 1) / a.g));
+    const int all = (max(0, end - p.begin) + STAGE - 1) / STAGE;
+    int stages = max(0, min(end, p.sees(first / a.g)) - p.begin) / STAGE;
+    if (stages > 0) {  // every wave looks at the same pages and comes to the same answer
+        bool gone = false;
+        const int last = (p.begin + stages * STAGE - 1) >> a.page_shift;
+        for (int i = (p.begin >> a.page_shift) + lane; i <= last; i += 64) gone |= (uint32_t)p.table[min(i, p.pages - 1)] >= (uint32_t)a.n_pages;
+        if (__ballot(gone)) stages = 0;
+    }
     f4_t s[2][QT][2];
     auto scores = [&](const uint8_t *ks, int half, f4_t (&to)[QT][2]) {
 #pragma unroll
@@ -781,6 +798,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES / 4) void attn_share_k(const Shar
             core.read_v(vs, 32 * half, g, c16);
             run.add(core, w);
         };
+        __syncthreads();
         int page = page_at(1);  // of the stage after the next copy's
         copy(0, page_at(0), k0, v0);
         if (stages > 1) copy(1, page, k1, v1);
@@ -835,6 +853,9 @@ __global__ __launch_bounds__(64 * WAVES, WAVES / 4) void attn_share_k(const Shar
         }
     }
     if (uniform(odd)) add_odd(a, p, max(least, p.begin + stages * STAGE), end, 0, 1, lim, run);
+    odd = 0;
+    p = whole_piece;
+    }
     const int parts = a.prefix_parts + a.own_parts;
 #pragma unroll
     for (int t = 0; t < QT; ++t) {
@@ -940,6 +961,15 @@ void plan_shared_attention(SharedAttnArgs &a, int64_t own_capacity) {
         a.own_parts = (int)parts(own_capacity, tiles * a.nkv, a.own_cols);
         a.own_groups64 = (int64_t)a.own_tiles * a.nkv * a.own_parts;
     }
+    // Enough workgroups without sharing out the prefix: each goes through prefix and own positions by itself, and nothing is
+    // left to join.
+    a.through = a.prefix_len > 0 && own_capacity > 0 && a.own_cols >= 64 && (columns + a.own_cols - 1) / a.own_cols * a.nkv >= 192;
+    if (a.through) {
+        a.prefix_parts = 0;
+        a.prefix_groups64 = 0;
+        a.own_parts = 1;
+        a.own_groups64 = (int64_t)a.own_tiles * a.nkv;
+    }
     a.prefix_groups = (uint32_t)a.prefix_groups64;
 }
 
@@ -978,7 +1008,7 @@ hipError_t launch_shared_attention(const SharedAttnArgs &args, hipStream_t s) {
     SharedAttnArgs a = args;
     if (a.prefix_groups64 + a.own_groups64 > 0x7fffffff) return hipErrorInvalidValue;
     hipError_t e;
-    if (a.prefix_cols == a.own_cols) {  // both in one launch
+    if (a.through || a.prefix_cols == a.own_cols) {  // both in one launch
         e = launch_head(a, a.own_cols, a.prefix_groups64 + a.own_groups64, s);
     } else {
         e = launch_head(a, a.prefix_cols, a.prefix_groups64, s);
