@@ -337,9 +337,9 @@ struct CoreF32 {
 
 // Parts of a sequence's own positions: `chunk` positions each, `used` of them (one, perhaps empty, at least).
 struct OwnParts { int len, chunk, used; };
-__device__ __forceinline__ OwnParts own_parts_of(const SharedAttnArgs &a, int b) {
+__device__ __forceinline__ OwnParts own_parts_of(const SharedAttnArgs &a, int own_len) {
     OwnParts p;
-    p.len = max(0, min(a.own_len[b], a.table_pages << a.page_shift));
+    p.len = max(0, min(own_len, a.table_pages << a.page_shift));
     p.chunk = max(MIN_PART, ((p.len + a.own_parts - 1) / a.own_parts + STAGE - 1) & ~(STAGE - 1));  // stages begin with their pages
     p.used = max(1, (p.len + p.chunk - 1) / p.chunk);
     return p;
@@ -386,8 +386,11 @@ __device__ __forceinline__ bool piece_of(const SharedAttnArgs &a, uint32_t id, P
     const int part = (int)(id / a.own_tiles);
     const int lane = threadIdx.x & 63;
     for (int s0 = 0; s0 < a.n_seq; s0 += 64) {
-        int first = 0, n = 0;
-        if (s0 + lane < a.n_seq) rows_of(a, s0 + lane, first, n);
+        int first = 0, n = 0, len = 0;
+        if (s0 + lane < a.n_seq) {
+            len = a.own_len[s0 + lane];
+            rows_of(a, s0 + lane, first, n);
+        }
         const int64_t tiles = ((int64_t)n * a.g + COLS - 1) / COLS;
         int64_t upto = tiles;
 #pragma unroll
@@ -401,7 +404,7 @@ __device__ __forceinline__ bool piece_of(const SharedAttnArgs &a, uint32_t id, P
             p.tile = uniform((int)(tile - __shfl(upto - tiles, src, WAVE)));
             p.row0 = uniform(__shfl(first, src, WAVE));
             p.n = uniform(__shfl(n, src, WAVE));
-            const OwnParts parts = own_parts_of(a, b);
+            const OwnParts parts = own_parts_of(a, uniform(__shfl(len, src, WAVE)));
             if (part >= parts.used) return false;
             p.own = true;
             p.len = uniform(parts.len);
@@ -610,11 +613,9 @@ __device__ __forceinline__ void limits(const SharedAttnArgs &a, const Piece &p, 
 // Few columns: the four waves of a workgroup take the same QT x 16 columns and every fourth tile of the positions, and
 // join their sums through shared memory at the end.
 template <class C>
-__global__ __launch_bounds__(256, sizeof(typename C::T) == 2 || C::HDP < 128 ? 2 : 1) void attn_split_k(const SharedAttnArgs a) {
+__device__ __forceinline__ void split(const SharedAttnArgs &a, float (*so)[16][C::HDP + 4], float (*sm)[32], float (*sl)[32]) {
     typedef typename C::T T;
-    constexpr int QT = C::QT, LD = C::HDP + 4;
-    __shared__ float so[4][16][LD];
-    __shared__ float sm[4][QT * 16], sl[4][QT * 16];
+    constexpr int QT = C::QT;
     Piece p;
     if (!piece_of<QT * 16>(a, workgroup(), p)) return;
     const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), g = lane >> 4, c16 = lane & 15;
@@ -678,6 +679,14 @@ __global__ __launch_bounds__(256, sizeof(typename C::T) == 2 || C::HDP < 128 ? 2
             if (sub == 0) *reinterpret_cast<f2_t *>(a.part_ml + 2 * at) = f2_t{top, sum};
         }
     }
+}
+
+// Pieces of the prefix as CP, of own positions as CO: the rows of all sequences are more columns than those of one.
+template <class CP, class CO>
+__global__ __launch_bounds__(256, sizeof(typename CP::T) == 2 ? (CP::HDP <= 128 ? 2 : 1) : (CP::HDP < 128 ? 2 : 1)) void attn_split_k(const SharedAttnArgs a) {
+    __shared__ float so[4][16][CP::HDP + 4], sm[4][32], sl[4][32];
+    if (std::is_same<CP, CO>::value || workgroup() < a.prefix_groups) split<CP>(a, so, sm, sl);
+    else split<CO>(a, so, sm, sl);
 }
 
 // f(num<0>) .. f(num<N - 1>)
@@ -881,45 +890,59 @@ __global__ __launch_bounds__(64 * WAVES, WAVES / 4) void attn_share_k(const Shar
     }
 }
 
-// The parts of one row and head, a wave each.
-template <typename T>
+// The parts of one row and head, a wave each: LPP lanes hold four neighbouring channels each, 64 / LPP parts at a time, four of
+// these on their way.
+template <typename T, int LPP>
 __global__ __launch_bounds__(256) void attn_join_k(const SharedAttnArgs a) {
     const uint32_t item = workgroup() * 4 + (threadIdx.x >> 6);  // below 2^31: the host bounds R * nq
     if (item >= (uint32_t)a.R * (uint32_t)a.nq) return;
     const int lane = threadIdx.x & 63, row = (int)(item / a.nq), head = (int)(item % a.nq);
-    int b = -1;
-    for (int s0 = 0; s0 < a.n_seq && b < 0; s0 += 64) {
-        int first = 0, n = 0;
-        if (s0 + lane < a.n_seq) rows_of(a, s0 + lane, first, n);
+    int used = -1;
+    for (int s0 = 0; s0 < a.n_seq && used < 0; s0 += 64) {
+        int first = 0, n = 0, len = 0;
+        if (s0 + lane < a.n_seq) {
+            if (a.own_parts) len = a.own_len[s0 + lane];
+            rows_of(a, s0 + lane, first, n);
+        }
         const uint64_t mine = __ballot(row >= first && row < first + n);
-        if (mine) b = s0 + __ffsll((unsigned long long)mine) - 1;
+        if (mine) used = a.own_parts ? own_parts_of(a, uniform(__shfl(len, __ffsll((unsigned long long)mine) - 1, WAVE))).used : 0;
     }
-    if (b < 0) return;  // a row of no sequence
-    int used = 0;
-    if (a.own_parts) used = own_parts_of(a, b).used;
+    if (used < 0) return;  // a row of no sequence
     const int n = a.prefix_parts + used, parts = a.prefix_parts + a.own_parts;
     if (a.prefix_parts == 0 && used == 1) return;  // written by its only part
     const float *ml = a.part_ml + (int64_t)item * parts * 2, *po = a.part_o + (int64_t)item * parts * a.hd;
-    float m = -INFINITY, l = 0.f;
-    if (lane < n) { m = ml[2 * lane]; l = ml[2 * lane + 1]; }
-    float m2 = -INFINITY, l2 = 0.f;
-    if (lane + 64 < n) { m2 = ml[2 * lane + 128]; l2 = ml[2 * lane + 129]; }
-    const float top = wave_max(fmaxf(m, m2)), base = top == -INFINITY ? 0.f : top;
-    const float f = exp2_(m - base), f2 = exp2_(m2 - base);
-    const float sum = wave_sum(f * l + f2 * l2);
-    float acc[4] = {0.f, 0.f, 0.f, 0.f};
-    for (int i = 0; i < n; ++i) {
-        const float w = __shfl(i < 64 ? f : f2, i & 63, WAVE);
-        // (a part without positions seen holds zeros)
+    f2_t x = {-INFINITY, 0.f}, y = {-INFINITY, 0.f};
+    if (lane < n) x = *reinterpret_cast<const f2_t *>(ml + 2 * lane);
+    if (lane + 64 < n) y = *reinterpret_cast<const f2_t *>(ml + 2 * lane + 128);
+    const float top = wave_max(fmaxf(x[0], y[0])), base = top == -INFINITY ? 0.f : top;
+    // (a part without positions seen has weight 0 and holds zeros)
+    const float f = exp2_(x[0] - base), f2 = exp2_(y[0] - base), sum = wave_sum(f * x[1] + f2 * y[1]);
+    const int ch = 4 * (lane % LPP), which = lane / LPP;
+    f4_t acc = {0.f, 0.f, 0.f, 0.f};
+    for (int i0 = 0; i0 < n; i0 += 4 * (64 / LPP)) {
+        f4_t v[4];
+        float w[4];
 #pragma unroll
-        for (int c = 0; c < 4; ++c)
-            if (lane + 64 * c < a.hd) acc[c] += w * po[(int64_t)i * a.hd + lane + 64 * c];
+        for (int j = 0; j < 4; ++j) {
+            const int i = i0 + j * (64 / LPP) + which;
+            const float fi = __shfl(f, i & 63, WAVE), fj = __shfl(f2, i & 63, WAVE);
+            w[j] = i < 64 ? fi : fj;
+            v[j] = f4_t{0.f, 0.f, 0.f, 0.f};
+            if (i < n && ch < a.hd) v[j] = *reinterpret_cast<const f4_t *>(po + (int64_t)i * a.hd + ch);
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (i0 + j * (64 / LPP) + which < n) acc += w[j] * v[j];
     }
-    const float inv = 1.f / sum;
-    T *dst = reinterpret_cast<T *>(a.out) + (int64_t)row * a.ldo + (int64_t)head * a.hd;
 #pragma unroll
-    for (int c = 0; c < 4; ++c)
-        if (lane + 64 * c < a.hd) dst[lane + 64 * c] = (T)(sum == 0.f ? 0.f : acc[c] * inv);
+    for (int m = LPP; m < 64; m <<= 1)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[e] += __shfl_xor(acc[e], m, WAVE);
+    if (which != 0 || ch >= a.hd) return;
+    const float inv = 1.f / sum;
+    T *dst = reinterpret_cast<T *>(a.out) + (int64_t)row * a.ldo + (int64_t)head * a.hd + ch;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) dst[e] = (T)(sum == 0.f ? 0.f : acc[e] * inv);
 }
 
 // Parts and tiles of a call; a function of the sizes alone, so that the workspace is known beforehand.
@@ -931,10 +954,17 @@ void plan_shared_attention(SharedAttnArgs &a, int64_t own_capacity) {
         if (n >= 64 && a.hd <= 128) return n > 128 ? 256 : n > 64 ? 128 : 64;
         return n > 16 && a.hd <= 128 ? 32 : 16;
     };
+    a.prefix_cols = kind(columns);
+    a.own_cols = kind(each_seq);
+    const int64_t prefix_tiles = a.prefix_len > 0 ? (columns + a.prefix_cols - 1) / a.prefix_cols : 0;
+    const int64_t own_tiles = own_capacity > 0 ? std::max<int64_t>((columns + a.own_cols - 1) / a.own_cols, a.n_seq) : 0;
+    // Pieces whose waves split the positions, of prefix and own together: a thousand workgroups, parts of the same length
+    const int64_t work = a.nkv * ((a.prefix_cols < 64 ? prefix_tiles * a.prefix_len : 0) + (a.own_cols < 64 ? own_tiles * own_capacity : 0));
+    const int64_t length = std::max<int64_t>(MIN_PART, (work + 1023) / 1024);
     auto parts = [&](int64_t positions, int64_t groups, int cols) -> int64_t {
         groups = std::max<int64_t>(groups, 1);
         const int64_t most = std::min<int64_t>((positions + MIN_PART - 1) / MIN_PART, MAX_PARTS);
-        if (cols < 64) return std::max<int64_t>(1, std::min((1024 + groups - 1) / groups, most));
+        if (cols < 64) return std::max<int64_t>(1, std::min((positions + length - 1) / length, most));
         // one workgroup a compute unit: rounds of 256, each as long as a part and a start (two stages' time)
         int64_t best = 1;
         double least = 1e300;
@@ -947,18 +977,15 @@ void plan_shared_attention(SharedAttnArgs &a, int64_t own_capacity) {
     };
     a.prefix_parts = a.own_parts = a.prefix_chunk = 0;
     a.prefix_groups64 = a.own_groups64 = 0;
-    a.prefix_cols = kind(columns);
-    a.own_cols = kind(each_seq);
     if (a.prefix_len > 0) {
-        const int64_t tiles = (columns + a.prefix_cols - 1) / a.prefix_cols, n = parts(a.prefix_len, tiles * a.nkv, a.prefix_cols);
+        const int64_t n = parts(a.prefix_len, prefix_tiles * a.nkv, a.prefix_cols);
         a.prefix_chunk = (int)(((a.prefix_len + n - 1) / n + STAGE - 1) / STAGE * STAGE);
         a.prefix_parts = (a.prefix_len + a.prefix_chunk - 1) / a.prefix_chunk;
-        a.prefix_groups64 = tiles * a.nkv * a.prefix_parts;
+        a.prefix_groups64 = prefix_tiles * a.nkv * a.prefix_parts;
     }
     a.own_tiles = (uint32_t)(a.n_seq + columns / a.own_cols);
     if (own_capacity > 0) {
-        const int64_t tiles = std::max<int64_t>((columns + a.own_cols - 1) / a.own_cols, a.n_seq);
-        a.own_parts = (int)parts(own_capacity, tiles * a.nkv, a.own_cols);
+        a.own_parts = (int)parts(own_capacity, own_tiles * a.nkv, a.own_cols);
         a.own_groups64 = (int64_t)a.own_tiles * a.nkv * a.own_parts;
     }
     // Enough workgroups without sharing out the prefix: each goes through prefix and own positions by itself, and nothing is
@@ -978,49 +1005,68 @@ int64_t shared_attention_parts(const SharedAttnArgs &a) {
     return a.prefix_parts == 0 && a.own_parts <= 1 ? 0 : n;
 }
 
-// `groups` workgroups of one width
+// Pieces of the prefix and of own positions, of either kind or (parts that split the positions) both.
 template <int HDP, bool EXACT>
-static hipError_t launch_cols(const SharedAttnArgs &a, int cols, int64_t groups, hipStream_t s) {
+static hipError_t launch_cols(const SharedAttnArgs &a, int prefix_cols, int own_cols, int64_t groups, hipStream_t s) {
     const dim3 grid = grid_of(groups), block(256);
+    typedef CoreBf16<HDP, 1, EXACT> One;
+    if (a.dtype == DT_F32) {
+        typedef CoreF32<HDP, EXACT> C;
+        hipLaunchKernelGGL((attn_split_k<C, C>), grid, block, 0, s, a);
+        return hipGetLastError();
+    }
     if constexpr (HDP <= 128) {
-        switch (a.dtype == DT_F32 ? 0 : cols) {
-            case 256: hipLaunchKernelGGL((attn_share_k<HDP, HDP == 32 ? 4 : 2, HDP == 32 ? 4 : 8, EXACT>), grid, dim3(HDP == 32 ? 256 : 512), 0, s, a); return hipGetLastError();
+        typedef CoreBf16<HDP, 2, EXACT> Two;
+        constexpr int WIDE = HDP == 32 ? 4 : 8;  // waves of 256 columns (heads of 32: a stage is too small to be copied by eight)
+        switch (prefix_cols) {
+            case 256: hipLaunchKernelGGL((attn_share_k<HDP, 16 / WIDE, WIDE, EXACT>), grid, dim3(64 * WIDE), 0, s, a); return hipGetLastError();
             case 128: hipLaunchKernelGGL((attn_share_k<HDP, 2, 4, EXACT>), grid, block, 0, s, a); return hipGetLastError();
             case 64: hipLaunchKernelGGL((attn_share_k<HDP, 1, 4, EXACT>), grid, block, 0, s, a); return hipGetLastError();
-            case 32: hipLaunchKernelGGL((attn_split_k<CoreBf16<HDP, 2, EXACT>>), grid, block, 0, s, a); return hipGetLastError();
+            case 32:
+                if (own_cols == 32) hipLaunchKernelGGL((attn_split_k<Two, Two>), grid, block, 0, s, a);
+                else hipLaunchKernelGGL((attn_split_k<Two, One>), grid, block, 0, s, a);
+                return hipGetLastError();
             default: break;
         }
     }
-    if (a.dtype == DT_F32) hipLaunchKernelGGL((attn_split_k<CoreF32<HDP, EXACT>>), grid, block, 0, s, a);
-    else hipLaunchKernelGGL((attn_split_k<CoreBf16<HDP, 1, EXACT>>), grid, block, 0, s, a);
+    hipLaunchKernelGGL((attn_split_k<One, One>), grid, block, 0, s, a);
     return hipGetLastError();
 }
 
-static hipError_t launch_head(const SharedAttnArgs &a, int cols, int64_t groups, hipStream_t s) {
+static hipError_t launch_head(const SharedAttnArgs &a, int prefix_cols, int own_cols, int64_t groups, hipStream_t s) {
     if (groups == 0) return hipSuccess;
-    if (a.hd <= 32) return a.hd == 32 ? launch_cols<32, true>(a, cols, groups, s) : launch_cols<32, false>(a, cols, groups, s);
-    if (a.hd <= 64) return a.hd == 64 ? launch_cols<64, true>(a, cols, groups, s) : launch_cols<64, false>(a, cols, groups, s);
-    if (a.hd <= 128) return a.hd == 128 ? launch_cols<128, true>(a, cols, groups, s) : launch_cols<128, false>(a, cols, groups, s);
-    return a.hd == 256 ? launch_cols<256, true>(a, cols, groups, s) : launch_cols<256, false>(a, cols, groups, s);
+    if (a.hd <= 32) return a.hd == 32 ? launch_cols<32, true>(a, prefix_cols, own_cols, groups, s) : launch_cols<32, false>(a, prefix_cols, own_cols, groups, s);
+    if (a.hd <= 64) return a.hd == 64 ? launch_cols<64, true>(a, prefix_cols, own_cols, groups, s) : launch_cols<64, false>(a, prefix_cols, own_cols, groups, s);
+    if (a.hd <= 128) return a.hd == 128 ? launch_cols<128, true>(a, prefix_cols, own_cols, groups, s) : launch_cols<128, false>(a, prefix_cols, own_cols, groups, s);
+    return a.hd == 256 ? launch_cols<256, true>(a, prefix_cols, own_cols, groups, s) : launch_cols<256, false>(a, prefix_cols, own_cols, groups, s);
+}
+
+template <typename T>
+static hipError_t launch_join(const SharedAttnArgs &a, hipStream_t s) {
+    const dim3 grid = grid_of(((int64_t)a.R * a.nq + 3) / 4), block(256);
+    if (a.hd <= 32) hipLaunchKernelGGL((attn_join_k<T, 8>), grid, block, 0, s, a);
+    else if (a.hd <= 64) hipLaunchKernelGGL((attn_join_k<T, 16>), grid, block, 0, s, a);
+    else if (a.hd <= 128) hipLaunchKernelGGL((attn_join_k<T, 32>), grid, block, 0, s, a);
+    else hipLaunchKernelGGL((attn_join_k<T, 64>), grid, block, 0, s, a);
+    return hipGetLastError();
 }
 
 hipError_t launch_shared_attention(const SharedAttnArgs &args, hipStream_t s) {
     SharedAttnArgs a = args;
     if (a.prefix_groups64 + a.own_groups64 > 0x7fffffff) return hipErrorInvalidValue;
     hipError_t e;
-    if (a.through || a.prefix_cols == a.own_cols) {  // both in one launch
-        e = launch_head(a, a.own_cols, a.prefix_groups64 + a.own_groups64, s);
+    if (a.through) {
+        e = launch_head(a, a.own_cols, a.own_cols, a.own_groups64, s);
+    } else if (a.prefix_cols == a.own_cols || (a.prefix_cols == 32 && a.own_cols == 16)) {  // in one launch
+        e = launch_head(a, a.prefix_cols, a.own_cols, a.prefix_groups64 + a.own_groups64, s);
     } else {
-        e = launch_head(a, a.prefix_cols, a.prefix_groups64, s);
+        e = launch_head(a, a.prefix_cols, a.prefix_cols, a.prefix_groups64, s);
         a.prefix_groups = 0;
-        if (e == hipSuccess) e = launch_head(a, a.own_cols, a.own_groups64, s);
+        if (e == hipSuccess) e = launch_head(a, a.own_cols, a.own_cols, a.own_groups64, s);
     }
     if (e != hipSuccess) return e;
     if (a.prefix_parts == 0 && a.own_parts == 1) return hipSuccess;  // every row is written by its only part
-    const dim3 grid = grid_of(((int64_t)a.R * a.nq + 3) / 4);
-    if (a.dtype == DT_F32) hipLaunchKernelGGL((attn_join_k<float>), grid, dim3(256), 0, s, a);
-    else hipLaunchKernelGGL((attn_join_k<__bf16>), grid, dim3(256), 0, s, a);
-    return hipGetLastError();
+    return a.dtype == DT_F32 ? launch_join<float>(a, s) : launch_join<__bf16>(a, s);
 }
 
 }  // namespace sd
