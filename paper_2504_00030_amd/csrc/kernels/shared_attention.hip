@@ -382,7 +382,7 @@ __device__ __forceinline__ bool piece_of(const SharedAttnArgs &a, uint32_t id, P
     id -= a.prefix_groups;
     p.h = (int)(id % a.nkv);
     id /= a.nkv;
-    int64_t tile = id % a.own_tiles;
+    uint32_t tile = id % a.own_tiles;
     const int part = (int)(id / a.own_tiles);
     const int lane = threadIdx.x & 63;
     for (int s0 = 0; s0 < a.n_seq; s0 += 64) {
@@ -391,24 +391,28 @@ __device__ __forceinline__ bool piece_of(const SharedAttnArgs &a, uint32_t id, P
             len = a.own_len[s0 + lane];
             rows_of(a, s0 + lane, first, n);
         }
-        const int64_t tiles = ((int64_t)n * a.g + COLS - 1) / COLS;
-        int64_t upto = tiles;
+        // tiles of this sequence, and of it and those in front (row numbers that make no sense may run past 2^32: then the
+        // tile found is not one of its sequence, and nobody works on it)
+        const uint32_t tiles = (uint32_t)(((int64_t)n * a.g + COLS - 1) / COLS);
+        uint32_t upto = tiles;
 #pragma unroll
         for (int m = 1; m < 64; m <<= 1) {
-            const int64_t o = __shfl_up(upto, m, WAVE);
+            const uint32_t o = __shfl_up(upto, m, WAVE);
             if (lane >= m) upto += o;
         }
         const uint64_t beyond = __ballot(upto > tile);
         if (beyond) {
             const int src = uniform(__ffsll((unsigned long long)beyond) - 1), b = s0 + src;
-            p.tile = uniform((int)(tile - __shfl(upto - tiles, src, WAVE)));
-            p.row0 = uniform(__shfl(first, src, WAVE));
-            p.n = uniform(__shfl(n, src, WAVE));
-            const OwnParts parts = own_parts_of(a, uniform(__shfl(len, src, WAVE)));
+            auto from = [&](int v) { return __builtin_amdgcn_readlane(v, src); };
+            p.tile = from((int)(tile - (upto - tiles)));
+            if ((uint32_t)p.tile >= (uint32_t)from((int)tiles)) return false;
+            p.row0 = from(first);
+            p.n = from(n);
+            const OwnParts parts = own_parts_of(a, from(len));
             if (part >= parts.used) return false;
             p.own = true;
-            p.len = uniform(parts.len);
-            p.chunk = uniform(parts.chunk);
+            p.len = parts.len;
+            p.chunk = parts.chunk;
             p.direct = a.prefix_parts == 0 && parts.used == 1;
             p.part = a.prefix_parts + part;
             p.begin = part * p.chunk;
@@ -416,7 +420,7 @@ __device__ __forceinline__ bool piece_of(const SharedAttnArgs &a, uint32_t id, P
             p.pages = a.table_pages;
             return true;
         }
-        tile -= __shfl(upto, 63, WAVE);
+        tile -= (uint32_t)__builtin_amdgcn_readlane((int)upto, 63);
     }
     return false;
 }
