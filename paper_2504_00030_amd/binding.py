@@ -715,27 +715,15 @@ def _vector(t, name: str, n: int, dtype):
         _need(t, name, f"a contiguous {dtype} tensor of {n} elements")
 
 
-def _work(workspace, dev: int):
-    if workspace is None:
-        return None, 0
-    if workspace.get_device() != dev or not workspace.is_contiguous():
-        _need(workspace, "workspace", "contiguous, on the device of the operands")
-    return workspace.data_ptr(), workspace.nbytes
-
-
-def _heads(t, name: str, R: int, hd: int) -> int:
-    """Row stride of a [R][heads][hd] tensor whose rows hold their heads one after the other."""
-    shape, stride = t.shape, t.stride()
-    if len(shape) != 3 or shape[0] != R or shape[2] != hd or stride[2] != 1 or (stride[1] != hd and shape[1] > 1):
-        _need(t, name, f"[{R}][heads][{hd}] with the heads of a row one after the other")
-    return stride[0] if R > 1 else shape[1] * hd  # (the stride of a single row says nothing)
-
-
 def _pool(k_pages, v_pages):
-    shape = k_pages.shape
-    if len(shape) != 4 or v_pages.shape != shape or k_pages.dtype is not v_pages.dtype or not (k_pages.is_contiguous() and v_pages.is_contiguous()):
-        raise ValueError("k_pages and v_pages must be contiguous tensors [pages][heads][page_tokens][hd] of one shape and type")
-    return shape
+    raise ValueError("k_pages and v_pages must be contiguous tensors [pages][heads][page_tokens][hd] of one shape and type, not "
+                     f"{tuple(k_pages.shape)} of {k_pages.dtype} and {tuple(v_pages.shape)} of {v_pages.dtype}")
+
+
+def _heads(t, name: str):
+    """Names a tensor whose rows do not hold their heads one after the other (the stride of a single head says nothing)."""
+    if (t.stride(1) != t.shape[2] and t.shape[1] > 1) or t.stride(2) != 1:
+        _need(t, name, "[rows][heads][hd] with the heads of a row one after the other")
 
 
 def k_rope_tables(cos, sin, theta: float = 10000.0, scaling: str = "plain", factor: float = 1.0, low: float = 1.0, high: float = 32.0,
@@ -770,45 +758,66 @@ def k_rope_cache(q, k, v, cos, sin, pos, slot, q_out, k_pages, v_pages, interlea
     and pages None: queries alone."""
     if not _KINDS:
         _setup()
-    if (q is None) != (q_out is None) or any((t is None) != (k is None) for t in (v, slot, k_pages, v_pages)) or (q is None and k is None):
-        raise ValueError("q and q_out go together, and so do k, v, slot, k_pages and v_pages; one of the two sets is needed")
-    main = q if q is not None else k
-    if len(main.shape) != 3:
-        _need(main, "q" if q is not None else "k", "[R][heads][hd]")
-    R, _, hd = main.shape
-    n_pos, half = cos.shape
-    nq = nkv = ldq = ldqo = ldk = ldv = n_pages = page = 0
+    ldq = ldqo = ldk = ldv = nq = nkv = n_pages = page = 0
     qp = qop = kp = vp = sp = kpp = vpp = None
-    dev = main.get_device()
-    on = [cos.get_device(), sin.get_device(), pos.get_device()]
+    n_pos, half = cos.shape
+    dev = cos.get_device()
     if q is not None:
-        nq, ldq, ldqo = q.shape[1], _heads(q, "q", R, hd), _heads(q_out, "q_out", R, hd)
-        if q_out.shape != q.shape:
-            _need(q_out, "q_out", f"of the shape of q, {tuple(q.shape)}")
-        qp, qop, out = q.data_ptr(), q_out.data_ptr(), q_out
-        on.append(q_out.get_device())
+        if q_out is None:
+            raise ValueError("q and q_out go together")
+        R, nq, hd = shape = q.shape
+        kind, out = q.dtype, q_out.dtype
+        ldq, hq, eq = q.stride()
+        if q_out.shape != shape:
+            _need(q_out, "q_out", f"of the shape of q, {tuple(shape)}")
+        ldqo, hqo, eqo = q_out.stride()
+        if not (hq == hqo == hd and eq == eqo == 1):
+            _heads(q, "q"), _heads(q_out, "q_out")
+        if not (q.get_device() == q_out.get_device() == dev):
+            _elsewhere(q, q_out, cos)
+        if R < 2:  # (the stride of a single row says nothing)
+            ldq = ldqo = nq * hd
+        qp, qop = q.data_ptr(), q_out.data_ptr()
+    elif q_out is not None or k is None:
+        raise ValueError("q and q_out go together, and where they are left out, k is needed")
     if k is not None:
-        nkv, ldk, ldv = k.shape[1], _heads(k, "k", R, hd), _heads(v, "v", R, hd)
-        shape = _pool(k_pages, v_pages)
-        n_pages, page = shape[0], shape[2]
-        if v.shape != k.shape or v.dtype is not k.dtype or shape[1] != nkv or shape[3] != hd:
-            raise ValueError("k, v and the pages must agree in heads and head size, k and v in type")
-        if q is not None and (q.dtype is not k.dtype or q_out.dtype is not k_pages.dtype):
-            raise ValueError("q and k must have one type, and q_out and the pages theirs")
-        _vector(slot, "slot", R, _I32T)
-        kp, vp, sp, kpp, vpp, out = k.data_ptr(), v.data_ptr(), slot.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(), k_pages
-        on += [k.get_device(), v.get_device(), slot.get_device(), k_pages.get_device(), v_pages.get_device()]
+        if v is None or slot is None or k_pages is None or v_pages is None:
+            raise ValueError("k, v, slot, k_pages and v_pages go together")
+        shape = k.shape
+        if q is None:
+            R, nkv, hd = shape
+            kind, out = k.dtype, k_pages.dtype
+        n_pages, nkv, page, pd = k_pages.shape
+        if shape != (R, nkv, hd) or v.shape != shape or pd != hd or not (k.dtype is v.dtype is kind and k_pages.dtype is out):
+            raise ValueError("k, v, the pages and q must agree in rows, heads and head size; q, k and v in type, and q_out and the pages in theirs")
+        if v_pages.shape != k_pages.shape or v_pages.dtype is not out or not (k_pages.is_contiguous() and v_pages.is_contiguous()):
+            _pool(k_pages, v_pages)
+        ldk, hk, ek = k.stride()
+        ldv, hv, ev = v.stride()
+        if not (hk == hv == hd and ek == ev == 1):
+            _heads(k, "k"), _heads(v, "v")
+        if slot.dtype is not _I32T or slot.numel() != R or not slot.is_contiguous():
+            _need(slot, "slot", f"a contiguous int32 tensor of {R} elements")
+        if not (k.get_device() == v.get_device() == slot.get_device() == k_pages.get_device() == v_pages.get_device() == dev):
+            _elsewhere(k, v, slot, k_pages, v_pages, cos)
+        if R < 2:
+            ldk = ldv = nkv * hd
+        kp, vp, sp, kpp, vpp = k.data_ptr(), v.data_ptr(), slot.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr()
+    elif v is not None or slot is not None or k_pages is not None or v_pages is not None:
+        raise ValueError("k, v, slot, k_pages and v_pages go together")
     if (R | nq | nkv | hd | n_pos | half * 2 | n_pages | page) >> 31:
         _too_long(R, nq, nkv, hd, n_pos, half, n_pages, page)
-    _vector(cos, "cos", n_pos * half, _F32T)
-    _vector(sin, "sin", n_pos * half, _F32T)
-    _vector(pos, "pos", R, _I32T)
-    if on.count(dev) != len(on):
-        _elsewhere(*[t for t in (q, k, v, cos, sin, pos, slot, q_out, k_pages, v_pages) if t is not None])
-    _on(dev, main)
-    rc = load().spec_k_rope_cache(qp, ldq, nq, kp, ldk, vp, ldv, nkv, _kind(main, "q"), hd, R, cos.data_ptr(), sin.data_ptr(), n_pos,
-                                  2 * half, 1 if interleaved else 0, pos.data_ptr(), sp, qop, ldqo, kpp, vpp, n_pages, page,
-                                  _kind(out, "q_out"), stream)
+    if cos.dtype is not _F32T or sin.dtype is not _F32T or sin.shape != (n_pos, half) or not (cos.is_contiguous() and sin.is_contiguous()):
+        _need(sin, "sin", f"a contiguous fp32 tensor of {n_pos} x {half}, as cos")
+    if pos.dtype is not _I32T or pos.numel() != R or not pos.is_contiguous():
+        _need(pos, "pos", f"a contiguous int32 tensor of {R} elements")
+    if not (sin.get_device() == pos.get_device() == dev):
+        _elsewhere(cos, sin, pos)
+    _on(dev, cos)
+    if kind not in _KINDS or out not in _KINDS:
+        raise ValueError(f"unsupported element types {kind} and {out}")
+    rc = load().spec_k_rope_cache(qp, ldq, nq, kp, ldk, vp, ldv, nkv, _KINDS[kind], hd, R, cos.data_ptr(), sin.data_ptr(), n_pos, 2 * half,
+                                  1 if interleaved else 0, pos.data_ptr(), sp, qop, ldqo, kpp, vpp, n_pages, page, _KINDS[out], stream)
     if rc != 0:
         _refused(rc, "spec_k_rope_cache")
 
@@ -836,34 +845,46 @@ def k_attn_shared(q, k_pages, v_pages, row_start, table, own_len, out, workspace
     defaults to hd ** -0.5.  workspace: a GPU tensor of k_attn_shared_workspace() bytes at least, or None where that is 0."""
     if not _KINDS:
         _setup()
-    if len(q.shape) != 3:
-        _need(q, "q", "[R][heads][hd]")
-    R, nq, hd = q.shape
-    ldq, ldo = _heads(q, "q", R, hd), _heads(out, "out", R, hd)
-    n_pages, nkv, page, pd = _pool(k_pages, v_pages)
-    if out.shape != q.shape or not (q.dtype is out.dtype is k_pages.dtype) or pd != hd:
+    R, nq, hd = shape = q.shape
+    kind = q.dtype
+    ldq, hq, eq = q.stride()
+    ldo, ho, eo = out.stride()
+    n_pages, nkv, page, pd = k_pages.shape
+    if out.shape != shape or not (out.dtype is k_pages.dtype is kind) or pd != hd:
         raise ValueError("q, out and the pages must have one type and head size, q and out one shape")
-    n_seq = own_len.numel()
-    if table.dtype is not _I32T or len(table.shape) != 2 or table.shape[0] != n_seq or not table.is_contiguous():
-        _need(table, "table", f"a contiguous int32 tensor of {n_seq} x pages")
-    if (R | nq | nkv | hd | n_pages | page | n_seq | table.shape[1]) >> 31 or prefix_len >> 31 > 0:
-        _too_long(R, nq, nkv, hd, n_pages, page, n_seq, table.shape[1], prefix_len)
-    _vector(own_len, "own_len", n_seq, _I32T)
-    _vector(row_start, "row_start", n_seq + 1, _I32T)
+    if not (hq == ho == hd and eq == eo == 1):
+        _heads(q, "q"), _heads(out, "out")
+    if R < 2:  # (the stride of a single row says nothing)
+        ldq = ldo = nq * hd
+    if v_pages.shape != k_pages.shape or v_pages.dtype is not kind or not (k_pages.is_contiguous() and v_pages.is_contiguous()):
+        _pool(k_pages, v_pages)
+    n_seq, table_pages = table.shape
+    if table.dtype is not _I32T or not table.is_contiguous():
+        _need(table, "table", "a contiguous int32 tensor [sequences][pages]")
+    if (R | nq | nkv | hd | n_pages | page | n_seq | table_pages) >> 31 or prefix_len >> 31 > 0:
+        _too_long(R, nq, nkv, hd, n_pages, page, n_seq, table_pages, prefix_len)
+    if own_len.dtype is not _I32T or own_len.numel() != n_seq or not own_len.is_contiguous():
+        _need(own_len, "own_len", f"a contiguous int32 tensor of {n_seq} elements")
+    if row_start.dtype is not _I32T or row_start.numel() != n_seq + 1 or not row_start.is_contiguous():
+        _need(row_start, "row_start", f"a contiguous int32 tensor of {n_seq + 1} elements")
     dev = q.get_device()
-    pt = None
+    pt = work = None
+    work_bytes = 0
     if prefix_len > 0:
         if prefix_table is None or prefix_table.dtype is not _I32T or prefix_table.numel() < (prefix_len + page - 1) // page or \
                 not prefix_table.is_contiguous() or prefix_table.get_device() != dev:
             raise ValueError("prefix_table must be a contiguous int32 tensor with a page for every page_tokens positions of the prefix, on the device of q")
         pt = prefix_table.data_ptr()
+    if workspace is not None:
+        if workspace.get_device() != dev or not workspace.is_contiguous():
+            _need(workspace, "workspace", "contiguous, on the device of the operands")
+        work, work_bytes = workspace.data_ptr(), workspace.nbytes
     if not (k_pages.get_device() == v_pages.get_device() == row_start.get_device() == table.get_device() == own_len.get_device() ==
             out.get_device() == dev):
         _elsewhere(q, k_pages, v_pages, row_start, table, own_len, out)
     _on(dev, q)
-    work, work_bytes = _work(workspace, dev)
     rc = load().spec_k_attn_shared(q.data_ptr(), ldq, nq, nkv, hd, _kind(q, "q"), R, row_start.data_ptr(), n_seq, k_pages.data_ptr(),
-                                   v_pages.data_ptr(), n_pages, page, pt, prefix_len, table.data_ptr(), table.shape[1], own_len.data_ptr(),
+                                   v_pages.data_ptr(), n_pages, page, pt, prefix_len, table.data_ptr(), table_pages, own_len.data_ptr(),
                                    hd ** -0.5 if scale is None else scale, out.data_ptr(), ldo, work, work_bytes, stream)
     if rc != 0:
         _refused(rc, "spec_k_attn_shared")
@@ -887,29 +908,33 @@ def k_verify(p, q, draft_start, drafted, u_accept, u_next, n_accepted, next_toke
     if not _KINDS:
         _setup()
     ldp = _rows(p, "p")
-    vocab, n_seq, n_drafts = p.shape[1], u_next.numel(), drafted.numel()
-    if (vocab | p.shape[0]) >> 31:
-        _too_long(vocab, p.shape[0])
-    if p.shape[0] != n_seq + n_drafts:
+    rows, vocab = p.shape
+    n_seq, n_drafts = u_next.numel(), drafted.numel()
+    if (vocab | rows) >> 31:
+        _too_long(vocab, rows)
+    if rows != n_seq + n_drafts:
         _need(p, "p", f"of {n_seq + n_drafts} rows, one for every draft and one for every sequence")
-    _vector(draft_start, "draft_start", n_seq + 1, _I32T)
-    _vector(drafted, "drafted", n_drafts, _I32T)
-    _vector(u_accept, "u_accept", n_drafts, _F32T)
-    _vector(u_next, "u_next", n_seq, _F32T)
-    _vector(n_accepted, "n_accepted", n_seq, _I32T)
-    _vector(next_token, "next_token", n_seq, _I32T)
+    if not (draft_start.dtype is drafted.dtype is n_accepted.dtype is next_token.dtype is _I32T and u_accept.dtype is u_next.dtype is _F32T and
+            draft_start.numel() == n_seq + 1 and u_accept.numel() == n_drafts and n_accepted.numel() == next_token.numel() == n_seq and
+            draft_start.is_contiguous() and drafted.is_contiguous() and u_accept.is_contiguous() and u_next.is_contiguous() and
+            n_accepted.is_contiguous() and next_token.is_contiguous()):
+        raise ValueError(f"draft_start ({n_seq + 1}), drafted ({n_drafts}), n_accepted and next_token ({n_seq}) must be contiguous int32 tensors, "
+                         f"u_accept ({n_drafts}) and u_next ({n_seq}) contiguous fp32 ones")
     dev = p.get_device()
-    qp, ldq = None, vocab
+    qp, ldq, work, work_bytes = None, vocab, None, 0
     if q is not None:
-        ldq = _rows(q, "q") if n_drafts else vocab
         if q.shape != (n_drafts, vocab) or q.dtype is not p.dtype or q.get_device() != dev:
             _need(q, "q", f"{n_drafts} x {vocab} of the type and on the device of p")
-        qp = q.data_ptr()
+        if n_drafts:
+            qp, ldq = q.data_ptr(), _rows(q, "q")
+    if workspace is not None:
+        if workspace.get_device() != dev or not workspace.is_contiguous():
+            _need(workspace, "workspace", "contiguous, on the device of the operands")
+        work, work_bytes = workspace.data_ptr(), workspace.nbytes
     if not (draft_start.get_device() == drafted.get_device() == u_accept.get_device() == u_next.get_device() == n_accepted.get_device() ==
             next_token.get_device() == dev):
         _elsewhere(p, draft_start, drafted, u_accept, u_next, n_accepted, next_token)
     _on(dev, p)
-    work, work_bytes = _work(workspace, dev)
     rc = load().spec_k_verify(p.data_ptr(), ldp, qp, ldq, _kind(p, "p"), vocab, draft_start.data_ptr(), n_seq, n_drafts, drafted.data_ptr(),
                               u_accept.data_ptr(), u_next.data_ptr(), n_accepted.data_ptr(), next_token.data_ptr(), work, work_bytes, stream)
     if rc != 0:

@@ -1,8 +1,8 @@
 // Verification of drafted tokens against given uniforms, a batch at once.
 //
-// Only one row a sequence needs summing: the accept test reads single elements.  verify_sum_k finds the row (every
-// workgroup for itself: two dependent loads, cheaper than a launch in front) and sums its tiles of max(0, p - q) and p;
-// verify_pick_k, one workgroup a sequence, finds the tile the draw falls into and the element inside it.  Sums are in 64 bits:
+// Only one row a sequence needs summing: the accept test reads single elements.  verify_sum_k finds the row (every wave for
+// itself: two dependent loads, cheaper than a launch in front) and sums its tiles of max(0, p - q) and p, a wave each;
+// verify_pick_k, one wave a sequence, finds the tile the draw falls into and the element inside it.  Sums are in 64 bits:
 // a draw in 2^17 elements moves by 1e-13 of the mass at most, and the tests u q < p are exact.
 #include "common.hpp"
 #include "params.hpp"
@@ -14,7 +14,7 @@ namespace {
 typedef float f4_t __attribute__((ext_vector_type(4)));
 typedef __bf16 b8_t __attribute__((ext_vector_type(8)));
 
-constexpr int PER = VERIFY_TILE / 256;  // elements of a tile a thread takes: 16 neighbours
+constexpr int PER = VERIFY_TILE / 64;  // elements of a tile a lane takes
 
 // sequence b's first draft and their number; false where draft_start does not make sense
 __device__ __forceinline__ bool drafts_of(const VerifyArgs &a, int b, int &first, int &k) {
@@ -24,7 +24,7 @@ __device__ __forceinline__ bool drafts_of(const VerifyArgs &a, int b, int &first
     return first >= 0 && end >= first && end <= a.n_drafts;
 }
 
-// leading drafts that pass the test; the same for every wave, sixty-four drafts at a time
+// leading drafts that pass the test, sixty-four at a time; every wave works them out for itself
 template <typename T>
 __device__ __forceinline__ int accepted_of(const VerifyArgs &a, int b, int first, int k) {
     const int lane = threadIdx.x & 63;
@@ -46,29 +46,38 @@ __device__ __forceinline__ int accepted_of(const VerifyArgs &a, int b, int first
     return k;
 }
 
-// PER neighbours of a row from element j on, zeros past its end
-template <typename T>
-__device__ __forceinline__ void load_row(const T *row, int j, int n, float (&v)[PER]) {
-    if (j + PER <= n && (reinterpret_cast<uintptr_t>(row + j) & 15) == 0) {
-        if constexpr (sizeof(T) == 4) {
+// This lane's elements of a tile that begins with element j0, zeros past the row's end: PER neighbours, or every 64th
+// vector (SPREAD: each load of the wave is then one run of memory; only sums can do with that order)
+template <bool SPREAD, typename T>
+__device__ __forceinline__ void load_tile(const T *row, int j0, int n, float (&v)[PER]) {
+    constexpr int N = 16 / sizeof(T);  // elements of a vector
+    const int lane = threadIdx.x & 63;
+    const bool whole = j0 + VERIFY_TILE <= n && (reinterpret_cast<uintptr_t>(row + j0) & 15) == 0;
 #pragma unroll
-            for (int w = 0; w < PER / 4; ++w) {
-                const f4_t x = reinterpret_cast<const f4_t *>(row + j)[w];
+    for (int w = 0; w < PER / N; ++w) {
+        const int j = j0 + (SPREAD ? (w * 64 + lane) * N : lane * PER + w * N);
+        if (whole) {
+            if constexpr (sizeof(T) == 4) {
+                const f4_t x = *reinterpret_cast<const f4_t *>(row + j);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) v[4 * w + e] = x[e];
-            }
-        } else {
-#pragma unroll
-            for (int w = 0; w < PER / 8; ++w) {
-                const b8_t x = reinterpret_cast<const b8_t *>(row + j)[w];
+            } else {
+                const b8_t x = *reinterpret_cast<const b8_t *>(row + j);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) v[8 * w + e] = (float)x[e];
             }
-        }
-        return;
-    }
+        } else {
 #pragma unroll
-    for (int e = 0; e < PER; ++e) v[e] = j + e < n ? (float)row[j + e] : 0.f;
+            for (int e = 0; e < N; ++e) v[N * w + e] = j + e < n ? (float)row[j + e] : 0.f;
+        }
+    }
+}
+// element e of load_tile()
+template <bool SPREAD, typename T>
+__device__ __forceinline__ int place(int j0, int e) {
+    constexpr int N = 16 / sizeof(T);
+    const int lane = threadIdx.x & 63;
+    return j0 + (SPREAD ? (e / N * 64 + lane) * N + e % N : lane * PER + e);
 }
 
 // the two weights of an element: of the residual and of the target's row alone (comparisons with NaN are false)
@@ -103,36 +112,21 @@ __device__ __forceinline__ double wave_scan(double v) {
     }
     return v;
 }
-// inclusive sums over the 256 threads; `waves` is shared, four elements
-__device__ __forceinline__ double block_scan(double v, double *waves, double &total) {
-    const int wave = threadIdx.x >> 6;
-    v = wave_scan(v);
-    __syncthreads();
-    if ((threadIdx.x & 63) == 63) waves[wave] = v;
-    __syncthreads();
-    double before = 0.0;
-    for (int w = 0; w < wave; ++w) before += waves[w];
-    total = ((waves[0] + waves[1]) + waves[2]) + waves[3];
-    return before + v;
-}
-
 }  // namespace
 
 template <typename T>
 __global__ __launch_bounds__(256) void verify_sum_k(const VerifyArgs a) {
-    __shared__ double part[4][2];
-    const int b = blockIdx.y, tile = blockIdx.x;
+    const int b = blockIdx.y, tile = blockIdx.x * 4 + (threadIdx.x >> 6);
     int first, k;
-    if (!drafts_of(a, b, first, k)) return;
+    if (tile >= a.tiles || !drafts_of(a, b, first, k)) return;
     const int A = accepted_of<T>(a, b, first, k);
-    if (tile == 0 && threadIdx.x == 0) a.taken[b] = A;
     const Draw<T> d = draw_of<T>(a, b, first, k, A);
-    const int j = tile * VERIFY_TILE + (int)threadIdx.x * PER;
+    const int j0 = tile * VERIFY_TILE;
     float p[PER], q[PER];
-    load_row(d.p, j, a.vocab, p);
+    load_tile<true>(d.p, j0, a.vocab, p);
     double sp = 0.0, sr = 0.0;
     if (d.q) {
-        load_row(d.q, j, a.vocab, q);
+        load_tile<true>(d.q, j0, a.vocab, q);
 #pragma unroll
         for (int e = 0; e < PER; ++e) { sp += weight_p(p[e]); sr += weight_rest(p[e], q[e]); }
     } else {
@@ -140,106 +134,100 @@ __global__ __launch_bounds__(256) void verify_sum_k(const VerifyArgs a) {
         for (int e = 0; e < PER; ++e) {
             const double w = weight_p(p[e]);
             sp += w;
-            sr += j + e == d.out ? 0.0 : w;
+            sr += place<true, T>(j0, e) == d.out ? 0.0 : w;
         }
     }
     sp = wave_sum(sp);
     sr = wave_sum(sr);
-    if ((threadIdx.x & 63) == 0) { part[threadIdx.x >> 6][0] = sr; part[threadIdx.x >> 6][1] = sp; }
-    __syncthreads();
-    if (threadIdx.x < 2) {
-        const int w = threadIdx.x;
-        a.sums[((int64_t)b * a.tiles + tile) * 2 + w] = ((part[0][w] + part[1][w]) + part[2][w]) + part[3][w];
+    if ((threadIdx.x & 63) == 0) {
+        double *to = a.sums + ((int64_t)b * a.tiles + tile) * 2;
+        to[0] = sr;
+        to[1] = sp;
+        if (tile == 0) a.taken[b] = A;
     }
 }
 
 template <typename T>
-__global__ __launch_bounds__(256) void verify_pick_k(const VerifyArgs a) {
-    __shared__ double waves[4];
-    __shared__ double before;   // mass in front of the chosen tile
-    __shared__ int hit, last;
-    const int b = blockIdx.x, tid = threadIdx.x;
+__global__ __launch_bounds__(64) void verify_pick_k(const VerifyArgs a) {
+    const int b = blockIdx.x, lane = threadIdx.x;
     int first, k;
     if (!drafts_of(a, b, first, k)) {
-        if (tid == 0) { a.n_accepted[b] = -1; a.next_token[b] = -1; }
+        if (lane == 0) { a.n_accepted[b] = -1; a.next_token[b] = -1; }
         return;
     }
     const int A = a.taken[b];
-    Draw<T> d = draw_of<T>(a, b, first, k, A);
     const double *sums = a.sums + (int64_t)b * a.tiles * 2;
-    const int each = (a.tiles + 255) / 256, t0 = min(tid * each, a.tiles), t1 = min(t0 + each, a.tiles);
-    double mine[2] = {0.0, 0.0}, total;
-    for (int t = t0; t < t1; ++t) { mine[0] += sums[2 * t]; mine[1] += sums[2 * t + 1]; }
-    if (tid == 0) { hit = 0x7fffffff; last = -1; }
-    double upto = block_scan(mine[0], waves, total);
+    const int each = (a.tiles + 63) / 64, t0 = min(lane * each, a.tiles), t1 = min(t0 + each, a.tiles);
+    double rest = 0.0, full = 0.0;
+    for (int t = t0; t < t1; ++t) { rest += sums[2 * t]; full += sums[2 * t + 1]; }
+    const double u = (double)a.u_next[b];
+    Draw<T> d = draw_of<T>(a, b, first, k, A);
+    // sums up to the end of this lane's tiles
+    double upto = wave_scan(rest), total = __shfl(upto, 63, WAVE);
     int which = 0;
     if (A == k || !(total > 0.0)) {  // no draft was refused, or the residual is empty: the target's row
         which = 1;
         d.q = nullptr;
         d.out = -1;
-        upto = block_scan(mine[1], waves, total);
+        rest = full;
+        upto = wave_scan(rest);
+        total = __shfl(upto, 63, WAVE);
     }
-    const double target = (double)a.u_next[b] * total;
-    // the first tile whose end lies beyond the target, or the last one with any weight
-    {
-        double at = upto - mine[which];
-        int full = -1;
-        for (int t = t0; t < t1; ++t) {
-            const double w = sums[2 * t + which];
-            at += w;
-            if (w > 0.0) full = t;
-            if (at > target && w > 0.0) { atomicMin(&hit, t); break; }
+    const double target = u * total;
+    // the first tile whose end lies beyond the target, or the last one with any weight, and the mass in front of it
+    int hit = -1, last = -1;
+    double at = upto - rest, before = 0.0;
+    for (int t = t0; t < t1; ++t) {
+        const double w = sums[2 * t + which];
+        if (w > 0.0 && hit < 0) {
+            last = t;
+            before = at;
+            if (at + w > target) hit = t;
         }
-        if (full >= 0) atomicMax(&last, full);
+        at += w;
     }
-    __syncthreads();
-    const int tile = hit != 0x7fffffff ? hit : last;
-    if (tile < 0) {  // no weight anywhere
-        if (tid == 0) { a.n_accepted[b] = A; a.next_token[b] = 0; }
+    const uint64_t hits = __ballot(hit >= 0), some = __ballot(last >= 0);
+    if (!some) {  // no weight anywhere
+        if (lane == 0) { a.n_accepted[b] = A; a.next_token[b] = 0; }
         return;
     }
-    if (tile >= t0 && tile < t1) {
-        double at = upto - mine[which];
-        for (int t = t0; t < tile; ++t) at += sums[2 * t + which];
-        before = at;
-    }
-    __syncthreads();
-    if (tid == 0) { hit = 0x7fffffff; last = -1; }
-    const int j = tile * VERIFY_TILE + tid * PER;
+    const int from = hits ? __ffsll((unsigned long long)hits) - 1 : 63 - __clzll((long long)some);
+    const int j0 = __shfl(last, from, WAVE) * VERIFY_TILE;
+    before = __shfl(before, from, WAVE);
+    // inside the tile
     float p[PER], q[PER];
     double w[PER], sum = 0.0;
-    load_row(d.p, j, a.vocab, p);
-    if (d.q) load_row(d.q, j, a.vocab, q);
+    load_tile<false>(d.p, j0, a.vocab, p);
+    if (d.q) load_tile<false>(d.q, j0, a.vocab, q);
 #pragma unroll
     for (int e = 0; e < PER; ++e) {
-        w[e] = d.q ? weight_rest(p[e], q[e]) : (j + e == d.out ? 0.0 : weight_p(p[e]));
+        w[e] = d.q ? weight_rest(p[e], q[e]) : (place<false, T>(j0, e) == d.out ? 0.0 : weight_p(p[e]));
         sum += w[e];
     }
-    double at = before + (block_scan(sum, waves, total) - sum);
-    int found = 0x7fffffff, full = -1;
+    at = before + (wave_scan(sum) - sum);
+    int found = -1, behind = -1;
 #pragma unroll
     for (int e = 0; e < PER; ++e) {
         at += w[e];
         if (w[e] > 0.0) {
-            full = j + e;
-            if (found == 0x7fffffff && at > target) found = j + e;
+            behind = place<false, T>(j0, e);
+            if (found < 0 && at > target) found = behind;
         }
     }
-    if (found != 0x7fffffff) atomicMin(&hit, found);
-    if (full >= 0) atomicMax(&last, full);
-    __syncthreads();
-    if (tid == 0) {
+    const uint64_t founds = __ballot(found >= 0), any = __ballot(behind >= 0);
+    const int y = founds ? __shfl(found, __ffsll((unsigned long long)founds) - 1, WAVE) : __shfl(behind, any ? 63 - __clzll((long long)any) : 0, WAVE);
+    if (lane == 0) {
         a.n_accepted[b] = A;
-        a.next_token[b] = hit != 0x7fffffff ? hit : last;
+        a.next_token[b] = max(y, 0);
     }
 }
 
 template <typename T>
 static hipError_t launch_verify_t(const VerifyArgs &a, hipStream_t s) {
-    hipLaunchKernelGGL((verify_sum_k<T>), dim3(a.tiles, a.n_seq), dim3(256), 0, s, a);
+    hipLaunchKernelGGL((verify_sum_k<T>), dim3((a.tiles + 3) / 4, a.n_seq), dim3(256), 0, s, a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((verify_pick_k<T>), dim3(a.n_seq), dim3(256), 0, s, a);
+    hipLaunchKernelGGL((verify_pick_k<T>), dim3(a.n_seq), dim3(64), 0, s, a);
     return hipGetLastError();
 }
 

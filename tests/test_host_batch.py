@@ -92,11 +92,11 @@ def test_workspaces():
     f, g = pk.load().spec_k_attn_shared_workspace, pk.load().spec_k_verify_workspace
     assert f(0, 1, 4, 2, 64, 1, 0, 0) == 0 and f(5, 2, 4, 2, 64, 1, 0, 16) == 0
     assert f(9, 2, 4, 2, 64, 1, 4096, 4096) > 0
-    assert f(2**20, 64, 32, 8, 128, 1, 4096, 4096) >= 2 * 2**20 * 32 * 130 * 4  # beyond 32 bits
+    assert f(2**20, 64, 32, 8, 128, 0, 4096, 4096) >= 2 * 2**20 * 32 * 130 * 4  # beyond 32 bits
     for bad in [(-1, 1, 4, 2, 64, 1, 0, 0), (1, 0, 4, 2, 64, 1, 0, 0), (1, 1, 4, 3, 64, 1, 0, 0), (1, 1, 4, 2, 65, 1, 0, 0), (1, 1, 4, 2, 64, 2, 0, 0),
                 (1, 1, 4, 2, 64, 1, -1, 0), (1, 1, 4, 2, 64, 1, 0, -1), (1, 1, 4, 2, 64, 1, 2**30, 0), (2**30, 1, 4, 2, 64, 1, 0, 0)]:
         assert f(*bad) == E
-    assert g(0, 100) == 0 and g(3, 4096) == 3 * 20 and g(3, 4097) == 3 * 36
+    assert g(0, 100) == 0 and g(3, 1024) == 3 * 20 and g(3, 1025) == 3 * 36
     assert g(-1, 100) == E and g(65536, 100) == E and g(1, 0) == E and g(1, 2**24 + 1) == E
     with pytest.raises(pk.SpecError):
         pk.k_attn_shared_workspace(1, 1, 4, 3, 64, torch.bfloat16, 0, 0)
