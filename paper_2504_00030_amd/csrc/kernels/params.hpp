@@ -284,7 +284,7 @@ struct SharedAttnArgs {
     float *part_ml;   // [R][nq][parts][2]: maximum (times scale2), sum
 };
 
-constexpr int VERIFY_TILE = 1024;  // elements of a row that one wave sums
+constexpr int VERIFY_TILE = 512;  // elements of a row that one wave sums
 
 // Verification against given uniforms (verify.hip).
 struct VerifyArgs {

@@ -70,6 +70,7 @@ template <int HDP_, int QT_, bool EXACT>
 struct CoreBf16 {
     typedef __bf16 T;
     static constexpr int HDP = HDP_, QT = QT_, W = HDP >= 128 ? 8 : HDP / 16, NB = HDP / (16 * W), KC = HDP / 32;
+    static constexpr int ROOM = HDP <= 128 || EXACT ? 2 : 1;  // waves a SIMD that leave it registers enough
     static constexpr bool LATE = HDP == 256;  // walk() loads V when K's registers are free: both do not fit
     // channel of row r of a lane's i-th block of results
     __device__ __forceinline__ static int channel(int i, int r, int g) { return 16 * W * (i / W) + W * (4 * g + r) + i % W; }
@@ -251,6 +252,7 @@ template <int HDP_, bool EXACT>
 struct CoreF32 {
     typedef float T;
     static constexpr int HDP = HDP_, QT = 1, W = HDP >= 64 ? 4 : HDP / 16, NB = HDP / (16 * W), KC = HDP / 16;
+    static constexpr int ROOM = HDP < 128 ? 2 : 1;
     static constexpr bool LATE = HDP == 256;
     __device__ __forceinline__ static int channel(int i, int r, int g) { return 16 * W * (i / W) + W * (4 * g + r) + i % W; }
     f4_t q[1][KC];   // channels 16 c + 4 g ..
@@ -687,7 +689,7 @@ __device__ __forceinline__ void split(const SharedAttnArgs &a, float (*so)[16][C
 
 // Pieces of the prefix as CP, of own positions as CO: the rows of all sequences are more columns than those of one.
 template <class CP, class CO>
-__global__ __launch_bounds__(256, sizeof(typename CP::T) == 2 ? (CP::HDP <= 128 ? 2 : 1) : (CP::HDP < 128 ? 2 : 1)) void attn_split_k(const SharedAttnArgs a) {
+__global__ __launch_bounds__(256, CP::ROOM) void attn_split_k(const SharedAttnArgs a) {
     __shared__ float so[4][16][CP::HDP + 4], sm[4][32], sl[4][32];
     if (std::is_same<CP, CO>::value || workgroup() < a.prefix_groups) split<CP>(a, so, sm, sl);
     else split<CO>(a, so, sm, sl);
@@ -773,101 +775,101 @@ __global__ __launch_bounds__(64 * WAVES, WAVES / 4) void attn_share_k(const Shar
     };
 #pragma unroll 1
     for (int segment = a.through ? 0 : 1; segment < 2; ++segment) {
-    const Piece whole_piece = p;
-    if (segment == 0) {  // the prefix in front of the sequence's own positions
-        p.table = a.prefix_table;
-        p.pages = ((a.prefix_len - 1) >> a.page_shift) + 1;
-        p.len = p.chunk = a.prefix_len;
-        p.begin = 0;
-        p.own = false;
-    }
-    limits(a, p, m0, lim);
-    // positions: of the part that some column sees, and stages that all columns see
-    const int end = min(p.begin + p.chunk, p.sees((min(first + COLS, cols) - 1) / a.g));
-    const int all = (max(0, end - p.begin) + STAGE - 1) / STAGE;
-    int stages = max(0, min(end, p.sees(first / a.g)) - p.begin) / STAGE;
-    if (stages > 0) {  // every wave looks at the same pages and comes to the same answer
-        bool gone = false;
-        const int last = (p.begin + stages * STAGE - 1) >> a.page_shift;
-        for (int i = (p.begin >> a.page_shift) + lane; i <= last; i += 64) gone |= (uint32_t)p.table[min(i, p.pages - 1)] >= (uint32_t)a.n_pages;
-        if (__ballot(gone)) stages = 0;
-    }
-    f4_t s[2][QT][2];
-    auto scores = [&](const uint8_t *ks, int half, f4_t (&to)[QT][2]) {
+        const Piece own = p;
+        if (segment == 0) {  // the prefix in front of the sequence's own positions
+            p.table = a.prefix_table;
+            p.pages = ((a.prefix_len - 1) >> a.page_shift) + 1;
+            p.len = p.chunk = a.prefix_len;
+            p.begin = 0;
+            p.own = false;
+        }
+        limits(a, p, m0, lim);
+        // positions: of the part that some column sees, and stages that all columns see
+        const int end = min(p.begin + p.chunk, p.sees((min(first + COLS, cols) - 1) / a.g));
+        const int all = (max(0, end - p.begin) + STAGE - 1) / STAGE;
+        int stages = max(0, min(end, p.sees(first / a.g)) - p.begin) / STAGE;
+        if (stages > 0) {  // every wave looks at the same pages and comes to the same answer
+            bool gone = false;
+            const int last = (p.begin + stages * STAGE - 1) >> a.page_shift;
+            for (int i = (p.begin >> a.page_shift) + lane; i <= last; i += 64) gone |= (uint32_t)p.table[min(i, p.pages - 1)] >= (uint32_t)a.n_pages;
+            if (__ballot(gone)) stages = 0;
+        }
+        f4_t s[2][QT][2];
+        auto scores = [&](const uint8_t *ks, int half, f4_t (&to)[QT][2]) {
 #pragma unroll
-        for (int h = 0; h < 2; ++h) core.read_k(h, ks, 32 * half + 16 * h + c16, g);
+            for (int h = 0; h < 2; ++h) core.read_k(h, ks, 32 * half + 16 * h + c16, g);
 #pragma unroll
-        for (int t = 0; t < QT; ++t) core.scores(t, to[t]);
-    };
-    if (stages > 0) {
-        auto kst = [&](auto n) -> uint8_t * { return n % 3 == 0 ? k0 : n % 3 == 1 ? k1 : k2; };
-        auto vst = [&](auto n) -> uint8_t * { return n % 3 == 0 ? v0 : n % 3 == 1 ? v1 : v2; };
-        // one half of a stage, whose scores are there; `next` computes those of the half behind it meanwhile
-        auto half_step = [&](const uint8_t *vs, int half, f4_t (&x)[QT][2], auto next) {
-            run.follow(x, a.scale2);
-            next();
-            typename C::Weights w[QT];
-            run.weigh(x, a.scale2, w);
-            core.read_v(vs, 32 * half, g, c16);
-            run.add(core, w);
+            for (int t = 0; t < QT; ++t) core.scores(t, to[t]);
         };
-        __syncthreads();
-        int page = page_at(1);  // of the stage after the next copy's
-        copy(0, page_at(0), k0, v0);
-        if (stages > 1) copy(1, page, k1, v1);
-        page = page_at(2);
-        meet();
-        scores(k0, 0, s[0]);
-        for (int st0 = 0; st0 < stages; st0 += 3) {
-            each<3>([&](auto n) {
-                const int st = st0 + n;
-                if (st >= stages) return;
-                half_step(vst(n), 0, s[0], [&]() { scores(kst(n), 1, s[1]); });
-                // the next stage has arrived; the one before this has been read by all
-                meet();
-                if (st + 2 < stages) {
-                    copy(st + 2, page, kst(num<n + 2>()), vst(num<n + 2>()));
-                    page = page_at(st + 3);
-                }
-                // (behind the last stage: scores of an old one, which nobody reads)
-                half_step(vst(n), 1, s[1], [&]() { scores(kst(num<n + 1>()), 0, s[0]); });
-            });
-        }
-    }
-    const int least = p.sees(min(m0, cols - 1) / a.g);  // positions that all of this wave's columns see
-    for (int st = stages; st < all; ++st) {
-        const int page = page_at(st);
-        const uint64_t there = __ballot((uint32_t)page < (uint32_t)a.n_pages);
-        __syncthreads();
-        copy(st, page, k0, v0);
-        meet();
-#pragma unroll 1
-        for (int half = 0; half < 2; ++half) {
-            const int t0 = p.begin + st * STAGE + 32 * half;
-            scores(k0, half, s[0]);
-            core.read_v(v0, 32 * half, g, c16);
-            uint32_t keep = 0, apart = 0;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const int pos = 16 * (i / 4) + 4 * g + i % 4;
-                const bool seen = (there >> (32 * half + pos) & 1) && t0 + pos < end;
-#pragma unroll
-                for (int t = 0; t < QT; ++t)
-                    if (!seen || t0 + pos >= lim[t]) s[0][t][i / 4][i % 4] = -INFINITY;
-                keep |= (uint32_t)seen << i;
-                apart |= (uint32_t)(t0 + pos >= least) << i;
+        if (stages > 0) {
+            auto kst = [&](auto n) -> uint8_t * { return n % 3 == 0 ? k0 : n % 3 == 1 ? k1 : k2; };
+            auto vst = [&](auto n) -> uint8_t * { return n % 3 == 0 ? v0 : n % 3 == 1 ? v1 : v2; };
+            // one half of a stage, whose scores are there; `next` computes those of the half behind it meanwhile
+            auto half_step = [&](const uint8_t *vs, int half, f4_t (&x)[QT][2], auto next) {
+                run.follow(x, a.scale2);
+                next();
+                typename C::Weights w[QT];
+                run.weigh(x, a.scale2, w);
+                core.read_v(vs, 32 * half, g, c16);
+                run.add(core, w);
+            };
+            __syncthreads();
+            int page = page_at(1);  // of the stage after the next copy's
+            copy(0, page_at(0), k0, v0);
+            if (stages > 1) copy(1, page, k1, v1);
+            page = page_at(2);
+            meet();
+            scores(k0, 0, s[0]);
+            for (int st0 = 0; st0 < stages; st0 += 3) {
+                each<3>([&](auto n) {
+                    const int st = st0 + n;
+                    if (st >= stages) return;
+                    half_step(vst(n), 0, s[0], [&]() { scores(kst(n), 1, s[1]); });
+                    // the next stage has arrived; the one before this has been read by all
+                    meet();
+                    if (st + 2 < stages) {
+                        copy(st + 2, page, kst(num<n + 2>()), vst(num<n + 2>()));
+                        page = page_at(st + 3);
+                    }
+                    // (behind the last stage: scores of an old one, which nobody reads)
+                    half_step(vst(n), 1, s[1], [&]() { scores(kst(num<n + 1>()), 0, s[0]); });
+                });
             }
-            core.forget(keep);
-            if (__ballot(core.clean(apart))) odd = 1;
-            run.follow(s[0], a.scale2);
-            typename C::Weights w[QT];
-            run.weigh(s[0], a.scale2, w);
-            run.add(core, w);
         }
-    }
-    if (uniform(odd)) add_odd(a, p, max(least, p.begin + stages * STAGE), end, 0, 1, lim, run);
-    odd = 0;
-    p = whole_piece;
+        const int least = p.sees(min(m0, cols - 1) / a.g);  // positions that all of this wave's columns see
+        for (int st = stages; st < all; ++st) {
+            const int page = page_at(st);
+            const uint64_t there = __ballot((uint32_t)page < (uint32_t)a.n_pages);
+            __syncthreads();
+            copy(st, page, k0, v0);
+            meet();
+#pragma unroll 1
+            for (int half = 0; half < 2; ++half) {
+                const int t0 = p.begin + st * STAGE + 32 * half;
+                scores(k0, half, s[0]);
+                core.read_v(v0, 32 * half, g, c16);
+                uint32_t keep = 0, apart = 0;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const int pos = 16 * (i / 4) + 4 * g + i % 4;
+                    const bool seen = (there >> (32 * half + pos) & 1) && t0 + pos < end;
+#pragma unroll
+                    for (int t = 0; t < QT; ++t)
+                        if (!seen || t0 + pos >= lim[t]) s[0][t][i / 4][i % 4] = -INFINITY;
+                    keep |= (uint32_t)seen << i;
+                    apart |= (uint32_t)(t0 + pos >= least) << i;
+                }
+                core.forget(keep);
+                if (__ballot(core.clean(apart))) odd = 1;
+                run.follow(s[0], a.scale2);
+                typename C::Weights w[QT];
+                run.weigh(s[0], a.scale2, w);
+                run.add(core, w);
+            }
+        }
+        if (uniform(odd)) add_odd(a, p, max(least, p.begin + stages * STAGE), end, 0, 1, lim, run);
+        odd = 0;
+        p = own;
     }
     const int parts = a.prefix_parts + a.own_parts;
 #pragma unroll

@@ -220,6 +220,61 @@ def test_attention_of_many_columns(rows, own, prefix, nq, nkv, hd, dtype):
     Attn(sum(rows), rows, own, prefix, nq, nkv, hd, 32, dtype).check()
 
 
+@pytest.mark.parametrize("page", [8, 32, 64, 128])
+@pytest.mark.parametrize("prefix", [0, 63, 64, 200, 1000])
+@pytest.mark.parametrize("rows,own,nq,nkv,hd", [([64], [70], 1, 1, 128), ([33, 40], [40, 300], 4, 2, 64), ([150], [150], 2, 2, 32),
+                                                 ([300, 1, 0, 5], [420, 90, 3, 5], 1, 1, 96), ([30, 60], [30, 200], 7, 1, 40)])
+def test_attention_of_columns_that_share_positions(rows, own, nq, nkv, hd, prefix, page):
+    Attn(sum(rows) + prefix, rows, own, prefix, nq, nkv, hd, page, BF16).check()
+
+
+@pytest.mark.parametrize("prefix,page", [(0, 64), (64, 64), (70, 16), (300, 128)])
+@pytest.mark.parametrize("rows,own,hd", [([64] * 6, [64, 65, 100, 130, 64, 90], 32), ([70] * 5 + [3], [70] * 5 + [200], 16), ([130, 100, 140], [130, 164, 150], 64)])
+def test_attention_of_workgroups_that_go_through_prefix_and_own_positions(rows, own, hd, prefix, page):
+    a = Attn(sum(own) + prefix, rows, own, prefix, 32, 32, hd, page, BF16, extra_rows=2)
+    assert (a.check()[-2:] == 3.0).all()
+
+
+@pytest.mark.parametrize("rows,hd,prefix,page", [(128, 32, 70, 16), (256, 64, 130, 64)])
+def test_attention_of_wide_workgroups_that_go_through_prefix_and_own_positions(rows, hd, prefix, page):
+    a = Attn(rows, [rows] * 6, [rows, rows + 1, rows + 70, rows, rows + 3, rows], prefix, 32, 32, hd, page, BF16)
+    assert pk.k_attn_shared_workspace(6 * rows, 6, 32, 32, hd, BF16, prefix, a.table.shape[1] * page) == 0  # nothing is left to join
+    a.check()
+
+
+@pytest.mark.parametrize("nq,nkv,hd,prefix", [(4, 4, 32, 200), (2, 2, 128, 100), (32, 32, 64, 130)])
+def test_attention_of_columns_that_share_positions_with_bounds_that_make_no_sense(nq, nkv, hd, prefix):
+    a = Attn(21, [70, 90], [400, 90], prefix, nq, nkv, hd, 16, BF16, junk=0.25)
+    a.own = [2**31 - 1, 90]
+    a.check()
+    a.table = a.table.copy()
+    a.table[0, 3], a.table[1, 1], a.prefix_table[2] = -7, 10**6, a.k.shape[0]
+    a.check()
+    a.prefix_table[:] = -1
+    a.table[0, :] = 2**31 - 1
+    a.check()
+    for starts in ([-5, 70, 160], [0, 70, 2**31 - 1], [0, 130, 20], [160, 160, 160], [100, 300, -100]):
+        a.row_start = np.array(starts, dtype=np.int32)
+        a.run()
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+@pytest.mark.parametrize("nq,nkv,hd,prefix", [(2, 2, 64, 100), (4, 1, 128, 0), (32, 32, 32, 70), (1, 1, 40, 64)])
+def test_attention_of_columns_that_share_positions_keeps_infinities_to_the_rows_that_see_them(nq, nkv, hd, prefix, bad):
+    rows, own = [80, 100], [80, 150]
+    a, clean = (Attn(12, rows, own, prefix, nq, nkv, hd, 16, BF16) for _ in range(2))
+    g = nq // nkv
+    seen = np.zeros((sum(rows), nq, hd), dtype=bool)
+    for b, j, ch in ((0, 5, 3), (0, 79, 0), (1, 77, 7), (1, 140, 1)):
+        a.v[a.table[b, j // 16], 0, j % 16, ch] = bad
+        seen[a.row_start[b] + j - (own[b] - rows[b]): a.row_start[b + 1], :g, ch] = True
+    a.k[a.table[1, 100 // 16], nkv - 1, 100 % 16, 2] = float("nan")
+    seen[a.row_start[1] + 50:, (nkv - 1) * g:, :] = True
+    got, want = _np(a.run()), _np(clean.run())
+    assert not np.isfinite(got[seen]).any() and np.isfinite(got[~seen]).all()
+    assert np.allclose(got[~seen], want[~seen], rtol=2.0 ** -7, atol=2.0 ** -10)
+
+
 @pytest.mark.parametrize("dtype", [F32, BF16])
 def test_attention_leaves_rows_of_no_sequence_alone(dtype):
     a = Attn(3, [3, 2], [40, 20], 33, 4, 2, 64, 16, dtype, extra_rows=4)
@@ -299,9 +354,9 @@ def test_attention_strides_and_alignment(extra, shift, dtype):
 
 def test_attention_repeats_bit_for_bit():
     for dtype in (F32, BF16):
-        a = Attn(9, [9] * 12, [100] * 12, 2000, 8, 2, 128, 64, dtype)
-        first = a.run()
-        assert all(torch.equal(first, a.run()) for _ in range(3))
+        for a in (Attn(9, [9] * 12, [100] * 12, 2000, 8, 2, 128, 64, dtype), Attn(9, [200], [300], 700, 8, 2, 128, 64, dtype)):
+            first = a.run()
+            assert all(torch.equal(first, a.run()) for _ in range(3))
 
 
 # ---- verification --------------------------------------------------------------------------------------------------

@@ -96,7 +96,7 @@ def test_workspaces():
     for bad in [(-1, 1, 4, 2, 64, 1, 0, 0), (1, 0, 4, 2, 64, 1, 0, 0), (1, 1, 4, 3, 64, 1, 0, 0), (1, 1, 4, 2, 65, 1, 0, 0), (1, 1, 4, 2, 64, 2, 0, 0),
                 (1, 1, 4, 2, 64, 1, -1, 0), (1, 1, 4, 2, 64, 1, 0, -1), (1, 1, 4, 2, 64, 1, 2**30, 0), (2**30, 1, 4, 2, 64, 1, 0, 0)]:
         assert f(*bad) == E
-    assert g(0, 100) == 0 and g(3, 1024) == 3 * 20 and g(3, 1025) == 3 * 36
+    assert g(0, 100) == 0 and g(3, 512) == 3 * 20 and g(3, 513) == 3 * 36
     assert g(-1, 100) == E and g(65536, 100) == E and g(1, 0) == E and g(1, 2**24 + 1) == E
     with pytest.raises(pk.SpecError):
         pk.k_attn_shared_workspace(1, 1, 4, 3, 64, torch.bfloat16, 0, 0)
