@@ -142,18 +142,23 @@ struct CoreBf16 {
             }
         return bad;
     }
-    struct Weights { b8_t p; };
+    // Weights in two bf16 terms, 16 significant bits: these pieces wait for memory, and the second instruction comes free.
+    struct Weights { b8_t p, rest; };
     __device__ __forceinline__ static Weights weights(const f4_t (&s)[2]) {
         Weights x;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) { x.p[i] = (__bf16)s[0][i]; x.p[4 + i] = (__bf16)s[1][i]; }
+        for (int i = 0; i < 8; ++i) {
+            x.p[i] = (__bf16)s[i / 4][i % 4];
+            x.rest[i] = (__bf16)(s[i / 4][i % 4] - (float)x.p[i]);
+        }
         return x;
     }
-    // sums of the weights as they were rounded: a product with ones, which leaves a column's whole sum with all its lanes
+    // sums of the weights as they were rounded: products with ones, which leave a column's whole sum with all its lanes
     __device__ __forceinline__ static void add_up(const Weights &w, f4_t &l) {
         const __bf16 one = (__bf16)1.f;
         const b8_t ones = {one, one, one, one, one, one, one, one};
         l = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, w.p, l, 0, 0, 0);
+        l = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, w.rest, l, 0, 0, 0);
     }
     __device__ __forceinline__ static float total(const f4_t &l) { return l[0]; }
     // channel pair w of block n, positions turned into rows: the first product operand of channels 2 w and 2 w + 1
@@ -179,6 +184,8 @@ struct CoreBf16 {
                     f4_t &x = o[t][n * W + 2 * w], &y = o[t][n * W + 2 * w + 1];
                     x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(even, p[t].p, x, 0, 0, 0);
                     y = __builtin_amdgcn_mfma_f32_16x16x32_bf16(odd_, p[t].p, y, 0, 0, 0);
+                    x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(even, p[t].rest, x, 0, 0, 0);
+                    y = __builtin_amdgcn_mfma_f32_16x16x32_bf16(odd_, p[t].rest, y, 0, 0, 0);
                 }
             }
     }
@@ -238,7 +245,20 @@ struct CoreLds : CoreBf16<HDP_, QT_, EXACT> {
             }
         return bad;
     }
-    __device__ __forceinline__ void values(const typename Base::Weights (&p)[QT], f4_t (&o)[QT][NB]) const {
+    // Weights rounded once: here the matrix units are what bounds the loop.
+    struct Weights { b8_t p; };
+    __device__ __forceinline__ static Weights weights(const f4_t (&s)[2]) {
+        Weights x;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x.p[i] = (__bf16)s[i / 4][i % 4];
+        return x;
+    }
+    __device__ __forceinline__ static void add_up(const Weights &w, f4_t &l) {
+        const __bf16 one = (__bf16)1.f;
+        const b8_t ones = {one, one, one, one, one, one, one, one};
+        l = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, w.p, l, 0, 0, 0);
+    }
+    __device__ __forceinline__ void values(const Weights (&p)[QT], f4_t (&o)[QT][NB]) const {
 #pragma unroll
         for (int n = 0; n < NB; ++n)
 #pragma unroll
