@@ -977,7 +977,7 @@ void plan_shared_attention(SharedAttnArgs &a, int64_t own_capacity) {
     // Columns a workgroup takes: 16 or 32 where its waves split the positions, 64, 128 or 256 where they share them.
     auto kind = [&](int64_t n) {
         if (a.dtype != DT_BF16) return 16;
-        if (n >= 64 && a.hd <= 128) return n > 128 ? 256 : n > 64 ? 128 : 64;
+        if (n > 32 && a.hd <= 128) return n > 128 ? 256 : n > 64 ? 128 : 64;
         return n > 16 && a.hd <= 128 ? 32 : 16;
     };
     a.prefix_cols = kind(columns);
