@@ -748,14 +748,14 @@ __global__ __launch_bounds__(64 * WAVES, WAVES / 4) void attn_share_k(const Shar
     constexpr int UNITS = C::UNITS, BYTES = STAGE * HDP * 2, SHARE = WAVES * 1024, COPIES = BYTES / SHARE, COLS = 16 * QT * WAVES;
     static_assert(COPIES >= 1 && BYTES % SHARE == 0, "every thread copies");
     __shared__ __attribute__((aligned(16))) uint8_t k0[BYTES], k1[BYTES], k2[BYTES], v0[BYTES], v1[BYTES], v2[BYTES];
-    Piece p;
-    if (!piece_of<COLS>(a, workgroup(), p)) return;
+    Piece whole;
+    if (!piece_of<COLS>(a, workgroup(), whole)) return;
     const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), g = lane >> 4, c16 = lane & 15;
-    const int cols = p.n * a.g, first = p.tile * COLS, m0 = first + wave * 16 * QT;
+    const int cols = whole.n * a.g, first = whole.tile * COLS, m0 = first + wave * 16 * QT;
     C core;
     Running<C> run;
     int lim[QT], odd = 0;
-    take_columns(a, p, m0, core);
+    take_columns(a, whole, m0, core);
     run.clear();
     if constexpr (!EXACT) {  // chunks beyond hd are never copied: the products need numbers there
         uint8_t *every[6] = {k0, k1, k2, v0, v1, v2};
@@ -764,38 +764,14 @@ __global__ __launch_bounds__(64 * WAVES, WAVES / 4) void attn_share_k(const Shar
             for (int b = threadIdx.x * 16; b < BYTES; b += SHARE) *reinterpret_cast<u4_t *>(every[i] + b) = u4_t{0, 0, 0, 0};
     }
     const T *kp = reinterpret_cast<const T *>(a.k_pages), *vp = reinterpret_cast<const T *>(a.v_pages);
-    auto page_at = [&](int st) { return p.table[min((p.begin + st * STAGE + lane) >> a.page_shift, p.pages - 1)]; };
     // what this thread copies of a stage: one chunk each of rows i * STEP + mine
     constexpr int STEP = SHARE / 16 / UNITS;
     static_assert(STEP % 16 == 0, "the chunk is the same in each of them");
     const int mine = (wave * 64 + lane) / UNITS, chunk = lane % UNITS ^ C::turn(mine), step = STEP * (EXACT ? HDP : a.hd);
     const uint32_t at = mine * (EXACT ? HDP : a.hd) + chunk * 8;
-    auto copy = [&](int st, int page, uint8_t *ks, uint8_t *vs) {
-        const int t0 = p.begin + st * STAGE;
-        const bool there = EXACT || chunk * 8 < a.hd;
-        if (a.page_shift >= 6) {  // one page
-            const int64_t whole = element(a, uniform(page), p.h, t0);
-            if (there) {
-#pragma unroll
-                for (int i = 0; i < COPIES; ++i) {
-                    copy16(kp + whole + i * step + at, ks + i * SHARE + wave * 1024);
-                    copy16(vp + whole + i * step + at, vs + i * SHARE + wave * 1024);
-                }
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < COPIES; ++i) {  // (every lane takes part in the exchange)
-                const int64_t from = element(a, __shfl(page, i * STEP + mine, WAVE), p.h, t0 + i * STEP + mine) + chunk * 8;
-                if (there) {
-                    copy16(kp + from, ks + i * SHARE + wave * 1024);
-                    copy16(vp + from, vs + i * SHARE + wave * 1024);
-                }
-            }
-        }
-    };
 #pragma unroll 1
     for (int segment = a.through ? 0 : 1; segment < 2; ++segment) {
-        const Piece own = p;
+        Piece p = whole;
         if (segment == 0) {  // the prefix in front of the sequence's own positions
             p.table = a.prefix_table;
             p.pages = ((a.prefix_len - 1) >> a.page_shift) + 1;
@@ -803,15 +779,45 @@ __global__ __launch_bounds__(64 * WAVES, WAVES / 4) void attn_share_k(const Shar
             p.begin = 0;
             p.own = false;
         }
+        auto page_at = [&](int st) { return p.table[min((p.begin + st * STAGE + lane) >> a.page_shift, p.pages - 1)]; };
+        auto copy = [&](int st, int page, uint8_t *ks, uint8_t *vs) {
+            const int t0 = p.begin + st * STAGE;
+            const bool there = EXACT || chunk * 8 < a.hd;
+            if (a.page_shift >= 6) {  // one page
+                const int64_t base = element(a, uniform(page), p.h, t0);
+                if (there) {
+#pragma unroll
+                    for (int i = 0; i < COPIES; ++i) {
+                        copy16(kp + base + i * step + at, ks + i * SHARE + wave * 1024);
+                        copy16(vp + base + i * step + at, vs + i * SHARE + wave * 1024);
+                    }
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < COPIES; ++i) {  // (every lane takes part in the exchange)
+                    const int64_t from = element(a, __shfl(page, i * STEP + mine, WAVE), p.h, t0 + i * STEP + mine) + chunk * 8;
+                    if (there) {
+                        copy16(kp + from, ks + i * SHARE + wave * 1024);
+                        copy16(vp + from, vs + i * SHARE + wave * 1024);
+                    }
+                }
+            }
+        };
         limits(a, p, m0, lim);
         // positions: of the part that some column sees, and stages that all columns see
         const int end = min(p.begin + p.chunk, p.sees((min(first + COLS, cols) - 1) / a.g));
         const int all = (max(0, end - p.begin) + STAGE - 1) / STAGE;
-        int stages = max(0, min(end, p.sees(first / a.g)) - p.begin) / STAGE;
-        if (stages > 0) {  // every wave looks at the same pages and comes to the same answer
+        int stages = max(0, min(end, p.sees(first / a.g)) - p.begin) / STAGE, page = 0;
+        if (stages > 0) {
+            // the first copies set out, and meanwhile every wave looks at the pages and comes to the same answer
+            __syncthreads();
+            const int page0 = page_at(0), page1 = page_at(1);
             bool gone = false;
             const int last = (p.begin + stages * STAGE - 1) >> a.page_shift;
             for (int i = (p.begin >> a.page_shift) + lane; i <= last; i += 64) gone |= (uint32_t)p.table[min(i, p.pages - 1)] >= (uint32_t)a.n_pages;
+            copy(0, page0, k0, v0);
+            if (stages > 1) copy(1, page1, k1, v1);
+            page = page_at(2);  // of the stage after the last copy's
             if (__ballot(gone)) stages = 0;
         }
         f4_t s[2][QT][2];
@@ -833,11 +839,6 @@ __global__ __launch_bounds__(64 * WAVES, WAVES / 4) void attn_share_k(const Shar
                 core.read_v(vs, 32 * half, g, c16);
                 run.add(core, w);
             };
-            __syncthreads();
-            int page = page_at(1);  // of the stage after the next copy's
-            copy(0, page_at(0), k0, v0);
-            if (stages > 1) copy(1, page, k1, v1);
-            page = page_at(2);
             meet();
             scores(k0, 0, s[0]);
             for (int st0 = 0; st0 < stages; st0 += 3) {
@@ -889,24 +890,23 @@ __global__ __launch_bounds__(64 * WAVES, WAVES / 4) void attn_share_k(const Shar
         }
         if (uniform(odd)) add_odd(a, p, max(least, p.begin + stages * STAGE), end, 0, 1, lim, run);
         odd = 0;
-        p = own;
     }
     const int parts = a.prefix_parts + a.own_parts;
 #pragma unroll
     for (int t = 0; t < QT; ++t) {
         const int col = m0 + 16 * t + c16;
         if (col >= cols) continue;
-        const int row = p.row0 + col / a.g, head = p.h * a.g + col % a.g;
+        const int row = whole.row0 + col / a.g, head = whole.h * a.g + col % a.g;
         const float sum = C::total(run.l[t]), inv = 1.f / sum;
-        const int64_t at = ((int64_t)row * a.nq + head) * parts + p.part;
+        const int64_t at = ((int64_t)row * a.nq + head) * parts + whole.part;
         float *po = a.part_o + at * a.hd;
         T *out = reinterpret_cast<T *>(a.out) + (int64_t)row * a.ldo + (int64_t)head * a.hd;
-        if (!p.direct && g == 0) *reinterpret_cast<f2_t *>(a.part_ml + 2 * at) = f2_t{run.m[t], sum};
+        if (!whole.direct && g == 0) *reinterpret_cast<f2_t *>(a.part_ml + 2 * at) = f2_t{run.m[t], sum};
 #pragma unroll
         for (int n = 0; n < C::NB; ++n) {
             const int ch = 16 * n + 4 * g;
             if (!EXACT && ch >= a.hd) continue;
-            if (p.direct) {
+            if (whole.direct) {
 #pragma unroll
                 for (int r = 0; r < 4; ++r) out[ch + r] = (T)(sum == 0.f ? 0.f : run.o[t][n][r] * inv);
             } else {
@@ -991,12 +991,13 @@ void plan_shared_attention(SharedAttnArgs &a, int64_t own_capacity) {
         groups = std::max<int64_t>(groups, 1);
         const int64_t most = std::min<int64_t>((positions + MIN_PART - 1) / MIN_PART, MAX_PARTS);
         if (cols < 64) return std::max<int64_t>(1, std::min((positions + length - 1) / length, most));
-        // one workgroup a compute unit: rounds of 256, each as long as a part and a start (two stages' time)
+        // one workgroup a compute unit, in rounds of 256.  Measured: 2 us a stage, 6 a start, and what the parts' sums take to
+        // be written and read (5 TB/s)
         int64_t best = 1;
         double least = 1e300;
-        const double stages = (double)((positions + STAGE - 1) / STAGE);
+        const double stages = (double)((positions + STAGE - 1) / STAGE), join = 8e-6 / 5.0 * (double)a.R * a.nq * a.hd;
         for (int64_t n = 1; n <= most; ++n) {
-            const double cost = (double)((groups * n + 255) / 256) * (std::ceil(stages / n) + 2.0) + 0.5 * n;
+            const double cost = (double)((groups * n + 255) / 256) * (2.0 * std::ceil(stages / n) + 6.0) + join * n;
             if (cost < least) { least = cost; best = n; }
         }
         return best;

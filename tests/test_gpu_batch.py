@@ -258,6 +258,16 @@ def test_attention_of_columns_that_share_positions_with_bounds_that_make_no_sens
         a.run()
 
 
+def test_attention_through_prefix_and_own_positions_with_pages_outside_the_pool():
+    a = Attn(22, [64] * 6, [64, 64, 130, 200, 64, 64], 200, 32, 32, 32, 16, BF16, junk=0.25)
+    a.table = a.table.copy()
+    a.table[3, 2], a.table[2, 0], a.prefix_table[5] = -1, 2**31 - 1, a.k.shape[0]
+    a.check()
+    a.prefix_table[:] = -1
+    a.own = [2**31 - 1, 0, 3, 200, -5, 64]
+    a.check()
+
+
 @pytest.mark.parametrize("bad", [float("nan"), float("inf")])
 @pytest.mark.parametrize("nq,nkv,hd,prefix", [(2, 2, 64, 100), (4, 1, 128, 0), (32, 32, 32, 70), (1, 1, 40, 64)])
 def test_attention_of_columns_that_share_positions_keeps_infinities_to_the_rows_that_see_them(nq, nkv, hd, prefix, bad):
