@@ -447,6 +447,17 @@ __device__ __forceinline__ bool piece_of(const SharedAttnArgs &a, uint32_t id, P
     return false;
 }
 
+// The prefix in front of a piece of own positions, for the same rows.
+__device__ __forceinline__ Piece prefix_of(const SharedAttnArgs &a, const Piece &own) {
+    Piece p = own;
+    p.table = a.prefix_table;
+    p.pages = ((a.prefix_len - 1) >> a.page_shift) + 1;
+    p.len = p.chunk = a.prefix_len;
+    p.begin = 0;
+    p.own = false;
+    return p;
+}
+
 // Positions a lane loads of one tile, by page.
 struct Places {
     int k[2], v[2];  // pages of the K row of each sixteen and of the V rows' quad
@@ -638,24 +649,28 @@ __device__ __forceinline__ void limits(const SharedAttnArgs &a, const Piece &p, 
 
 // Few columns: the four waves of a workgroup take the same QT x 16 columns and every fourth tile of the positions, and
 // join their sums through shared memory at the end.
-template <class C>
+template <class C, bool THROUGH>
 __device__ __forceinline__ void split(const SharedAttnArgs &a, float (*so)[16][C::HDP + 4], float (*sm)[32], float (*sl)[32]) {
     typedef typename C::T T;
     constexpr int QT = C::QT;
-    Piece p;
-    if (!piece_of<QT * 16>(a, workgroup(), p)) return;
+    Piece whole;
+    if (!piece_of<QT * 16>(a, workgroup(), whole)) return;
     const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), g = lane >> 4, c16 = lane & 15;
-    const int cols = p.n * a.g, m0 = p.tile * QT * 16;
+    const int cols = whole.n * a.g, m0 = whole.tile * QT * 16;
     C core;
     Running<C> run;
-    int lim[QT], odd = 0;
-    take_columns(a, p, m0, core);
-    limits(a, p, m0, lim);
+    take_columns(a, whole, m0, core);
     run.clear();
-    // positions that the first column sees, and those that the last one does within this part
-    const int least = p.sees(m0 / a.g), end = min(p.begin + p.chunk, p.sees((min(m0 + QT * 16, cols) - 1) / a.g));
-    walk(a, p, core, lim, run, p.begin + TILE * wave, 4 * TILE, end, least, odd);
-    if (uniform(odd)) add_odd(a, p, least, end, wave, 4, lim, run);
+#pragma unroll 1
+    for (int segment = THROUGH ? 0 : 1; segment < 2; ++segment) {
+        const Piece p = THROUGH && segment == 0 ? prefix_of(a, whole) : whole;
+        int lim[QT], odd = 0;
+        limits(a, p, m0, lim);
+        // positions that the first column sees, and those that the last one does within this part
+        const int least = p.sees(m0 / a.g), end = min(p.begin + p.chunk, p.sees((min(m0 + QT * 16, cols) - 1) / a.g));
+        walk(a, p, core, lim, run, p.begin + TILE * wave, 4 * TILE, end, least, odd);
+        if (uniform(odd)) add_odd(a, p, least, end, wave, 4, lim, run);
+    }
     // the waves' sums meet: 16 columns at a time
 #pragma unroll
     for (int t = 0; t < QT; ++t) {
@@ -683,8 +698,8 @@ __device__ __forceinline__ void split(const SharedAttnArgs &a, float (*so)[16][C
             f[w] = exp2_(sm[w][16 * t + my] - (top == -INFINITY ? 0.f : top));
             sum += f[w] * sl[w][16 * t + my];
         }
-        const int row = p.row0 + col / a.g, head = p.h * a.g + col % a.g;
-        if (p.direct) {
+        const int row = whole.row0 + col / a.g, head = whole.h * a.g + col % a.g;
+        if (whole.direct) {
             const float inv = 1.f / sum;
             T *dst = reinterpret_cast<T *>(a.out) + (int64_t)row * a.ldo + (int64_t)head * a.hd;
             for (int ch = sub; ch < a.hd; ch += 16) {
@@ -694,7 +709,7 @@ __device__ __forceinline__ void split(const SharedAttnArgs &a, float (*so)[16][C
                 dst[ch] = (T)(sum == 0.f ? 0.f : x * inv);
             }
         } else {
-            const int64_t at = ((int64_t)row * a.nq + head) * parts + p.part;
+            const int64_t at = ((int64_t)row * a.nq + head) * parts + whole.part;
             float *dst = a.part_o + at * a.hd;
             for (int ch = 4 * sub; ch < a.hd; ch += 64) {
                 f4_t x = {0.f, 0.f, 0.f, 0.f};
@@ -707,12 +722,13 @@ __device__ __forceinline__ void split(const SharedAttnArgs &a, float (*so)[16][C
     }
 }
 
-// Pieces of the prefix as CP, of own positions as CO: the rows of all sequences are more columns than those of one.
-template <class CP, class CO>
+// Pieces of the prefix as CP, of own positions as CO: the rows of all sequences are more columns than those of one.  THROUGH:
+// pieces of own positions alone, and each goes through the prefix first.
+template <class CP, class CO, bool THROUGH>
 __global__ __launch_bounds__(256, CP::ROOM) void attn_split_k(const SharedAttnArgs a) {
     __shared__ float so[4][16][CP::HDP + 4], sm[4][32], sl[4][32];
-    if (std::is_same<CP, CO>::value || workgroup() < a.prefix_groups) split<CP>(a, so, sm, sl);
-    else split<CO>(a, so, sm, sl);
+    if (std::is_same<CP, CO>::value || workgroup() < a.prefix_groups) split<CP, THROUGH>(a, so, sm, sl);
+    else split<CO, THROUGH>(a, so, sm, sl);
 }
 
 // f(num<0>) .. f(num<N - 1>)
@@ -771,14 +787,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES / 4) void attn_share_k(const Shar
     const uint32_t at = mine * (EXACT ? HDP : a.hd) + chunk * 8;
 #pragma unroll 1
     for (int segment = a.through ? 0 : 1; segment < 2; ++segment) {
-        Piece p = whole;
-        if (segment == 0) {  // the prefix in front of the sequence's own positions
-            p.table = a.prefix_table;
-            p.pages = ((a.prefix_len - 1) >> a.page_shift) + 1;
-            p.len = p.chunk = a.prefix_len;
-            p.begin = 0;
-            p.own = false;
-        }
+        const Piece p = segment == 0 ? prefix_of(a, whole) : whole;
         auto page_at = [&](int st) { return p.table[min((p.begin + st * STAGE + lane) >> a.page_shift, p.pages - 1)]; };
         auto copy = [&](int st, int page, uint8_t *ks, uint8_t *vs) {
             const int t0 = p.begin + st * STAGE;
@@ -1015,9 +1024,11 @@ void plan_shared_attention(SharedAttnArgs &a, int64_t own_capacity) {
         a.own_parts = (int)parts(own_capacity, own_tiles * a.nkv, a.own_cols);
         a.own_groups64 = (int64_t)a.own_tiles * a.nkv * a.own_parts;
     }
-    // Enough workgroups without sharing out the prefix: each goes through prefix and own positions by itself, and nothing is
-    // left to join.
-    a.through = a.prefix_len > 0 && own_capacity > 0 && a.own_cols >= 64 && (columns + a.own_cols - 1) / a.own_cols * a.nkv >= 192;
+    // A workgroup goes through prefix and own positions by itself, and nothing is left to join, where there are enough of them
+    // without sharing out the prefix, or so little to go through that the second launch would take longer.
+    const int64_t groups = (a.own_cols >= 64 ? (columns + a.own_cols - 1) / a.own_cols : own_tiles) * a.nkv;
+    const bool most = groups >= 192 && (a.own_cols >= 64 || (a.prefix_cols >= 64 && a.prefix_len <= 1024 && own_capacity <= 1024));
+    a.through = a.prefix_len > 0 && own_capacity > 0 && (most || (a.own_cols < 64 && a.prefix_len + own_capacity <= 384));
     if (a.through) {
         a.prefix_parts = 0;
         a.prefix_groups64 = 0;
@@ -1039,7 +1050,8 @@ static hipError_t launch_cols(const SharedAttnArgs &a, int prefix_cols, int own_
     typedef CoreBf16<HDP, 1, EXACT> One;
     if (a.dtype == DT_F32) {
         typedef CoreF32<HDP, EXACT> C;
-        hipLaunchKernelGGL((attn_split_k<C, C>), grid, block, 0, s, a);
+        if (a.through) hipLaunchKernelGGL((attn_split_k<C, C, true>), grid, block, 0, s, a);
+        else hipLaunchKernelGGL((attn_split_k<C, C, false>), grid, block, 0, s, a);
         return hipGetLastError();
     }
     if constexpr (HDP <= 128) {
@@ -1050,13 +1062,15 @@ static hipError_t launch_cols(const SharedAttnArgs &a, int prefix_cols, int own_
             case 128: hipLaunchKernelGGL((attn_share_k<HDP, 2, 4, EXACT>), grid, block, 0, s, a); return hipGetLastError();
             case 64: hipLaunchKernelGGL((attn_share_k<HDP, 1, 4, EXACT>), grid, block, 0, s, a); return hipGetLastError();
             case 32:
-                if (own_cols == 32) hipLaunchKernelGGL((attn_split_k<Two, Two>), grid, block, 0, s, a);
-                else hipLaunchKernelGGL((attn_split_k<Two, One>), grid, block, 0, s, a);
+                if (a.through) hipLaunchKernelGGL((attn_split_k<Two, Two, true>), grid, block, 0, s, a);
+                else if (own_cols == 32) hipLaunchKernelGGL((attn_split_k<Two, Two, false>), grid, block, 0, s, a);
+                else hipLaunchKernelGGL((attn_split_k<Two, One, false>), grid, block, 0, s, a);
                 return hipGetLastError();
             default: break;
         }
     }
-    hipLaunchKernelGGL((attn_split_k<One, One>), grid, block, 0, s, a);
+    if (a.through) hipLaunchKernelGGL((attn_split_k<One, One, true>), grid, block, 0, s, a);
+    else hipLaunchKernelGGL((attn_split_k<One, One, false>), grid, block, 0, s, a);
     return hipGetLastError();
 }
 

@@ -198,6 +198,19 @@ def test_attention_head_layouts(nq, nkv, hd, dtype):
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("hd", [32, 24, 64, 40, 128, 80, 256, 200])
+@pytest.mark.parametrize("rows,own,prefix,heads", [
+    ([1, 2], [500, 3], 130, 2), ([1, 2], [90, 3], 100, 2),       # up to 16 columns: parts, and through prefix and own positions
+    ([5] * 5, [400, 5, 70, 5, 33], 300, 2), ([5] * 5, [100, 5, 70, 5, 33], 90, 2),  # 25 for the prefix, 5 for a sequence
+    ([20, 18], [400, 18], 200, 1), ([20, 18], [100, 18], 70, 1),  # up to 32
+    ([1] * 40, [300] + [2] * 39, 150, 1),                        # 40 for the prefix, one for a sequence
+    ([40], [400], 200, 1), ([70], [200], 200, 1), ([140], [400], 200, 1),  # 64, 128 and 256 that share positions
+    ([1] * 100, [20] * 100, 70, 2)])                             # enough of them to go through a prefix that 100 columns share
+def test_attention_of_every_width_and_head_size(rows, own, prefix, heads, hd, dtype):
+    Attn(hd + sum(rows), rows, own, prefix, heads, heads, hd, 16, dtype).check()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("page", [8, 16, 32, 64, 128])
 @pytest.mark.parametrize("prefix", [0, 1, 31, 64, 200])
 def test_attention_pages_and_prefixes(prefix, page, dtype):
