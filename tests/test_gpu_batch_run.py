@@ -159,6 +159,37 @@ def test_passes_on_two_streams_with_workspaces_of_their_own():
             assert all(torch.equal(t, u) for t, u in zip(a.results(), w))
 
 
+@pytest.mark.parametrize("rows", [3, 100])
+def test_caches_beyond_32_bit_offsets(rows):
+    """Pools of more than 2^31 elements: pages at their ends hold what pages of a small pool hold, and attention reads the same."""
+    page, nkv, hd, n = 64, 8, 128, 150
+    s = torch.cuda.current_stream().cuda_stream
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    qkv = torch.randn((n, (8 + 2 * nkv) * hd), generator=gen, device="cuda").to(torch.bfloat16)
+    q, k, v = qkv[:, : 8 * hd].unflatten(1, (8, hd)), qkv[:, 8 * hd: 16 * hd].unflatten(1, (nkv, hd)), qkv[:, 16 * hd:].unflatten(1, (nkv, hd))
+    cos, sin = torch.rand((n, hd // 2), generator=gen, device="cuda"), torch.rand((n, hd // 2), generator=gen, device="cuda")
+    got = []
+    for n_pages in (5, 34000):
+        pools = [torch.empty((n_pages, nkv, page, hd), dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+        assert n_pages == 5 or pools[0].numel() > 2**31
+        table = [n_pages - 1, n_pages - 3, n_pages - 2]
+        slot = _i32([table[j // page] * page + j % page for j in range(n)])
+        out, qo = torch.zeros((rows, 8, hd), dtype=torch.bfloat16, device="cuda"), torch.zeros((n, 8, hd), dtype=torch.bfloat16, device="cuda")
+        pk.k_rope_cache(q, k, v, cos, sin, _i32(range(n)), slot, qo, *pools, stream=s)
+        work = torch.empty(max(1, pk.k_attn_shared_workspace(rows, 1, 8, nkv, hd, torch.bfloat16, page, 2 * page)), dtype=torch.uint8, device="cuda")
+        pk.k_attn_shared(qo[-rows:], *pools, _i32([0, rows]), _i32([table[1:]]), _i32([n - page]), out, work, prefix_table=_i32(table[:1]),
+                         prefix_len=page, stream=s)
+        torch.cuda.synchronize()
+        got.append((qo, out, *[p[table].clone() for p in pools]))
+        del pools
+    places = torch.arange(3 * page, device="cuda") < n  # (places behind the last position were never written)
+    for i, (a, b) in enumerate(zip(*got)):
+        if i < 2:
+            assert a.any() and torch.equal(a, b)
+        else:
+            assert torch.equal(a.transpose(1, 2).flatten(0, 1)[places], b.transpose(1, 2).flatten(0, 1)[places])
+
+
 CHILD = """
 import sys
 sys.path.insert(0, "tests")

@@ -30,7 +30,7 @@ def _rope(q=P, ldq=256, nq=2, k=P, ldk=128, v=P, ldv=128, nkv=1, dtype=0, hd=128
                                        n_pages, page, ot, None)
 
 
-def _attn(q=P, ldq=256, nq=4, nkv=2, hd=64, dtype=1, R=3, rows=P, n_seq=2, k=P, v=P, n_pages=8, page=16, pt=P, prefix=20, table=P, tp=2,
+def _attn(q=P, ldq=256, nq=4, nkv=2, hd=64, dtype=1, R=3, rows=P, n_seq=2, k=P, v=P, n_pages=8, page=16, pt=P, prefix=500, table=P, tp=20,
           own=P, scale=0.125, out=P, ldo=256, work=P, nb=1 << 30):
     return pk.load().spec_k_attn_shared(q, ldq, nq, nkv, hd, dtype, R, rows, n_seq, k, v, n_pages, page, pt, prefix, table, tp, own, scale, out,
                                         ldo, work, nb, None)
