@@ -77,15 +77,15 @@ int spec_k_rope_cache(const void *q, int64_t ldq, int32_t nq, const void *k, int
  * rows are the last n: its row i sees the prefix and own positions 0 .. own_len[b] - n + i.
  *     o = sum_j softmax_j(scale * q . k_j) v_j  over the positions seen;  a row that sees none gets zeros.
  * q, out: device, dtype, head i of row r at element r * ld + i * hd; query head i reads cache head i / (nq / nkv).  Queries, pages and
- * results have one type: SPEC_BF16 (matrix units; scores, weights' sums and results in fp32, the weights rounded to bf16 in
- * front of the values' product: another 2^-8 of each term at most) or SPEC_F32 (fp32 throughout).
+ * results have one type: SPEC_BF16 (scores, weights' sums and results are held in fp32; in front of the values' product the weights
+ * are rounded to two bf16 terms, or, where a sequence has many rows, to one: 2^-8 of each term at most) or SPEC_F32 (fp32 throughout).
  * row_start: device int32 [n_seq + 1]; own_len: device int32 [n_seq]; table: device int32 [n_seq][table_pages], the page of own
  * positions p * page_tokens ..; prefix_table: device int32 [ceil(prefix_len / page_tokens)], the pages of the prefix (NULL where
  * prefix_len is 0).  The own positions begin with a page of their own, wherever the prefix ends.  Rows in front of row_start[0]
  * and from row_start[n_seq] on are left as they were.  Bounds in device memory are never trusted: rows are those within 0 .. R,
  * own_len counts at most table_pages * page_tokens, and positions on pages outside the pool are not seen.  What lies in the pages
  * behind a sequence's end, or at positions that a row does not see, does not reach that row, NaN and infinities included.
- * 8 <= hd <= 256, hd % 8 == 0; nq a multiple of nkv; 1 <= n_seq <= 65536; scale > 0; prefix_len and table_pages * page_tokens below
+ * 8 <= hd <= 256, hd % 8 == 0; nq a multiple of nkv, at most 65536; 1 <= n_seq <= 65536; scale > 0; prefix_len and table_pages * page_tokens below
  * 2^30 (table_pages may be 0: prefix alone); R * nq <= 2^30.  Scores times 1.45 have to stay within fp32's range.  workspace: device scratch, 16-byte aligned, of at least
  * spec_k_attn_shared_workspace() bytes for these sizes (0: NULL will do).  The same call gives the same bits every time. */
 int spec_k_attn_shared(const void *q, int64_t ldq, int32_t nq, int32_t nkv, int32_t hd, int32_t dtype, int32_t R,

@@ -6,12 +6,14 @@
 // S^T = K Q^T (16 positions x 16 columns an instruction), then O^T += V^T P^T.  Transposed, column c of S, P and O is held by
 // lanes c, c + 16, c + 32, c + 48, so m, l and the rescaling are one number a lane, and what a lane holds of S^T (positions
 // 4 g .. 4 g + 3 of each 16, g = lane / 16) is, rounded, its share of the second product's operand: no exchange between lanes
-// and no shared memory in the loop.  The positions' order inside a product is free, so a lane loads the rows of V for just
+// and no shared memory needed in between.  The positions' order inside a product is free, so a lane loads the rows of V for just
 // those positions, 16 bytes of each, and turns 2 x 2 blocks in registers.  Which channels a lane holds is free too: lane
 // l % 16 takes W neighbours, so loads and stores are whole vectors.
 //
 // Pieces.  The prefix is read once for all rows (columns: every row of the batch), the own positions once a sequence; either
-// is split into parts along the positions, and a second kernel joins the parts of a row.
+// is split into parts along the positions, and a second kernel joins the parts of a row.  Two kernels, by columns: up to 32 a
+// workgroup's waves split the positions (bound by memory), from 33 on they share them (bound by the issue of instructions beside
+// the matrix units).  4 sequences of 48 columns, 8000 positions: 55 us split, 41 shared; 64 of 36 columns, 1000: 90 and 76.
 #include "common.hpp"
 #include "params.hpp"
 
@@ -648,7 +650,9 @@ __device__ __forceinline__ void limits(const SharedAttnArgs &a, const Piece &p, 
 }  // namespace
 
 // Few columns: the four waves of a workgroup take the same QT x 16 columns and every fourth tile of the positions, and
-// join their sums through shared memory at the end.
+// join their sums through shared memory at the end.  8 sequences of 40 heads of 128, 2001 + up to 4096 positions: 84 us for
+// 398 MB, 4.7 TB/s (read only; a copy reaches 6.1 both ways).  One token behind 356 positions: 7.7, a chain of dependent loads
+// (row numbers, pages, keys).
 template <class C, bool THROUGH>
 __device__ __forceinline__ void split(const SharedAttnArgs &a, float (*so)[16][C::HDP + 4], float (*sm)[32], float (*sl)[32]) {
     typedef typename C::T T;
@@ -757,6 +761,10 @@ __device__ __forceinline__ void copy16(const void *from, uint8_t *to) {
 // Many columns: every wave has QT x 16 of its own, and those of a workgroup share the positions, which pass through shared
 // memory in stages of 64, three in turn.  The loop is for whole stages that all columns see; the positions behind them, and
 // pieces with pages outside the pool, follow stage by stage.
+// 8 x 256 rows of 32 heads of 128 on 8 behind 8192 positions (256 columns, eight waves of 32): 270 us, 1.03 PFLOP/s, about 2 us a
+// stage: the matrix units are half busy, beside them a wave issues 16 exponentials, 16 multiply-adds, 8 conversions and 24 LDS
+// reads for its 34 matrix instructions.  Four waves of 64 columns read LDS half as often, but what ends in the second half of
+// the register file has to be moved: 352.  Turning values by permutes costs 32 instructions more: 307.
 template <int HDP, int QT, int WAVES, bool EXACT>
 __global__ __launch_bounds__(64 * WAVES, WAVES / 4) void attn_share_k(const SharedAttnArgs a) {
     typedef CoreLds<HDP, QT, EXACT> C;
@@ -926,7 +934,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES / 4) void attn_share_k(const Shar
 }
 
 // The parts of one row and head, a wave each: LPP lanes hold four neighbouring channels each, 64 / LPP parts at a time, four of
-// these on their way.
+// these on their way (319 rows of 32 heads, eight parts: 10 us, 42 MB; 24 rows of 40 heads, one part at a time: 21, so 5).
 template <typename T, int LPP>
 __global__ __launch_bounds__(256) void attn_join_k(const SharedAttnArgs a) {
     const uint32_t item = workgroup() * 4 + (threadIdx.x >> 6);  // below 2^31: the host bounds R * nq
@@ -993,9 +1001,12 @@ void plan_shared_attention(SharedAttnArgs &a, int64_t own_capacity) {
     a.own_cols = kind(each_seq);
     const int64_t prefix_tiles = a.prefix_len > 0 ? (columns + a.prefix_cols - 1) / a.prefix_cols : 0;
     const int64_t own_tiles = own_capacity > 0 ? std::max<int64_t>((columns + a.own_cols - 1) / a.own_cols, a.n_seq) : 0;
-    // Pieces whose waves split the positions, of prefix and own together: a thousand workgroups, parts of the same length
+    // Pieces whose waves split the positions, of prefix and own together: a thousand workgroups, parts of the same length; no
+    // shorter ones than 512 where the pieces are enough by themselves (16 sequences of 40 fp32 heads, 500 positions behind
+    // 500: 88 us in two parts, 76 in one)
+    const int64_t pieces = a.nkv * ((a.prefix_cols < 64 ? prefix_tiles : 0) + (a.own_cols < 64 ? own_tiles : 0));
     const int64_t work = a.nkv * ((a.prefix_cols < 64 ? prefix_tiles * a.prefix_len : 0) + (a.own_cols < 64 ? own_tiles * own_capacity : 0));
-    const int64_t length = std::max<int64_t>(MIN_PART, (work + 1023) / 1024);
+    const int64_t length = std::max<int64_t>(pieces >= 512 ? 512 : MIN_PART, (work + 1023) / 1024);
     auto parts = [&](int64_t positions, int64_t groups, int cols) -> int64_t {
         groups = std::max<int64_t>(groups, 1);
         const int64_t most = std::min<int64_t>((positions + MIN_PART - 1) / MIN_PART, MAX_PARTS);
@@ -1025,7 +1036,9 @@ void plan_shared_attention(SharedAttnArgs &a, int64_t own_capacity) {
         a.own_groups64 = (int64_t)a.own_tiles * a.nkv * a.own_parts;
     }
     // A workgroup goes through prefix and own positions by itself, and nothing is left to join, where there are enough of them
-    // without sharing out the prefix, or so little to go through that the second launch would take longer.
+    // without sharing out the prefix (8 x 256 rows behind 8192 positions: 285 us, 307 in parts; few columns, whose prefix would take
+    // a launch of its own: 32 tokens behind 512 + 512 positions 22 and 31, behind 1000 + 1000 43 and 53), or so little to go
+    // through that the second launch would take longer (one token behind 356 positions 7.7 and 8.4, behind 512 10.7 and 8.4).
     const int64_t groups = (a.own_cols >= 64 ? (columns + a.own_cols - 1) / a.own_cols : own_tiles) * a.nkv;
     const bool most = groups >= 192 && (a.own_cols >= 64 || (a.prefix_cols >= 64 && a.prefix_len <= 1024 && own_capacity <= 1024));
     a.through = a.prefix_len > 0 && own_capacity > 0 && (most || (a.own_cols < 64 && a.prefix_len + own_capacity <= 384));

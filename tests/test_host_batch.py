@@ -63,7 +63,7 @@ def test_rotation_refuses(bad):
 
 
 @pytest.mark.parametrize("bad", [dict(q=None), dict(rows=None), dict(k=None), dict(v=None), dict(pt=None), dict(table=None), dict(own=None), dict(out=None),
-                                 dict(work=None), dict(nb=100), dict(nb=-1), dict(dtype=2), dict(dtype=3), dict(nq=3), dict(nq=0), dict(nkv=0), dict(nkv=-2),
+                                 dict(work=None), dict(nb=100), dict(nb=-1), dict(dtype=2), dict(dtype=3), dict(nq=3), dict(nq=0), dict(nkv=0), dict(nkv=-2), dict(nq=2**17, R=1, ldq=2**24, ldo=2**24),
                                  dict(hd=4), dict(hd=60), dict(hd=264), dict(R=-1), dict(R=2**30), dict(n_seq=0), dict(n_seq=65537), dict(page=4), dict(page=48),
                                  dict(n_pages=0), dict(n_pages=2**27), dict(prefix=-1), dict(prefix=2**30), dict(tp=-1), dict(tp=2**26), dict(scale=0.0),
                                  dict(scale=-1.0), dict(scale=NAN), dict(scale=INF), dict(scale=3e38), dict(ldq=255), dict(ldo=200), dict(q=P + 1), dict(out=P + 1), dict(k=P + 8),
