@@ -1920,7 +1920,7 @@ int spec_k_rope_cache(const void *q, int64_t ldq, int32_t nq, const void *k, int
 // The sizes of an attention call in `a`; false where they are refused.
 static bool shared_sizes(SharedAttnArgs &a, int32_t R, int32_t n_seq, int32_t nq, int32_t nkv, int32_t hd, int32_t dtype,
                          int32_t prefix_len, int64_t own_capacity) {
-    if (!wide(dtype) || R < 0 || n_seq < 1 || n_seq > 65536 || nq < 1 || nkv < 1 || nq > 65536 || nq % nkv || hd < 8 || hd > 256 || hd % 8 ||
+    if (!wide(dtype) || R < 0 || n_seq < 1 || n_seq > 4096 || nq < 1 || nkv < 1 || nq > 65536 || nq % nkv || hd < 8 || hd > 256 || hd % 8 ||
         prefix_len < 0 || prefix_len >= 1 << 30 || own_capacity < 0 || own_capacity >= 1 << 30 || (int64_t)R * nq > 1 << 30)
         return false;
     a.dtype = dtype; a.R = R; a.n_seq = n_seq; a.nq = nq; a.nkv = nkv; a.g = nq / nkv; a.hd = hd; a.prefix_len = prefix_len;
@@ -1946,7 +1946,7 @@ int spec_k_attn_shared(const void *q, int64_t ldq, int32_t nq, int32_t nkv, int3
         return refuse(SPEC_EINVAL, "attn_shared: page_tokens must be a power of two from 8 to 2^20, and the pool hold 1 to 2^31 - 1 slots");
     SharedAttnArgs a{};
     if (table_pages < 0 || !shared_sizes(a, R, n_seq, nq, nkv, hd, dtype, prefix_len, (int64_t)table_pages << shift))
-        return refuse(SPEC_EINVAL, "attn_shared: fp32 or bf16; hd a multiple of 8 up to 256, nq one of nkv up to 65536, 1 to 65536 sequences, R * nq up to 2^30, prefix and tables below 2^30 positions");
+        return refuse(SPEC_EINVAL, "attn_shared: fp32 or bf16; hd a multiple of 8 up to 256, nq one of nkv up to 65536, 1 to 4096 sequences, R * nq up to 2^30, prefix and tables below 2^30 positions");
     a.scale2 = (float)((double)scale * 1.4426950408889634);
     if (!(scale > 0.f) || !(a.scale2 > 0.f) || !std::isfinite(a.scale2)) return refuse(SPEC_EINVAL, "attn_shared: scale must be positive and finite");
     if (ldq < (int64_t)nq * hd || ldo < (int64_t)nq * hd || workspace_bytes < 0) return refuse(SPEC_EINVAL, "attn_shared: row stride below the heads' width");

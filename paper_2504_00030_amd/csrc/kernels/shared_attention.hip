@@ -28,7 +28,6 @@ namespace {
 typedef float f4_t __attribute__((ext_vector_type(4)));
 typedef float f2_t __attribute__((ext_vector_type(2)));
 typedef __bf16 b8_t __attribute__((ext_vector_type(8)));
-typedef __bf16 b2_t __attribute__((ext_vector_type(2)));
 typedef uint32_t u4_t __attribute__((ext_vector_type(4)));
 
 constexpr int TILE = 32;      // positions a wave takes at a time
@@ -36,16 +35,13 @@ constexpr int MIN_PART = 128; // least positions of a part: a tile for each of a
 constexpr int MAX_PARTS = 64;
 constexpr int STAGE = 64;     // positions of a stage in shared memory
 
-template <int N> struct words { uint32_t w[N]; };
-template <int BYTES, typename E> struct vec_of;
-template <> struct vec_of<16, uint32_t> { typedef uint32_t type __attribute__((ext_vector_type(4))); };
-template <> struct vec_of<8, uint32_t> { typedef uint32_t type __attribute__((ext_vector_type(2))); };
-template <> struct vec_of<4, uint32_t> { typedef uint32_t type; };
+template <int N> struct words { typedef uint32_t type __attribute__((ext_vector_type(N))); };
+template <> struct words<1> { typedef uint32_t type; };
 
 // N words from N * 4-byte aligned memory
 template <int N>
 __device__ __forceinline__ void load_words(const void *p, uint32_t (&w)[N]) {
-    const typename vec_of<N * 4, uint32_t>::type v = *reinterpret_cast<const typename vec_of<N * 4, uint32_t>::type *>(p);
+    const typename words<N>::type v = *reinterpret_cast<const typename words<N>::type *>(p);
     if constexpr (N == 1) w[0] = v;
     else {
 #pragma unroll
@@ -386,7 +382,8 @@ struct Piece {
     __device__ __forceinline__ int sees(int row) const { return own ? max(0, len - n + row + 1) : len; }  // positions
 };
 
-// Which piece workgroup `id` has: prefix pieces first, tiles of `cols` columns.  false: none.  Same answer in every wave.
+// Which piece workgroup `id` has: prefix pieces first, tiles of COLS columns.  false: none.  Same answer in every wave.  Sequences
+// are looked through sixty-four at a time, a load and seven exchanges each.
 template <int COLS>
 __device__ __forceinline__ bool piece_of(const SharedAttnArgs &a, uint32_t id, Piece &p) {
     if (id < a.prefix_groups) {

@@ -221,7 +221,7 @@ def test_attention_pages_and_prefixes(prefix, page, dtype):
 @pytest.mark.parametrize("rows,own,prefix", [
     ([1], [1], 0), ([1], [0], 0), ([1], [0], 1), ([3], [1], 0), ([3], [1], 5), ([2, 0, 3], [0, 9, 2], 0), ([0, 0, 1], [4, 4, 4], 3),
     ([33], [33], 0), ([70], [90], 10), ([1], [1500], 0), ([1], [0], 1500), ([2, 1], [1300, 3], 700), ([1] * 70, list(range(1, 71)), 40),
-    ([3, 1, 2] * 30, [9, 1, 130] * 30, 130), ([4, 2], [-3, 6], 9), ([4, 2], [-2**31, 6], 0), ([130, 1], [200, 1], 70)])
+    ([3, 1, 2] * 30, [9, 1, 130] * 30, 130), ([4, 2], [-3, 6], 9), ([4, 2], [-2**31, 6], 0), ([130, 1], [200, 1], 70), ([1, 0, 2] * 100, [9, 3, 40] * 100, 20)])
 def test_attention_lengths(rows, own, prefix, dtype):
     Attn(len(rows) + prefix, rows, own, prefix, 4, 2, 32, 16, dtype).check()
 

@@ -1,5 +1,7 @@
 """Refusals of the operators of include/spec_batch.h, before anything reaches a GPU, and the sizes of their workspaces."""
 import ctypes as C
+import os
+import re
 
 import numpy as np
 import pytest
@@ -7,7 +9,7 @@ import torch
 
 import batch_reference as ref
 import paper_2504_00030_amd as pk
-from paper_2504_00030_amd import binding
+from paper_2504_00030_amd import binding, build
 
 E = binding.SPEC_EINVAL
 P = 1 << 20  # stands for a device pointer: aligned, never read
@@ -64,7 +66,7 @@ def test_rotation_refuses(bad):
 
 @pytest.mark.parametrize("bad", [dict(q=None), dict(rows=None), dict(k=None), dict(v=None), dict(pt=None), dict(table=None), dict(own=None), dict(out=None),
                                  dict(work=None), dict(nb=100), dict(nb=-1), dict(dtype=2), dict(dtype=3), dict(nq=3), dict(nq=0), dict(nkv=0), dict(nkv=-2), dict(nq=2**17, R=1, ldq=2**24, ldo=2**24),
-                                 dict(hd=4), dict(hd=60), dict(hd=264), dict(R=-1), dict(R=2**30), dict(n_seq=0), dict(n_seq=65537), dict(page=4), dict(page=48),
+                                 dict(hd=4), dict(hd=60), dict(hd=264), dict(R=-1), dict(R=2**30), dict(n_seq=0), dict(n_seq=4097), dict(page=4), dict(page=48),
                                  dict(n_pages=0), dict(n_pages=2**27), dict(prefix=-1), dict(prefix=2**30), dict(tp=-1), dict(tp=2**26), dict(scale=0.0),
                                  dict(scale=-1.0), dict(scale=NAN), dict(scale=INF), dict(scale=3e38), dict(ldq=255), dict(ldo=200), dict(q=P + 1), dict(out=P + 1), dict(k=P + 8),
                                  dict(v=P + 2), dict(rows=P + 2), dict(own=P + 1), dict(table=P + 2), dict(pt=P + 2), dict(work=P + 8)])
@@ -186,3 +188,16 @@ def test_reference_attention_and_verification():
     assert A.tolist() == [1] and y.tolist() == [2]  # u w = 0.25 is not exceeded by 0.25
     A, y = ref.verify(p, np.array([[1.0, 0.0, 0.0]]), [0, 1], [0], [0.5], [0.25])
     assert A.tolist() == [0] and y.tolist() == [1]
+
+
+# ---- what the compiler made of the attention kernels ---------------------------------------------------------------
+def test_attention_kernels_keep_their_registers():
+    """No instance spills: a register reloaded from scratch memory in the loop would wait for the copies in flight behind it."""
+    path = os.path.join(build.BUILD, "kernels_shared_attention.hip.s")
+    if not os.path.exists(path):
+        pytest.skip("the library was not built here")
+    with open(path) as f:
+        asm = f.read()
+    names, spills = re.findall(r"\.symbol:\s+(\S+)\.kd", asm), [int(n) for n in re.findall(r"\.vgpr_spill_count:\s+(\d+)", asm)]
+    assert len(names) == len(spills) and sum("attn_share_k" in n for n in names) == 18 and sum("attn_split_k" in n for n in names) >= 40
+    assert not any(spills), [n for n, s in zip(names, spills) if s]
