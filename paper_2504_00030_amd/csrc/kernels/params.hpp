@@ -279,6 +279,7 @@ struct SharedAttnArgs {
     int32_t prefix_cols, own_cols, prefix_parts, prefix_chunk, own_parts;  // columns of a workgroup, parts along the positions
     bool through;     // a workgroup goes through the prefix and the own positions of its columns
     uint32_t prefix_groups, own_tiles;
+    uint32_t groups;  // workgroups of a launch that have work
     int64_t prefix_groups64, own_groups64;
     float *part_o;    // [R][nq][parts][hd]
     float *part_ml;   // [R][nq][parts][2]: maximum (times scale2), sum

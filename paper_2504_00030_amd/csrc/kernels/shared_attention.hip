@@ -386,6 +386,7 @@ struct Piece {
 // are looked through sixty-four at a time, a load and seven exchanges each.
 template <int COLS>
 __device__ __forceinline__ bool piece_of(const SharedAttnArgs &a, uint32_t id, Piece &p) {
+    if (id >= a.groups) return false;  // a long grid ends in whole rows
     if (id < a.prefix_groups) {
         // tiles outermost: the workgroups that read one head's part follow each other at a distance of heads x parts,
         // a multiple of eight where the heads are, so that they meet in one cache
@@ -1104,16 +1105,20 @@ static hipError_t launch_join(const SharedAttnArgs &a, hipStream_t s) {
 
 hipError_t launch_shared_attention(const SharedAttnArgs &args, hipStream_t s) {
     SharedAttnArgs a = args;
+    auto launch = [&](int prefix_cols, int64_t groups) {
+        a.groups = (uint32_t)groups;
+        return launch_head(a, prefix_cols, a.own_cols, groups, s);
+    };
     if (a.prefix_groups64 + a.own_groups64 > 0x7fffffff) return hipErrorInvalidValue;
     hipError_t e;
     if (a.through) {
-        e = launch_head(a, a.own_cols, a.own_cols, a.own_groups64, s);
+        e = launch(a.own_cols, a.own_groups64);
     } else if (a.prefix_cols == a.own_cols || (a.prefix_cols == 32 && a.own_cols == 16)) {  // in one launch
-        e = launch_head(a, a.prefix_cols, a.own_cols, a.prefix_groups64 + a.own_groups64, s);
+        e = launch(a.prefix_cols, a.prefix_groups64 + a.own_groups64);
     } else {
-        e = launch_head(a, a.prefix_cols, a.prefix_cols, a.prefix_groups64, s);
+        e = launch(a.prefix_cols, a.prefix_groups64);
         a.prefix_groups = 0;
-        if (e == hipSuccess) e = launch_head(a, a.own_cols, a.own_cols, a.own_groups64, s);
+        if (e == hipSuccess) e = launch(a.own_cols, a.own_groups64);
     }
     if (e != hipSuccess) return e;
     if (a.prefix_parts == 0 && a.own_parts == 1) return hipSuccess;  // every row is written by its only part
