@@ -87,7 +87,8 @@ int spec_k_rope_cache(const void *q, int64_t ldq, int32_t nq, const void *k, int
  * behind a sequence's end, or at positions that a row does not see, does not reach that row, NaN and infinities included; a row that sees one
  * has NaN or an infinity in its channel (a key's: in its whole head).
  * 8 <= hd <= 256, hd % 8 == 0; nq a multiple of nkv, at most 65536; 1 <= n_seq <= 4096; scale > 0; prefix_len and table_pages * page_tokens below
- * 2^30 (table_pages may be 0: prefix alone); R * nq <= 2^30.  Scores times 1.45 have to stay within fp32's range.  workspace: device scratch, 16-byte aligned, of at least
+ * 2^30 (table_pages may be 0: prefix alone); R * nq <= 2^30.  q . k has to stay within fp32's range,
+ * and so have values times 2^9 and the number of positions seen.  workspace: device scratch, 16-byte aligned, of at least
  * spec_k_attn_shared_workspace() bytes for these sizes (0: NULL will do).  The same call gives the same bits every time. */
 int spec_k_attn_shared(const void *q, int64_t ldq, int32_t nq, int32_t nkv, int32_t hd, int32_t dtype, int32_t R,
                        const int32_t *row_start, int32_t n_seq, const void *k_pages, const void *v_pages, int32_t n_pages,

@@ -18,6 +18,7 @@
 #include <cstdlib>
 #include <cstring>
 #include <chrono>
+#include <limits>
 #include <map>
 #include <mutex>
 #include <new>
@@ -1949,6 +1950,7 @@ int spec_k_attn_shared(const void *q, int64_t ldq, int32_t nq, int32_t nkv, int3
         return refuse(SPEC_EINVAL, "attn_shared: fp32 or bf16; hd a multiple of 8 up to 256, nq one of nkv up to 65536, 1 to 4096 sequences, R * nq up to 2^30, prefix and tables below 2^30 positions");
     a.scale2 = (float)((double)scale * 1.4426950408889634);
     if (!(scale > 0.f) || !(a.scale2 > 0.f) || !std::isfinite(a.scale2)) return refuse(SPEC_EINVAL, "attn_shared: scale must be positive and finite");
+    a.lift = (float)std::min(8.0 / (double)a.scale2, (double)std::numeric_limits<float>::max());
     if (ldq < (int64_t)nq * hd || ldo < (int64_t)nq * hd || workspace_bytes < 0) return refuse(SPEC_EINVAL, "attn_shared: row stride below the heads' width");
     if (R == 0) return SPEC_OK;
     if (!q || !out || !row_start || !own_len || !k_pages || !v_pages || (prefix_len && !prefix_table) || (table_pages && !table))

@@ -275,6 +275,7 @@ struct SharedAttnArgs {
     int32_t prefix_len, table_pages;
     bool q_whole;     // query rows can be read in 16-byte vectors
     float scale2;     // scale * log2(e)
+    float lift;       // 8 / scale2: how far a score may lie above its column's reference
     // what plan_shared_attention() lays down
     int32_t prefix_cols, own_cols, prefix_parts, prefix_chunk, own_parts;  // columns of a workgroup, parts along the positions
     bool through;     // a workgroup goes through the prefix and the own positions of its columns
@@ -282,7 +283,7 @@ struct SharedAttnArgs {
     uint32_t groups;  // workgroups of a launch that have work
     int64_t prefix_groups64, own_groups64;
     float *part_o;    // [R][nq][parts][hd]
-    float *part_ml;   // [R][nq][parts][2]: maximum (times scale2), sum
+    float *part_ml;   // [R][nq][parts][2]: reference (a score not yet scaled), sum
 };
 
 constexpr int VERIFY_TILE = 512;  // elements of a row that one wave sums

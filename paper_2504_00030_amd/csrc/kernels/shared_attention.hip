@@ -487,11 +487,16 @@ __device__ __forceinline__ int64_t element(const SharedAttnArgs &a, int page, in
 // Reference, sum and results of a wave's columns.  Weights are powers of two over a reference, which follows the maximum
 // at a distance: it moves when a score (in powers of two) lies more than 8 above it.  Weights stay below 2^8, which costs no
 // precision, and most tiles need neither the exchange between lanes nor the rescaling.
+// An exponent is one multiply-add, s * scale2 - m * scale2: rounding the second product moves a reference below FAR by 2^-14
+// at most, in the range of what rounding the scores themselves does, but beyond it would grow past the range of the weights.
+// There every tile looks at its maximum, and the reference is taken off before the scaling.
 template <class C>
 struct Running {
     static constexpr int QT = C::QT, NO = C::NB * C::W;
-    float m[QT], base[QT];  // the reference: -infinity and 0 before there is one
-    float bound[QT];        // scores, not yet scaled, that move it
+    static constexpr float FAR = 1024.f;
+    float m[QT];      // the reference, a score not yet scaled: -infinity before there is one
+    float base[QT];   // scaled; 0 before there is one and beyond FAR
+    float bound[QT];  // scores, not yet scaled, that move it
     f4_t l[QT], o[QT][NO];
     __device__ __forceinline__ void clear() {
 #pragma unroll
@@ -503,7 +508,7 @@ struct Running {
             for (int i = 0; i < NO; ++i) o[t][i] = l[t];
         }
     }
-    __device__ __forceinline__ void follow(const f4_t (&s)[QT][2], float scale2) {
+    __device__ __forceinline__ void follow(f4_t (&s)[QT][2], float scale2, float lift) {
         float top[QT];
         bool above = false;
 #pragma unroll
@@ -516,12 +521,15 @@ struct Running {
         if (__ballot(above)) {
 #pragma unroll
             for (int t = 0; t < QT; ++t) {
-                const float to = fmaxf(m[t], group_max(top[t]) * scale2);
-                const float ref = to == -INFINITY ? 0.f : to, by = exp2_(m[t] - ref);
+                const float to = fmaxf(m[t], group_max(top[t]));
+                const float ref = to == -INFINITY ? 0.f : to, by = exp2_((m[t] - ref) * scale2), scaled = ref * scale2;
+                const bool far = fabsf(scaled) >= FAR;
                 m[t] = to;
-                base[t] = ref;
-                bound[t] = (to + 8.f) * __builtin_amdgcn_rcpf(scale2);
+                base[t] = far ? 0.f : scaled;
+                bound[t] = far ? -INFINITY : to + lift;
                 l[t] *= by;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) s[t][i / 4][i % 4] -= far ? ref : 0.f;
 #pragma unroll
                 for (int i = 0; i < NO; ++i) o[t][i] *= by;
             }
@@ -613,7 +621,7 @@ __device__ __forceinline__ void walk(const SharedAttnArgs &a, const Piece &p, C 
             }
             if (__ballot(bad)) odd = 1;
         }
-        run.follow(s, a.scale2);
+        run.follow(s, a.scale2, a.lift);
         typename C::Weights w[QT];
         run.weigh(s, a.scale2, w);
         run.add(core, w);
@@ -697,7 +705,7 @@ __device__ __forceinline__ void split(const SharedAttnArgs &a, float (*so)[16][C
         for (int w = 0; w < 4; ++w) top = fmaxf(top, sm[w][16 * t + my]);
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
-            f[w] = exp2_(sm[w][16 * t + my] - (top == -INFINITY ? 0.f : top));
+            f[w] = exp2_((sm[w][16 * t + my] - (top == -INFINITY ? 0.f : top)) * a.scale2);
             sum += f[w] * sl[w][16 * t + my];
         }
         const int row = whole.row0 + col / a.g, head = whole.h * a.g + col % a.g;
@@ -847,7 +855,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES / 4) void attn_share_k(const Shar
             auto vst = [&](auto n) -> uint8_t * { return n % 3 == 0 ? v0 : n % 3 == 1 ? v1 : v2; };
             // one half of a stage, whose scores are there; `next` computes those of the half behind it meanwhile
             auto half_step = [&](const uint8_t *vs, int half, f4_t (&x)[QT][2], auto next) {
-                run.follow(x, a.scale2);
+                run.follow(x, a.scale2, a.lift);
                 next();
                 typename C::Weights w[QT];
                 run.weigh(x, a.scale2, w);
@@ -897,7 +905,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES / 4) void attn_share_k(const Shar
                 }
                 core.forget(keep);
                 if (__ballot(core.clean(apart))) odd = 1;
-                run.follow(s[0], a.scale2);
+                run.follow(s[0], a.scale2, a.lift);
                 typename C::Weights w[QT];
                 run.weigh(s[0], a.scale2, w);
                 run.add(core, w);
@@ -957,7 +965,7 @@ __global__ __launch_bounds__(256) void attn_join_k(const SharedAttnArgs a) {
     if (lane + 64 < n) y = *reinterpret_cast<const f2_t *>(ml + 2 * lane + 128);
     const float top = wave_max(fmaxf(x[0], y[0])), base = top == -INFINITY ? 0.f : top;
     // (a part without positions seen has weight 0 and holds zeros)
-    const float f = exp2_(x[0] - base), f2 = exp2_(y[0] - base), sum = wave_sum(f * x[1] + f2 * y[1]);
+    const float f = exp2_((x[0] - base) * a.scale2), f2 = exp2_((y[0] - base) * a.scale2), sum = wave_sum(f * x[1] + f2 * y[1]);
     const int ch = 4 * (lane % LPP), which = lane / LPP;
     f4_t acc = {0.f, 0.f, 0.f, 0.f};
     for (int i0 = 0; i0 < n; i0 += 4 * (64 / LPP)) {

@@ -3,8 +3,9 @@ import numpy as np
 import pytest
 import torch
 
+import batch_reference as ref
 import paper_2504_00030_amd as pk
-from test_gpu_batch import BF16, F32, Attn, _int, _stream
+from test_gpu_batch import BF16, F32, HALF_STEP, Attn, _int, _np, _stream
 
 pytestmark = pytest.mark.gpu
 
@@ -47,3 +48,54 @@ def test_attention_of_a_prefix_alone_in_more_than_2_to_the_20_workgroups():
         rel = 2 * ((hd + 4) * size + 1) * 2.0 ** -23 + (4 * prefix + 16) * 2.0 ** -23
         err = (out[r: r + 32768].double().transpose(0, 1) - want).abs()
         assert (err <= rel * mag + 2.0 ** -24 * want.abs()).all(), f"rows from {r}: off by {err.max():.3g}"
+
+
+# ---- attention: scores of any size ---------------------------------------------------------------------------------
+# Scores here are exact: one channel of powers of two (queries) times small whole numbers (keys).  A weight is then off by the two
+# roundings of its exponent, 2^-24 of it each (times ln 2; what is left of a weight 2^-a times a is below 0.54), by exp2's 2^-23 and
+# by half a step of the reference times the scale, 2^-14 where that is below 2^10 and none beyond; numerator and sum: 2^-12 in all.
+SPLIT_AND_SHARED = [([5], [700], 300, 2), ([4], [200], 100, 1), ([20, 3], [60, 400], 100, 1), ([48], [300], 260, 1), ([70], [400], 100, 1),
+                    ([150], [300], 300, 1), ([1] * 100, [20] * 100, 70, 2)]
+
+
+def _near(a, got, scale, n_most):
+    want, mag, _, _ = ref.attention(_np(a.q), _np(a.k), _np(a.v), a.row_start, a.table, a.own, a.prefix_table, a.prefix, scale, np.full(got.shape, 3.0))
+    half = HALF_STEP[a.dtype]
+    rel = 2.0 ** -12 + (4 * n_most + 16) * 2.0 ** -23 + (2.0 ** -8 if a.dtype == BF16 else 0.0)
+    err, tol = np.abs(got - want), rel * mag * (1 + half) + half * np.abs(want)
+    assert (err <= tol).all(), f"{np.count_nonzero(~(err <= tol))} of {err.size} beyond the tolerance, worst {np.nanmax(err):.3g}"
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("order", ["rising", "falling", "any"])
+@pytest.mark.parametrize("rows,own,prefix,heads", SPLIT_AND_SHARED)
+def test_attention_with_scores_of_any_size(rows, own, prefix, heads, order, dtype):
+    """Scores up to 2^127, rows of small and large ones side by side, maxima that repeat."""
+    for hd, scale in ((64, None), (40, 0.37), (32, 2.0 ** 40)):  # (the last: scaled, they leave fp32's range)
+        a = Attn(sum(rows), rows, own, prefix, heads, heads, hd, 16, dtype, junk=0.0)
+        for b, table in [(None, a.prefix_table)] + list(enumerate(a.table)):
+            n = prefix if b is None else own[b]
+            j = a.rng.integers(-100, 101, n)
+            j = j if order == "any" else np.sort(j) if order == "rising" else np.sort(j)[::-1]
+            for p in range(n):
+                a.k[int(table[p // 16]), :, p % 16] = 0.0
+                a.k[int(table[p // 16]), :, p % 16, 3] = float(j[p])
+        a.q[:] = 0.0
+        powers = torch.tensor([-6, 4, 8, 14, 23, 30, 34, 40, 60, 100, 120])
+        at = torch.from_numpy(a.rng.integers(0, len(powers), a.q.shape[:2]))
+        a.q[:, :, 3] = torch.where(torch.from_numpy(a.rng.random(a.q.shape[:2]) < 0.3), -1.0, 1.0).to(dtype) * (2.0 ** powers[at].double()).to(dtype)
+        got = _np(a.run(scale=scale))
+        _near(a, got, hd ** -0.5 if scale is None else scale, prefix + max(own))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("rows,own,prefix,heads", SPLIT_AND_SHARED)
+def test_attention_with_scores_that_differ_by_little_of_their_size(rows, own, prefix, heads, dtype):
+    """Scores of 2^24 and an even number below 256, all exact, times 2^-6: weights over a factor of 50 far from zero."""
+    a = Attn(sum(rows), rows, own, prefix, heads, heads, 64, 16, dtype, junk=0.0)
+    a.k[:] = 0.0
+    a.k[..., 0] = 2.0 ** 12
+    a.k[..., 1] = torch.from_numpy(2.0 * a.rng.integers(0, 128, a.k.shape[:3])).to(dtype)
+    a.q[:] = 0.0
+    a.q[..., 0], a.q[..., 1] = 2.0 ** 12, 1.0
+    _near(a, _np(a.run(scale=2.0 ** -6)), 2.0 ** -6, prefix + max(own))
