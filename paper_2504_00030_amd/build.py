@@ -81,13 +81,24 @@ def build(verbose: bool = True, jobs: int = 8) -> str:
             raise RuntimeError(f"{src}: " + "\n".join(bad[:10]))
         return src + " (matrix-instruction guard)", ""
 
+    def guard_operands(src):
+        # a third one that ends behind the allocator of the vector registers (its rewriter runs a third time there)
+        cmd = [HIPCC, *HIP_FLAGS, "--cuda-device-only", "-S", os.path.join(CSRC, src), "-o", "-", "-mllvm", "-stop-after=virtregrewriter,2"]
+        with subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.DEVNULL, text=True) as p:
+            bad = isa_guard.undefined_operands(p.stdout)
+        if p.returncode != 0:
+            raise RuntimeError("command failed: " + " ".join(cmd))
+        if bad:
+            raise RuntimeError(f"{src}: {len(bad)} of them\n" + "\n".join(bad[:10]))
+        return src + " (operand guard)", ""
+
     def compile_c(src):
         out = _run(["gcc", *C_FLAGS, "-c", os.path.join(CSRC, src), "-o", _obj(src)])
         return src, out
 
     with ThreadPoolExecutor(max_workers=jobs) as ex:
         futs = [ex.submit(compile_hip, s) for s in hip_sources] + [ex.submit(compile_c, s) for s in C_SOURCES]
-        futs += [ex.submit(guard_hip, s) for s in hip_sources if s in MFMA_SOURCES]
+        futs += [ex.submit(guard, s) for guard in (guard_hip, guard_operands) for s in hip_sources if s in MFMA_SOURCES]
         for f in futs:
             src, out = f.result()
             if verbose:

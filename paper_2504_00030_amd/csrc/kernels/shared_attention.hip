@@ -35,19 +35,9 @@ constexpr int MIN_PART = 128; // least positions of a part: a tile for each of a
 constexpr int MAX_PARTS = 64;
 constexpr int STAGE = 64;     // positions of a stage in shared memory
 
-template <int N> struct words { typedef uint32_t type __attribute__((ext_vector_type(N))); };
-template <> struct words<1> { typedef uint32_t type; };
-
-// N words from N * 4-byte aligned memory
-template <int N>
-__device__ __forceinline__ void load_words(const void *p, uint32_t (&w)[N]) {
-    const typename words<N>::type v = *reinterpret_cast<const typename words<N>::type *>(p);
-    if constexpr (N == 1) w[0] = v;
-    else {
-#pragma unroll
-        for (int i = 0; i < N; ++i) w[i] = v[i];
-    }
-}
+// What a lane loads at once stays one vector: words that are loop variables of their own share a register tuple whose elements
+// the compiler may take for undefined (see isa_guard.py).
+template <int N> using words = uint32_t __attribute__((ext_vector_type(N)));
 
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 __device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
@@ -74,7 +64,7 @@ struct CoreBf16 {
     __device__ __forceinline__ static int channel(int i, int r, int g) { return 16 * W * (i / W) + W * (4 * g + r) + i % W; }
     b8_t q[QT][KC];
     u4_t k[2][KC];            // positions lane % 16 of the tile's two sixteens, channels 32 c + 8 g ..
-    uint32_t v[8][NB][W / 2]; // positions 4 g + i of the first (i < 4) and second sixteen, channels W (lane % 16) ..
+    words<W / 2> v[8][NB];    // positions 4 g + i of the first (i < 4) and second sixteen, channels W (lane % 16) ..
 
     __device__ __forceinline__ void load_q(int t, const T *row, bool whole, int hd, int g) {
 #pragma unroll
@@ -105,11 +95,7 @@ struct CoreBf16 {
 #pragma unroll
             for (int n = 0; n < NB; ++n) {
                 const int ch = 16 * W * n + W * c16;
-                if (EXACT || ch < hd) load_words<W / 2>(rows + i * (EXACT ? HDP : hd) + ch, v[4 * s + i][n]);
-                else {
-#pragma unroll
-                    for (int w = 0; w < W / 2; ++w) v[4 * s + i][n][w] = 0;
-                }
+                v[4 * s + i][n] = EXACT || ch < hd ? *reinterpret_cast<const words<W / 2> *>(rows + i * (EXACT ? HDP : hd) + ch) : words<W / 2>(0);
             }
     }
     __device__ __forceinline__ void scores(int t, f4_t (&s)[2]) const {
@@ -122,9 +108,7 @@ struct CoreBf16 {
     }
     __device__ __forceinline__ void forget(int i, bool keep) {
 #pragma unroll
-        for (int n = 0; n < NB; ++n)
-#pragma unroll
-            for (int w = 0; w < W / 2; ++w) v[i][n][w] = keep ? v[i][n][w] : 0u;
+        for (int n = 0; n < NB; ++n) v[i][n] = keep ? v[i][n] : words<W / 2>(0);
     }
     // infinities and NaN of row i of this lane's values become zeros (where `on`); whether there were any
     __device__ __forceinline__ bool clean(int i, bool on) {
@@ -133,9 +117,9 @@ struct CoreBf16 {
         for (int n = 0; n < NB; ++n)
 #pragma unroll
             for (int w = 0; w < W / 2; ++w) {
-                uint32_t &x = v[i][n][w];
+                const uint32_t x = v[i][n][w];
                 const bool lo = on && (x & 0x7f80u) == 0x7f80u, hi = on && (x & 0x7f800000u) == 0x7f800000u;
-                x &= (lo ? 0xffff0000u : 0xffffffffu) & (hi ? 0x0000ffffu : 0xffffffffu);
+                v[i][n][w] = x & (lo ? 0xffff0000u : 0xffffffffu) & (hi ? 0x0000ffffu : 0xffffffffu);
                 bad |= lo || hi;
             }
         return bad;
@@ -275,7 +259,7 @@ struct CoreF32 {
     __device__ __forceinline__ static int channel(int i, int r, int g) { return 16 * W * (i / W) + W * (4 * g + r) + i % W; }
     f4_t q[1][KC];   // channels 16 c + 4 g ..
     f4_t k[2][KC];
-    uint32_t v[8][NB][W];
+    words<W> v[8][NB];
 
     __device__ __forceinline__ void load_q(int t, const T *row, bool whole, int hd, int g) {
 #pragma unroll
@@ -305,11 +289,7 @@ struct CoreF32 {
 #pragma unroll
             for (int n = 0; n < NB; ++n) {
                 const int ch = 16 * W * n + W * c16;
-                if (EXACT || ch < hd) load_words<W>(rows + i * (EXACT ? HDP : hd) + ch, v[4 * s + i][n]);
-                else {
-#pragma unroll
-                    for (int w = 0; w < W; ++w) v[4 * s + i][n][w] = 0;
-                }
+                v[4 * s + i][n] = EXACT || ch < hd ? *reinterpret_cast<const words<W> *>(rows + i * (EXACT ? HDP : hd) + ch) : words<W>(0);
             }
     }
     __device__ __forceinline__ void scores(int t, f4_t (&s)[2]) const {
@@ -324,9 +304,7 @@ struct CoreF32 {
     }
     __device__ __forceinline__ void forget(int i, bool keep) {
 #pragma unroll
-        for (int n = 0; n < NB; ++n)
-#pragma unroll
-            for (int w = 0; w < W; ++w) v[i][n][w] = keep ? v[i][n][w] : 0u;
+        for (int n = 0; n < NB; ++n) v[i][n] = keep ? v[i][n] : words<W>(0);
     }
     __device__ __forceinline__ bool clean(int i, bool on) {
         bool bad = false;

@@ -1,16 +1,23 @@
-"""Build-time guard over the compiler's gfx950 assembly of the matrix-core kernels.
+"""Build-time guards over what the compiler makes of the matrix-core kernels for gfx950.
 
+scan(), over the assembly:
 v_mfma ignores the execution mask.  The compiler lowers a branch on a value it cannot prove
 wave-uniform to an exec-mask update, and for short blocks it drops the branch that would skip the
 block when the mask is empty; a matrix instruction in such a block then runs on registers whose loads
 were skipped.  The kernels keep every condition around a matrix instruction scalar; this scan checks
 the result: it fails when a v_mfma sits between a saveexec that no skip branch follows and the
 restore of exec.
+
+undefined_operands(), over the machine code behind the register allocator: elements of one vector that are loop variables of their
+own share a register tuple, and where a loop's exit leaves them undefined, this compiler (ROCm 7.2) notes that for the tuple's
+first element alone.  The allocator then takes the others for undefined inside the loop as well, where they hold values, and
+may give their registers to temporaries: wrong results in some builds and not in others.  It marks such operands "undef".  The
+kernels keep such vectors whole; no matrix instruction in them reads a value that the source left undefined, so any mark is a fault.
 """
 from __future__ import annotations
 
 import re
-from typing import List
+from typing import Iterable, List
 
 _LABEL = re.compile(r"^(_Z\w+):")
 
@@ -43,4 +50,22 @@ def scan(asm_text: str) -> List[str]:
         if ins.startswith("v_mfma") and masked:
             out.append(f"line {ln}: {kernel}: matrix instruction in a masked block without a skip branch "
                        f"(exec narrowed at line {masked})")
+    return out
+
+
+_FUNCTION = re.compile(r"^name:\s+(\S+)")
+_UNDEF = re.compile(r"\bundef \$[av]gpr\d+")
+
+
+def undefined_operands(mir: Iterable[str]) -> List[str]:
+    """One message per matrix instruction with a source register that the allocator takes for undefined, from the lines of the
+    machine code printed behind it."""
+    out: List[str] = []
+    kernel = "?"
+    for line in mir:
+        m = _FUNCTION.match(line)
+        if m:
+            kernel = m.group(1)
+        elif "V_MFMA" in line and _UNDEF.search(line):
+            out.append(f"{kernel}: operand taken for undefined: {line.strip()[:120]}")
     return out
