@@ -84,8 +84,10 @@ int spec_k_rope_cache(const void *q, int64_t ldq, int32_t nq, const void *k, int
  * prefix_len is 0).  The own positions begin with a page of their own, wherever the prefix ends.  Rows in front of row_start[0]
  * and from row_start[n_seq] on are left as they were.  Bounds in device memory are never trusted: rows are those within 0 .. R,
  * own_len counts at most table_pages * page_tokens, and positions on pages outside the pool are not seen.  What lies in the pages
- * behind a sequence's end, or at positions that a row does not see, does not reach that row, NaN and infinities included; a row that sees one
- * has NaN or an infinity in its channel (a key's: in its whole head).
+ * behind a sequence's end, or at positions that a row does not see, does not reach that row, NaN and infinities included.  A row
+ * that sees a value that is one has NaN or an infinity in its channel.  A key's count by their scores: a row with a score that is NaN or
+ * plus infinity has NaN in its whole head, and a position whose score is minus infinity has weight 0 (a row whose scores are
+ * all of that kind gets zeros, as if it saw none).
  * 8 <= hd <= 256, hd % 8 == 0; nq a multiple of nkv, at most 65536; 1 <= n_seq <= 4096; scale > 0; prefix_len and table_pages * page_tokens below
  * 2^30 (table_pages may be 0: prefix alone); R * nq <= 2^30.  q . k has to stay within fp32's range,
  * and so have values times 2^9 and the number of positions seen.  workspace: device scratch, 16-byte aligned, of at least

@@ -99,3 +99,48 @@ def test_attention_with_scores_that_differ_by_little_of_their_size(rows, own, pr
     a.q[:] = 0.0
     a.q[..., 0], a.q[..., 1] = 2.0 ** 12, 1.0
     _near(a, _np(a.run(scale=2.0 ** -6)), 2.0 ** -6, prefix + max(own))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("rows,own,prefix,nq,nkv,hd", [([6, 4], [40, 4], 30, 4, 2, 64), ([4, 2], [4, 70], 0, 2, 2, 40), ([20, 3], [600, 3], 300, 2, 1, 128),
+                                                       ([80, 70], [100, 70], 70, 2, 2, 64), ([150, 30], [400, 30], 0, 1, 1, 32), ([70], [90], 200, 4, 1, 96)])
+def test_attention_with_infinities_in_keys(rows, own, prefix, nq, nkv, hd, dtype):
+    """Scores of plus infinity make their head NaN, those of minus infinity have weight 0; queries of both signs."""
+    a = Attn(sum(own) + hd, rows, own, prefix, nq, nkv, hd, 16, dtype)
+    spoilt = [(a.table[b], j) for b, n in enumerate(own) for j in (0, n // 2, n - 1)] + [(a.prefix_table, j) for j in range(3, prefix, 100)]
+    for table, j in spoilt:
+        a.k[int(table[j // 16]), :, j % 16, 3] = -float("inf")  # (minus infinity where the query is positive)
+    got, q, k, v = _np(a.run()), _np(a.q), _np(a.k), _np(a.v)
+    half, kinds = HALF_STEP[dtype], [0, 0, 0]  # heads that are NaN, zeros, numbers
+    for b, n in enumerate(rows):
+        for i in range(n):
+            at = [(a.prefix_table[j // 16], j % 16) for j in range(prefix)] + [(a.table[b, j // 16], j % 16) for j in range(own[b] - n + i + 1)]
+            pages, places = np.array(at).T
+            for h in range(nq):
+                r = a.row_start[b] + i
+                kk, vv, x = k[pages, h // (nq // nkv), places], v[pages, h // (nq // nkv), places], got[r, h]
+                s = kk @ q[r, h] * a.scale
+                some = s > -np.inf
+                kinds[0 if np.isnan(s).any() or (s == np.inf).any() else 1 if not some.any() else 2] += 1
+                if np.isnan(s).any() or (s == np.inf).any():
+                    assert np.isnan(x).all()
+                elif not some.any():
+                    assert (x == 0).all()
+                else:
+                    w = np.exp(s[some] - s[some].max())
+                    w /= w.sum()
+                    want, mag, m = w @ vv[some], w @ np.abs(vv[some]), len(w)
+                    size = (np.abs(kk[some]) @ np.abs(q[r, h])).max() * a.scale
+                    rel = 2 * ((hd + 4) * size + 1) * 2.0 ** -23 + (4 * m + 16) * 2.0 ** -23 + (2.0 ** -8 if dtype == BF16 else 0.0)
+                    assert (np.abs(x - want) <= rel * mag * (1 + half) + half * np.abs(want)).all()
+    assert kinds[0] and kinds[2]
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("rows,own,prefix", [([5], [9], 0), ([3, 1], [700, 4], 300), ([80], [90], 70), ([150], [150], 0)])
+def test_attention_of_rows_whose_scores_are_all_minus_infinity(rows, own, prefix, dtype):
+    a = Attn(sum(own), rows, own, prefix, 2, 2, 64, 16, dtype, extra_rows=1)
+    a.k[..., 7] = -float("inf")
+    a.q[..., 7] = a.q[..., 7].abs() + 0.5
+    got = _np(a.run())
+    assert (got[:-1] == 0).all() and (got[-1] == 3.0).all()
