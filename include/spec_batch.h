@@ -52,8 +52,8 @@ typedef struct {
 } spec_rope;
 
 /* rope_cos[p][j] = cos(p * f_j), rope_sin[p][j] = sin(p * f_j) for p < n_pos, j < rot / 2 (times the magnitude with
- * SPEC_ROPE_RAMP); angles in 64 bits, results rounded once: off by half a step of fp32 and 1e-15 * (1 + p * f_j).  Tables: device fp32
- * [n_pos][rot / 2], as spec_k_rope_cache and spec_k_qk_norm_rope read them.  rope: host, read by the call.  rot even, 2 to
+ * SPEC_ROPE_RAMP); f_j as arithmetic in 64 bits gives it, angles in 64 bits, results rounded once: off by half a step of fp32 and by
+ * 7e-15 + 1e-15 * p * f_j (times the magnitude).  Tables: device fp32 [n_pos][rot / 2], as spec_k_rope_cache and spec_k_qk_norm_rope read them.  rope: host, read by the call.  rot even, 2 to
  * 512; 1 <= n_pos <= 2^28. */
 int spec_k_rope_tables(const spec_rope *rope, int32_t rot, int32_t n_pos, float *rope_cos, float *rope_sin, void *stream);
 

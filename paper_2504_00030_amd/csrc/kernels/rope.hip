@@ -56,8 +56,8 @@ __device__ __forceinline__ void store_v(T *p, const float (&v)[V]) {
 
 // ---- tables --------------------------------------------------------------------------------------------------------
 // cos(p f_j), sin(p f_j) of STRIP positions of one pair a thread: the first position's angle and the step's by the 64-bit
-// functions, the others by the addition theorem in 64 bits (each step adds less than 2^-51 to the error; the angle's own
-// rounding, p f_j 2^-53, is as large at the first position already).  Bound by the writes (131072 x 64: 12.8 us, 5.2 TB/s) or, for
+// functions, the others by the addition theorem in 64 bits (each of the fifteen steps adds less than 2^-51 to the error, 7e-15 together;
+// the angle's own rounding is p f_j 2^-53).  Bound by the writes (131072 x 64: 12.8 us, 5.2 TB/s) or, for
 // short tables, by two evaluations of sine and cosine (512 x 16: 3.1 us).
 template <int STRIP>
 __global__ __launch_bounds__(256) void rope_tables_k(const RopeTableArgs a) {

@@ -144,3 +144,21 @@ def test_attention_of_rows_whose_scores_are_all_minus_infinity(rows, own, prefix
     a.q[..., 7] = a.q[..., 7].abs() + 0.5
     got = _np(a.run())
     assert (got[:-1] == 0).all() and (got[-1] == 3.0).all()
+
+
+# ---- tables --------------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("magnitude", [1.0, 3e5])
+@pytest.mark.parametrize("every", [30, 62, 7, 1000])
+def test_tables_where_cosines_and_sines_vanish(every, magnitude):
+    """Half a turn every few positions: what is left there are the angles' and the recurrence's own errors, magnitude * (7e-15 + 1e-15 of
+    the angle), beside half a step of fp32.  (The ramp interpolates its second pair here, which turns less than twice over the context.)"""
+    n_pos, theta = 4099, 2.0
+    factor = theta ** -0.5 * every / np.pi
+    cos, sin = torch.zeros((n_pos, 2), device="cuda"), torch.zeros((n_pos, 2), device="cuda")
+    pk.k_rope_tables(cos, sin, theta=theta, scaling="ramp", factor=factor, low=2.0, high=3.0, context=1.0, magnitude=magnitude, stream=_stream())
+    f, size = ref.frequencies(4, theta, scaling="ramp", factor=factor, low=2.0, high=3.0, context=1.0, magnitude=magnitude)
+    assert size == magnitude and abs(f[1] * every - np.pi) < 1e-14
+    ang = np.arange(n_pos).astype(np.longdouble)[:, None] * f.astype(np.longdouble)[None, :]
+    for got, want in ((_np(cos), np.cos(ang) * magnitude), (_np(sin), np.sin(ang) * magnitude)):
+        err = np.abs(got.astype(np.longdouble) - want)
+        assert (err <= 2.0 ** -24 * np.abs(want) + magnitude * (7e-15 + 1e-15 * ang)).all(), float((err / magnitude).max())
