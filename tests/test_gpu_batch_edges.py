@@ -5,7 +5,7 @@ import torch
 
 import batch_reference as ref
 import paper_2504_00030_amd as pk
-from test_gpu_batch import BF16, F32, HALF_STEP, Attn, _int, _np, _stream
+from test_gpu_batch import BF16, F32, HALF_STEP, Attn, _int, _np, _stream, _verify
 
 pytestmark = pytest.mark.gpu
 
@@ -162,3 +162,47 @@ def test_tables_where_cosines_and_sines_vanish(every, magnitude):
     for got, want in ((_np(cos), np.cos(ang) * magnitude), (_np(sin), np.sin(ang) * magnitude)):
         err = np.abs(got.astype(np.longdouble) - want)
         assert (err <= 2.0 ** -24 * np.abs(want) + magnitude * (7e-15 + 1e-15 * ang)).all(), float((err / magnitude).max())
+
+
+# ---- verification --------------------------------------------------------------------------------------------------
+BORDERS = [1, 7, 8, 63, 64, 100, 511, 512, 513, 4096, 7680, 8191]
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("tail", [0, 808])
+def test_verification_draws_exactly_on_borders(tail, dtype):
+    """Equal weights 2^-13 and u = x 2^-13, all exact: the sum of the first x weights does not exceed u times all of them, so the draw is
+    x; the next smaller u draws x - 1.  Rows of no draft, residuals of a refused draft, and the token left out of a looked-up one."""
+    V, n = 8192 + tail, len(BORDERS)
+    below = np.nextafter(np.float32(BORDERS) * np.float32(2.0 ** -13), np.float32(0))
+    p = torch.zeros((n, V), dtype=dtype)
+    p[:, :8192] = 2.0 ** -13
+    A, y = _verify(p, None, [0] * n, np.array([], dtype=int), np.array([]), np.float32(BORDERS) * np.float32(2.0 ** -13))
+    assert A.tolist() == [0] * n and y.tolist() == BORDERS
+    assert _verify(p, None, [0] * n, np.array([], dtype=int), np.array([]), below)[1].tolist() == [x - 1 for x in BORDERS]
+    # one draft each, refused: u q = p exactly; the residual is 2^-13 on 8192 tokens again
+    p, q = torch.zeros((2 * n, V), dtype=dtype), torch.zeros((n, V), dtype=dtype)
+    p[:, :8192], q[:, :8192] = 2.0 ** -12, 2.0 ** -13
+    drafted = np.full(n, 5)
+    A, y = _verify(p, q, [1] * n, drafted, np.full(n, 2.0), np.float32(BORDERS) * np.float32(2.0 ** -13))
+    assert A.tolist() == [0] * n and y.tolist() == BORDERS
+    assert _verify(p, q, [1] * n, drafted, np.full(n, 2.0), below)[1].tolist() == [x - 1 for x in BORDERS]
+    # looked up: the drafted token, here the first, weighs nothing, 8192 others do
+    p = torch.zeros((2 * n, V + 1), dtype=dtype)
+    p[:, :8193] = 2.0 ** -13
+    A, y = _verify(p, None, [1] * n, np.zeros(n, dtype=int), np.full(n, 2.0 ** -13), np.float32(BORDERS) * np.float32(2.0 ** -13))
+    assert A.tolist() == [0] * n and y.tolist() == [x + 1 for x in BORDERS]
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_verification_accepts_below_the_border_alone(dtype):
+    """u q < p: at u = 0 any p above zero accepts and none at zero does, at u = p / q nothing, at the next smaller u the draft."""
+    V = 600
+    p, q = torch.zeros((10, V), dtype=dtype), torch.zeros((5, V), dtype=dtype)
+    least = 2.0 ** -149 if dtype == F32 else 2.0 ** -133
+    for b, (px, qx) in enumerate([(least, 1.0), (0.0, 1.0), (0.25, 0.5), (0.25, 0.5), (0.5, 0.25)]):
+        p[2 * b, 300 + b], q[b, 300 + b], p[2 * b, 7], p[2 * b + 1, 9] = px, qx, 1.0, 1.0
+    u = np.array([0.0, 0.0, 0.5, 0.0, 1.0], dtype=np.float32)
+    u[3] = np.nextafter(np.float32(0.5), np.float32(0))
+    A, y = _verify(p, q, [1] * 5, np.arange(300, 305), u, np.zeros(5))
+    assert A.tolist() == [1, 0, 0, 1, 1] and y.tolist() == [9, 7, 7, 9, 9]
