@@ -206,3 +206,39 @@ def test_verification_accepts_below_the_border_alone(dtype):
     u[3] = np.nextafter(np.float32(0.5), np.float32(0))
     A, y = _verify(p, q, [1] * 5, np.arange(300, 305), u, np.zeros(5))
     assert A.tolist() == [1, 0, 0, 1, 1] and y.tolist() == [9, 7, 7, 9, 9]
+
+
+# ---- attention: weights in two terms -------------------------------------------------------------------------------
+@pytest.mark.parametrize("g", [1, 20])  # 16 and 32 columns a workgroup
+@pytest.mark.parametrize("hd", [8, 32, 64, 128, 200])
+@pytest.mark.parametrize("n", [5, 40, 150])  # (the last in two parts)
+def test_attention_of_few_columns_keeps_weights_in_two_terms(n, hd, g):
+    """Values that cancel under the weights: what is left of a result shows how exact the weights are.  Two bf16 terms leave 2^-8 of
+    2^-8, 2^-16 of a weight, numerator and sum each: 2^-15 of sum p |v| in all; one term would leave far more, which is checked too."""
+    a = Attn(n + hd + g, [1, 1], [n, n], 0, 2 * g, 2, hd, 16, BF16)
+    a.q = a.q.reshape(2, 2, g, hd)[:, :, :1].repeat(1, 1, g, 1).reshape(2, 2 * g, hd)  # one query for all heads of a cache head
+    a.q *= 0.5
+    one_term_fails = False
+    places = [np.array([(a.table[b, j // 16], j % 16) for j in range(n)]).T for b in range(2)]
+    for b, (pages, at) in enumerate(places):
+        for h in range(2):
+            s = _np(a.k)[pages, h, at] @ _np(a.q)[b, h * g] * a.scale
+            w = np.exp(s - s.max())
+            order = np.argsort(w)[::-1]
+            v = _np(a.v)[pages, h, at]
+            for j in (order[0], order[1], order[1]):  # the two heaviest positions take what the others leave
+                x = v[j] - (w @ v) / w[j]
+                v[j] = _np(torch.from_numpy(x).to(BF16))
+            a.v[torch.from_numpy(pages), h, torch.from_numpy(at)] = torch.from_numpy(v).to(BF16)
+    got = _np(a.run())
+    want, mag, m, size = ref.attention(_np(a.q), _np(a.k), _np(a.v), a.row_start, a.table, a.own, a.prefix_table, 0, a.scale, got)
+    rel = 2 * ((hd + 4) * size + 1) * 2.0 ** -23 + (4 * m + 16) * 2.0 ** -23 + 2.0 ** -15
+    tol = rel * mag * (1 + 2.0 ** -8) + 2.0 ** -8 * np.abs(want)
+    err = np.abs(got - want)
+    assert (err <= tol).all(), f"worst {np.max(err / tol):.3g} of the tolerance"
+    for b, (pages, at) in enumerate(places):
+        for h in range(2):
+            s = _np(a.k)[pages, h, at] @ _np(a.q)[b, h * g] * a.scale
+            w = _np(torch.from_numpy(np.exp(s - s.max())).to(BF16))
+            one_term_fails |= bool((np.abs(w @ _np(a.v)[pages, h, at] / w.sum() - want[b, h * g]) > tol[b, h * g]).any())
+    assert one_term_fails
