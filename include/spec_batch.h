@@ -77,8 +77,10 @@ int spec_k_rope_cache(const void *q, int64_t ldq, int32_t nq, const void *k, int
  * rows are the last n: its row i sees the prefix and own positions 0 .. own_len[b] - n + i.
  *     o = sum_j softmax_j(scale * q . k_j) v_j  over the positions seen;  a row that sees none gets zeros.
  * q, out: device, dtype, head i of row r at element r * ld + i * hd; query head i reads cache head i / (nq / nkv).  Queries, pages and
- * results have one type: SPEC_BF16 (scores, weights' sums and results are held in fp32; in front of the values' product the weights
- * are rounded to two bf16 terms, or, where a sequence has many rows, to one: 2^-8 of each term at most) or SPEC_F32 (fp32 throughout).
+ * results have one type: SPEC_F32 (fp32 throughout) or SPEC_BF16 (scores, weights' sums and results are held in fp32; in front of the
+ * values' product a weight is rounded to two bf16 terms, off by 2^-16 of itself, or to one, off by 2^-8, in heads of up to 128 elements
+ * where more than 32 columns go through the same positions: rows times nq / nkv, of a sequence on average, or of all of them
+ * for a prefix that no sequence goes through by itself.  Results are then off by 0.0023 of their norm instead of 0.0017).
  * row_start: device int32 [n_seq + 1]; own_len: device int32 [n_seq]; table: device int32 [n_seq][table_pages], the page of own
  * positions p * page_tokens ..; prefix_table: device int32 [ceil(prefix_len / page_tokens)], the pages of the prefix (NULL where
  * prefix_len is 0).  The own positions begin with a page of their own, wherever the prefix ends.  Rows in front of row_start[0]
