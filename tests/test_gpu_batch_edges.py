@@ -50,6 +50,26 @@ def test_attention_of_a_prefix_alone_in_more_than_2_to_the_20_workgroups():
         assert (err <= rel * mag + 2.0 ** -24 * want.abs()).all(), f"rows from {r}: off by {err.max():.3g}"
 
 
+# ---- attention: tables as a server keeps them ----------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("rows,own,prefix,nq,nkv,hd", [([1], [40], 0, 4, 2, 64), ([3, 20, 1], [70, 300, 0], 100, 4, 1, 128), ([70, 3], [70, 900], 0, 2, 2, 64),
+                                                       ([5] * 9, [5, 0, 7, 130, 64, 65, 128, 3, 2], 500, 4, 4, 32), ([130], [140], 300, 2, 1, 80)])
+def test_attention_with_tables_far_longer_than_the_sequences(rows, own, prefix, nq, nkv, hd, dtype):
+    """Parts are planned for 32000 positions a sequence; most hold none, and the pages named there lie outside the pool."""
+    a = Attn(sum(own) + hd, rows, own, prefix, nq, nkv, hd, 16, dtype)
+    wide = np.full((len(own), 2000), 2**31 - 1, dtype=np.int32)
+    wide[:, : a.table.shape[1]] = a.table
+    a.table = wide
+    a.check()
+
+
+def test_attention_of_as_many_sequences_as_there_may_be():
+    rng = np.random.default_rng(1)
+    rows, own = rng.integers(0, 3, 4096).tolist(), rng.integers(0, 20, 4096).tolist()
+    for dtype in (F32, BF16):
+        Attn(2, rows, own, 9, 1, 1, 16, 8, dtype, extra_rows=3).check()
+
+
 # ---- attention: scores of any size ---------------------------------------------------------------------------------
 # Scores here are exact: one channel of powers of two (queries) times small whole numbers (keys).  A weight is then off by the two
 # roundings of its exponent, 2^-24 of it each (times ln 2; what is left of a weight 2^-a times a is below 0.54), by exp2's 2^-23 and
