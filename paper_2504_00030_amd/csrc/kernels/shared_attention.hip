@@ -1022,12 +1022,16 @@ void plan_shared_attention(SharedAttnArgs &a, int64_t own_capacity) {
         a.own_groups64 = (int64_t)a.own_tiles * a.nkv * a.own_parts;
     }
     // A workgroup goes through prefix and own positions by itself, and nothing is left to join, where there are enough of them
-    // without sharing out the prefix (8 x 256 rows behind 8192 positions: 285 us, 307 in parts; few columns, whose prefix would take
-    // a launch of its own: 32 tokens behind 512 + 512 positions 22 and 31, behind 1000 + 1000 43 and 53), or so little to go
-    // through that the second launch would take longer (one token behind 356 positions 7.7 and 8.4, behind 512 10.7 and 8.4).
+    // without sharing out the prefix (8 x 256 rows behind 8192 positions: 285 us, 316 in parts; few columns, whose prefix would take
+    // a launch of its own: 32 tokens behind 512 + 512 positions 21 and 32, behind 1000 + 1000 42 and 53), or so little to go
+    // through that the second launch would take longer.  One token of 32 heads on 8, through and in parts, by positions of
+    // both: heads of 32 (64 bytes) 512 6.6 and 7.6; of 64 448 7.6 and 7.8, 512 8.0 and 7.8; of 128 320 8.6 and 8.8, 384 9.4 and
+    // 8.8; of 256 192 9.9 and 10.2, 256 10.9 and 10.3; fp32 like the bf16 heads of as many bytes.
     const int64_t groups = (a.own_cols >= 64 ? (columns + a.own_cols - 1) / a.own_cols : own_tiles) * a.nkv;
     const bool most = groups >= 192 && (a.own_cols >= 64 || (a.prefix_cols >= 64 && a.prefix_len <= 1024 && own_capacity <= 1024));
-    a.through = a.prefix_len > 0 && own_capacity > 0 && (most || (a.own_cols < 64 && a.prefix_len + own_capacity <= 384));
+    const int64_t bytes = (int64_t)a.hd * (a.dtype == DT_F32 ? 4 : 2);
+    const bool little = a.own_cols < 64 && (a.prefix_len + own_capacity) * (128 + bytes) <= 125000;
+    a.through = a.prefix_len > 0 && own_capacity > 0 && (most || little);
     if (a.through) {
         a.prefix_parts = 0;
         a.prefix_groups64 = 0;
