@@ -748,9 +748,10 @@ __device__ __forceinline__ void copy16(const void *from, uint8_t *to) {
 // memory in stages of 64, three in turn.  The loop is for whole stages that all columns see; the positions behind them, and
 // pieces with pages outside the pool, follow stage by stage.
 // 8 x 256 rows of 32 heads of 128 on 8 behind 8192 positions (256 columns, eight waves of 32): 272 - 288 us, 1.0 PFLOP/s, about 2 us
-// a stage: the matrix units are busy 42 % of the cycles, shared memory 40 %; a SIMD's two waves leave each meeting together, and each issues 16 exponentials, 16 multiply-adds, 8 conversions and 24 LDS
-// reads for its 34 matrix instructions.  Four waves of 64 columns read LDS half as often, but what ends in the second half of
-// the register file has to be moved: 352.  Turning values by permutes costs 32 instructions more: 307.
+// a stage: the matrix units are busy 42 % of the cycles, shared memory 40 %; a SIMD's two waves leave each meeting together, and
+// each issues 16 exponentials, 16 multiply-adds, 8 conversions and 24 LDS reads for its 34 matrix instructions.  Four waves of 64
+// columns read LDS half as often, but what ends in the second half of the register file has to be moved: 352.  Turning values
+// by permutes costs 32 instructions more: 307.
 template <int HDP, int QT, int WAVES, bool EXACT>
 __global__ __launch_bounds__(64 * WAVES, WAVES / 4) void attn_share_k(const SharedAttnArgs a) {
     typedef CoreLds<HDP, QT, EXACT> C;

@@ -12,7 +12,7 @@ undefined_operands(), over the machine code behind the register allocator: eleme
 own share a register tuple, and where a loop's exit leaves them undefined, this compiler (ROCm 7.2) notes that for the tuple's
 first element alone.  The allocator then takes the others for undefined inside the loop as well, where they hold values, and
 may give their registers to temporaries: wrong results in some builds and not in others.  It marks such operands "undef".  The
-kernels keep such vectors whole; no matrix instruction in them reads a value that the source left undefined, so any mark is a fault.
+kernels keep such vectors whole; nothing in them reads a value that the source left undefined, so any marked vector register is a fault.
 """
 from __future__ import annotations
 
@@ -54,18 +54,21 @@ def scan(asm_text: str) -> List[str]:
 
 
 _FUNCTION = re.compile(r"^name:\s+(\S+)")
-_UNDEF = re.compile(r"\bundef \$[av]gpr\d+")
+_UNDEF = re.compile(r"\bundef (?:renamable )?\$[av]gpr\d+")
 
 
 def undefined_operands(mir: Iterable[str]) -> List[str]:
-    """One message per matrix instruction with a source register that the allocator takes for undefined, from the lines of the
-    machine code printed behind it."""
+    """One message per instruction with a source among the vector registers that the allocator takes for undefined, from the lines of
+    the machine code printed behind it."""
     out: List[str] = []
     kernel = "?"
     for line in mir:
-        m = _FUNCTION.match(line)
-        if m:
-            kernel = m.group(1)
-        elif "V_MFMA" in line and _UNDEF.search(line):
-            out.append(f"{kernel}: operand taken for undefined: {line.strip()[:120]}")
+        if "undef" in line:
+            if _UNDEF.search(line.split(" = ", 1)[-1]):  # (in front of it: a result, of which only a part is written)
+                out.append(f"{kernel}: operand taken for undefined: {line.strip()[:120]}")
+        elif line.startswith("name:"):
+            m = _FUNCTION.match(line)
+            kernel = m.group(1) if m else "?"
+    if kernel == "?":
+        out.append("no function in what was printed: the compiler knows another name for the place behind the allocator")
     return out
