@@ -262,3 +262,16 @@ def test_attention_of_few_columns_keeps_weights_in_two_terms(n, hd, g):
             w = _np(torch.from_numpy(np.exp(s - s.max())).to(BF16))
             one_term_fails |= bool((np.abs(w @ _np(a.v)[pages, h, at] / w.sum() - want[b, h * g]) > tol[b, h * g]).any())
     assert one_term_fails
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("rows,own,prefix,heads", SPLIT_AND_SHARED)
+def test_attention_with_scales_at_the_ends_of_fp32(rows, own, prefix, heads, dtype):
+    """A scale below fp32's normal numbers weighs all positions alike; one near its end leaves the largest score alone."""
+    for scale in (1e-42, 1e-38):
+        Attn(sum(rows), rows, own, prefix, heads, heads, 64, 16, dtype).check(scale=scale)
+    a = Attn(sum(rows), rows, own, prefix, heads, heads, 64, 16, dtype, junk=0.0)
+    a.k[:], a.q[:] = 0.0, 0.0
+    a.k[..., 5] = torch.from_numpy(a.rng.integers(0, 101, a.k.shape[:3]).astype(np.float32)).to(dtype)
+    a.q[..., 5] = torch.from_numpy(np.where(a.rng.random(a.q.shape[:2]) < 0.5, -1.0, 1.0).astype(np.float32)).to(dtype)
+    _near(a, _np(a.run(scale=2e38)), 2e38, prefix + max(own))
