@@ -752,8 +752,11 @@ __device__ __forceinline__ void copy16(const void *from, uint8_t *to) {
 // each issues 16 exponentials, 16 multiply-adds, 8 conversions and 24 LDS reads for its 34 matrix instructions.  Four waves of 64
 // columns read LDS half as often, but what ends in the second half of the register file has to be moved: 352.  Turning values
 // by permutes costs 32 instructions more: 307.
+// Heads up to 64 are compiled for two waves a SIMD, also four waves a workgroup: with one, the compiler spreads what fits over both
+// halves of the file and moves it (8 x 256 rows behind 8192 positions, heads of 32: 182 us for 155; 4 sequences of 80 columns,
+// 8000 positions, heads of 64: 35.3 for 32.5).  Larger heads' stages leave room for one workgroup anyway.
 template <int HDP, int QT, int WAVES, bool EXACT>
-__global__ __launch_bounds__(64 * WAVES, WAVES / 4) void attn_share_k(const SharedAttnArgs a) {
+__global__ __launch_bounds__(64 * WAVES, HDP <= 64 ? 2 : WAVES / 4) void attn_share_k(const SharedAttnArgs a) {
     typedef CoreLds<HDP, QT, EXACT> C;
     typedef __bf16 T;
     constexpr int UNITS = C::UNITS, BYTES = STAGE * HDP * 2, SHARE = WAVES * 1024, COPIES = BYTES / SHARE, COLS = 16 * QT * WAVES;
